@@ -264,10 +264,10 @@ def _own_call(case, s):
     from paper_2201_05587_b200 import binding as B
     op = case["op"]
     if op == "quantize":
-        return B.quantize_f8(s["x"], s["q"], s["scales"], block_rows=case["rows"])
+        return B.quantize(s["x"], s["q"], s["scales"], block_rows=case["rows"])
     if op == "dense":
         act = {"none": B.TT_ACT_NONE, "relu": B.TT_ACT_RELU, "gelu": B.TT_ACT_GELU_ERF}[case["act"]]
-        return B.dense_f8(s["x"], s["x_scale"], s["w"], s["w_scale"], s["y"], bias=s["bias"], act=act)
+        return B.dense_quantized(s["x"], s["x_scale"], s["w"], s["w_scale"], s["y"], bias=s["bias"], act=act)
     if op == "rotary":
         table = B.rotary_table(s["frequencies"])
         return B.rotary(s["x"], s["positions"], table, s["y"], interleaved=case["interleaved"], factor=s["factor"], inverse=case["inverse"])
