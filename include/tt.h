@@ -470,6 +470,110 @@ tt_status tt_dense_static_scratch(const void* x, const void* w, const void* bias
                                   int32_t kk, int32_t act, const tt_schedule_record* rec, void* cuda_stream,
                                   int64_t* scratch_bytes_used);
 
+/* ---- 8-bit operators of a transformer's inference pass (no counterpart in the paper) --------------------------------------
+ *
+ * What a program calls that keeps weights, keys and values in e4m3 (one sign, four exponent and three mantissa bits, largest value
+ * 448, no infinities): the dense layer, the quantisation in front of it, rotary positions, and a paged cache with its attention.
+ * Each call takes its arguments in a structure of plain pointers, sizes and strides (in elements, unless stated otherwise; the
+ * innermost axis of every tensor is contiguous), checks them, enqueues one kernel on `cuda_stream` of the current device and returns.
+ * Nothing is kept between calls and no device memory is allocated, so calls may be captured, and calls that share no output, status word
+ * or workspace may run at the same time.  Null pointers, unknown types, sizes that are negative or too large and strides or addresses that a call
+ * cannot take are TT_ERR_INVALID_ARG; what an e4m3 kernel is not built for (a head size, a page size) is TT_ERR_NOT_IMPLEMENTED.
+ * A call with nothing to do (no rows, no tokens) is TT_OK and enqueues nothing.
+ *
+ * What only the device sees (a page number, a length, a wait that gave up) is reported in the status word, a device word that the
+ * caller clears: a kernel that meets such a thing leaves TT_ERR_INVALID_ARG or TT_ERR_TIMEOUT in its low byte,
+ * touches nothing outside the tensors, and the outputs concerned are not to be used.  */
+typedef enum { TT_TYPE_F32 = 0, TT_TYPE_F16 = 1, TT_TYPE_BF16 = 2 } tt_type;
+
+/* q = e4m3(x / s) for blocks of 128 columns and block_rows rows (1: activations, 128: weights), s the smallest power of two, 2^-126 at least,
+ * with |x| <= 448 s for all finite values of the block; rounding to nearest even.  A power of two costs at most one bit of the type's
+ * range and none of its precision, and x / s is exact.  Infinities and NaN become NaN.  s goes to
+ * scales[block * s_block + (row / block_rows) * s_row]. */
+typedef struct tt_quantize_args {
+    const void* x; void* q; float* scales;
+    int64_t x_row, q_row;               /* elements from row to row */
+    int64_t s_row, s_block;
+    int32_t x_type, m, kk, block_rows;
+} tt_quantize_args;
+tt_status tt_quantize(const tt_quantize_args* a, void* cuda_stream);
+
+/* y[m,nn] = act(bias[nn] + sum over blocks b of 128 columns of xs(m,b) ws(nn/128,b) sum_kk x[m,kk] w[nn,kk]): x [m,kk] and w [nn,kk] in e4m3,
+ * xs a scale for each row and block, ws one for each 128 x 128 block, any values.  A block's products are summed by the tensor core,
+ * blocks are added up in 32 bits.  x and w start on 16-byte boundaries and so do their rows (x_row, w_row multiples of 16).
+ * bias may be NULL.  Deterministic. */
+typedef struct tt_dense_quantized_args {
+    const void* x; const void* w; const float* x_scale; const float* w_scale; const float* bias; void* y; uint32_t* status;
+    int64_t x_row, w_row, y_row;
+    int64_t xs_row, xs_block;           /* x_scale[row * xs_row + block * xs_block] */
+    int64_t ws_row, ws_block;           /* w_scale[(column / 128) * ws_row + block * ws_block] */
+    int32_t y_type, m, nn, kk, act;
+} tt_dense_quantized_args;
+tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* cuda_stream);
+
+/* Rotary positions of one or two tensors [tokens, heads, d] (queries and keys) at once: the first rot values of a head are rot / 2 pairs
+ * (interleaved: 2i and 2i + 1, else i and i + rot / 2), and pair i of the token at position p is turned by p * frequency_i,
+ * (a, b) -> factor * (a cos - b sin, b cos + a sin); the other values are copied.  inverse turns the other way: the gradient of the
+ * call (with the same factor).  y may be x.
+ * turns[i] is frequency_i in turns per position, as a fraction of 2^64 (tt_rotary_turns): p * turns[i] modulo 2^64 is the exact phase of any
+ * position, far ones lose nothing.  positions has one entry per token, of 32 or 64 bits (position_bits), negative ones too. */
+typedef struct tt_rotary_args {
+    const void* x[2]; void* y[2];
+    int64_t x_token[2], x_head[2], y_token[2], y_head[2];
+    const void* positions; const uint64_t* turns;
+    int32_t heads[2];                   /* heads[1] = 0: one tensor */
+    int32_t type, position_bits, tokens, d, rot, interleaved, inverse;
+    float factor;
+} tt_rotary_args;
+tt_status tt_rotary(const tt_rotary_args* a, void* cuda_stream);
+/* Pure host: angles per position in radians -> turns per position as fractions of 2^64 (rounded to nearest). */
+tt_status tt_rotary_turns(const double* frequencies, size_t n, uint64_t* turns);
+
+/* A cache of keys (index 0) and values (1) in e4m3.  Page p holds `block` tokens of every head: the value i of slot t of head h is the byte
+ * data[p * page + h * head + t * token + i] times scale[p * s_page + h * s_head].  Token j of sequence b is slot j % block of page
+ * table[b * table_row + j / block].  data starts on a 16-byte boundary, page, head and token are multiples of 16; block is 16, 32, 64 or
+ * 128; d is a multiple of 32 up to 256. */
+typedef struct tt_cache {
+    void* data[2]; float* scale[2];
+    int64_t page[2], head[2], token[2], s_page[2], s_head[2];
+    const int32_t* table; int64_t table_row;
+    int32_t pages, heads, block, d, batch, max_pages;
+} tt_cache;
+
+/* New tokens x[0] (keys) and x[1] (values) [tokens, heads, d] into the pages.  The tokens of sequence b are starts[b] .. starts[b + 1] - 1
+ * (starts has batch + 1 entries, rising from 0; tokens behind the last are ignored), and they become the last of its lengths[b] tokens.
+ * A page that holds none yet gets the scale of tt_quantize over its new tokens; one that does keeps its scale if that is no
+ * smaller, and is otherwise brought to the new one (its values rounded once more).  A page that receives tokens
+ * belongs to one sequence.  Slots behind the last token are left as they were. */
+typedef struct tt_cache_append_args {
+    tt_cache cache;
+    const void* x[2]; int64_t x_token[2], x_head[2];
+    const int32_t* starts; const int32_t* lengths; uint32_t* status;
+    int32_t type, tokens;
+} tt_cache_append_args;
+tt_status tt_cache_append(const tt_cache_append_args* a, void* cuda_stream);
+
+/* y[t,h] = sum_j softmax_j(scale * q[t,h] . k_j) v_j over the tokens j of t's sequence that t sees; query head h reads the cache's head
+ * h / (heads_q / heads).  q and y are [tokens, heads_q, d] in 16 bits.  The queries of sequence b are starts[b] .. starts[b + 1] - 1 (as above), the
+ * last of its lengths[b] tokens; a query sees the tokens up to its own (causal) or all of them, and of those the last `window`
+ * if that is not 0 (counted from its own token; causal only).  A query that sees none gives zeros; rows of y behind the last query are left as they were.
+ * max_count: the most queries of any sequence, max_length: the longest of the lengths, bounds that the work is dealt by (0: not known, then
+ * tokens and max_pages * block); a longer sequence is an error of its status word, more queries only cost time.
+ * workspace: tt_cache_attention_workspace bytes of device memory on a 16-byte boundary, cleared once before its first call; calls leave it
+ * ready for the next one.  Runs that share a workspace follow each other: the caller orders them when they go to different streams.
+ * Deterministic. */
+typedef struct tt_cache_attention_args {
+    tt_cache cache;
+    const void* q; void* y; int64_t q_token, q_head, y_token, y_head;
+    const int32_t* starts; const int32_t* lengths; uint32_t* status;
+    void* workspace; int64_t workspace_bytes;
+    int32_t type, tokens, heads_q, causal, window, max_count, max_length;
+    float scale;
+} tt_cache_attention_args;
+tt_status tt_cache_attention(const tt_cache_attention_args* a, void* cuda_stream);
+/* Pure host: what the call needs (workspace and workspace_bytes are not looked at). */
+tt_status tt_cache_attention_workspace(const tt_cache_attention_args* a, int64_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

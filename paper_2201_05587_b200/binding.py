@@ -23,11 +23,12 @@ TT_OP_CONV2D, TT_OP_DWCONV2D, TT_OP_DENSE, TT_OP_BATCH_MATMUL, TT_OP_SOFTMAX = r
 TT_ACT_NONE, TT_ACT_RELU, TT_ACT_RELU6, TT_ACT_GELU_ERF = range(4)
 TT_FAMILY_GEMM_TC, TT_FAMILY_DW_SIMT, TT_FAMILY_ROW_SIMT = range(3)
 TT_MODE_LEGALISE, TT_MODE_STRICT = 0, 1
+TT_TYPE_F32, TT_TYPE_F16, TT_TYPE_BF16 = range(3)
 TT_RECORD_VERSION = 3
 TT_CHG_TILE_M, TT_CHG_TILE_N, TT_CHG_TILE_K, TT_CHG_STAGES, TT_CHG_SPLIT_K, TT_CHG_VEC, TT_CHG_BLOCK, TT_CHG_ITEMS, TT_CHG_SLAB, TT_CHG_ACC, TT_CHG_KORDER, TT_CHG_FORM, \
     TT_CHG_CLUSTER = 1, 2, 4, 8, 16, 32, 64, 128, 256, 512, 1024, 2048, 4096
 
-i32, u32, f32 = C.c_int32, C.c_uint32, C.c_float
+i32, i64, u32, f32 = C.c_int32, C.c_int64, C.c_uint32, C.c_float
 
 
 class tt_shapes(C.Structure):
@@ -103,6 +104,40 @@ class tt_tune_result(C.Structure):
                 ("pairs_invalid", i32), ("pairs_skipped", i32)]
 
 
+class tt_quantize_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("q", C.c_void_p), ("scales", C.c_void_p), ("x_row", i64), ("q_row", i64), ("s_row", i64), ("s_block", i64),
+                ("x_type", i32), ("m", i32), ("kk", i32), ("block_rows", i32)]
+
+
+class tt_dense_quantized_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("x", "w", "x_scale", "w_scale", "bias", "y", "status")] + \
+               [(n, i64) for n in ("x_row", "w_row", "y_row", "xs_row", "xs_block", "ws_row", "ws_block")] + \
+               [(n, i32) for n in ("y_type", "m", "nn", "kk", "act")]
+
+
+class tt_rotary_args(C.Structure):
+    _fields_ = [("x", C.c_void_p * 2), ("y", C.c_void_p * 2), ("x_token", i64 * 2), ("x_head", i64 * 2), ("y_token", i64 * 2), ("y_head", i64 * 2),
+                ("positions", C.c_void_p), ("turns", C.c_void_p), ("heads", i32 * 2)] + \
+               [(n, i32) for n in ("type", "position_bits", "tokens", "d", "rot", "interleaved", "inverse")] + [("factor", f32)]
+
+
+class tt_cache(C.Structure):
+    _fields_ = [("data", C.c_void_p * 2), ("scale", C.c_void_p * 2), ("page", i64 * 2), ("head", i64 * 2), ("token", i64 * 2), ("s_page", i64 * 2),
+                ("s_head", i64 * 2), ("table", C.c_void_p), ("table_row", i64)] + \
+               [(n, i32) for n in ("pages", "heads", "block", "d", "batch", "max_pages")]
+
+
+class tt_cache_append_args(C.Structure):
+    _fields_ = [("cache", tt_cache), ("x", C.c_void_p * 2), ("x_token", i64 * 2), ("x_head", i64 * 2), ("starts", C.c_void_p), ("lengths", C.c_void_p),
+                ("status", C.c_void_p), ("type", i32), ("tokens", i32)]
+
+
+class tt_cache_attention_args(C.Structure):
+    _fields_ = [("cache", tt_cache), ("q", C.c_void_p), ("y", C.c_void_p), ("q_token", i64), ("q_head", i64), ("y_token", i64), ("y_head", i64),
+                ("starts", C.c_void_p), ("lengths", C.c_void_p), ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", i64)] + \
+               [(n, i32) for n in ("type", "tokens", "heads_q", "causal", "window", "max_count", "max_length")] + [("scale", f32)]
+
+
 EXPORTS = {
     "tt_status_string": (C.c_char_p, [i32]),
     "tt_workload_create": (i32, [i32, C.POINTER(tt_shapes), C.POINTER(C.c_void_p)]),
@@ -152,6 +187,13 @@ EXPORTS = {
     "tt_pool_load": (i32, [C.c_char_p, C.POINTER(tt_schedule_record), C.POINTER(f32), C.c_size_t, C.POINTER(C.c_size_t)]),
     "tt_dense_static_scratch": (i32, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, i32, i32, i32, i32,
                                       C.POINTER(tt_schedule_record), C.c_void_p, C.POINTER(C.c_int64)]),
+    "tt_quantize": (i32, [C.POINTER(tt_quantize_args), C.c_void_p]),
+    "tt_dense_quantized": (i32, [C.POINTER(tt_dense_quantized_args), C.c_void_p]),
+    "tt_rotary": (i32, [C.POINTER(tt_rotary_args), C.c_void_p]),
+    "tt_rotary_turns": (i32, [C.POINTER(C.c_double), C.c_size_t, C.POINTER(C.c_uint64)]),
+    "tt_cache_append": (i32, [C.POINTER(tt_cache_append_args), C.c_void_p]),
+    "tt_cache_attention": (i32, [C.POINTER(tt_cache_attention_args), C.c_void_p]),
+    "tt_cache_attention_workspace": (i32, [C.POINTER(tt_cache_attention_args), C.POINTER(i64)]),
 }
 
 _lib = None
@@ -542,6 +584,239 @@ def dense_static_scratch(x, w, bias, y, act, rec):
     st = lib().tt_dense_static_scratch(_ptr(x), _ptr(w), _ptr(bias), _ptr(y), m, nn, kk, act, C.byref(rec), _stream(),
                                        C.byref(used))
     return st, used.value
+
+
+# ---- 8-bit operators of a transformer's inference pass ----------------------------------------------------------------------
+#
+# Each function below checks its tensors and returns a Call: the arguments of the native call, made once, for a program that repeats it
+# on the same tensors (Call.run enqueues it on the current stream, which may be capturing).  It keeps references to the tensors.
+
+class Call:
+    """One call of an 8-bit operator: ``run`` enqueues it on the current stream of its tensors' device, ``status`` reads what only the
+    device has seen.  A call that has a status word or a workspace is made outside of stream captures; its runs share them, so they
+    follow each other: the caller orders them when they go to different streams."""
+
+    def __init__(self, name, args, keep, device, status=None):
+        lib()
+        self.name, self.args, self._keep, self._status = name, args, keep, status
+        self._device, self._index = device, device.index
+        self._address = C.cast(getattr(_lib, name), C.c_void_p).value
+
+    def run(self):
+        torch = _torch
+        if torch.cuda.current_device() == self._index:
+            st = _call.call(self._address, self.args, torch._C._cuda_getCurrentRawStream(self._index))
+        else:
+            with torch.cuda.device(self._index):
+                st = _call.call(self._address, self.args, torch._C._cuda_getCurrentRawStream(self._index))
+        if st != TT_OK:
+            raise TTError(st, self.name)
+
+    def status(self) -> int:
+        """Waits for the runs on the current stream; TT_OK, or what one of them has reported since the last look (and clears it)."""
+        if self._status is None:
+            _torch.cuda.current_stream(self._device).synchronize()
+            return TT_OK
+        word = int(self._status.item())
+        if word:
+            self._status.zero_()
+        return word & 0xff
+
+
+def _need(ok, what):
+    if not ok:
+        raise TTError(TT_ERR_INVALID_ARG, what)
+
+
+def _type_of(t):
+    torch = _import_torch()
+    types = {torch.float32: TT_TYPE_F32, torch.float16: TT_TYPE_F16, torch.bfloat16: TT_TYPE_BF16}
+    _need(t.dtype in types, f"elements of {t.dtype}")
+    return types[t.dtype]
+
+
+def _same_device(first, *others):
+    _need(first.is_cuda, "tensors live on a GPU")
+    _need(all(t is None or t.device == first.device for t in others), "tensors live on one device")
+    return first.device
+
+
+def _is_f8(t):
+    torch = _import_torch()
+    return t.dtype in (torch.float8_e4m3fn, torch.uint8)
+
+
+def _inner(t, what):
+    _need(t.shape[-1] <= 1 or t.stride(-1) == 1, f"{what}: the last axis is contiguous")
+
+
+def _row(t):
+    """Elements from row to row; a single row's may be anything."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def _f32(t, shape, what):
+    _need(t.dtype == _torch.float32 and tuple(t.shape) == tuple(shape), f"{what}: float32 {tuple(shape)}")
+
+
+def _device_words(device, n_bytes):
+    """Device memory that is zero when this returns, whatever stream is used afterwards."""
+    torch = _torch
+    _need(not torch.cuda.is_current_stream_capturing(), "a call with device words of its own is made outside of captures")
+    t = torch.zeros(max(int(n_bytes), 4), dtype=torch.uint8, device=device)
+    torch.cuda.current_stream(device).synchronize()
+    return t
+
+
+def _status_word(device):
+    return _device_words(device, 4).view(_torch.int32)
+
+
+def quantize(x, q, scales, block_rows=1) -> Call:
+    """tt_quantize: x [m, k] (float32, float16 or bfloat16) -> q [m, k] (e4m3) and scales [ceil(k / 128), ceil(m / block_rows)] (float32),
+    of any strides; the last axis of x and q is contiguous.  For dense_quantized the rows of q start on 16-byte boundaries."""
+    _need(x.dim() == 2 and q.shape == x.shape and _is_f8(q), "x [m, k] and q [m, k] in e4m3")
+    _need(block_rows in (1, 128), "block_rows is 1 or 128")
+    m, k = x.shape
+    device = _same_device(x, q, scales)
+    _f32(scales, (-(-k // 128), -(-m // block_rows)), "scales")
+    _inner(x, "x"), _inner(q, "q")
+    a = tt_quantize_args(x=x.data_ptr(), q=q.data_ptr(), scales=scales.data_ptr(), x_row=_row(x), q_row=_row(q), s_row=scales.stride(1),
+                            s_block=scales.stride(0), x_type=_type_of(x), m=m, kk=k, block_rows=block_rows)
+    return Call("tt_quantize", a, (x, q, scales), device)
+
+
+def dense_quantized(x, x_scale, w, w_scale, y, bias=None, act=TT_ACT_NONE) -> Call:
+    """tt_dense_quantized: y [m, n] = act(x w^T + bias) of x [m, k] and w [n, k] in e4m3 with x_scale [ceil(k / 128), m] and w_scale
+    [ceil(n / 128), ceil(k / 128)] (float32, any strides); y float32, float16 or bfloat16, bias float32 [n] or None."""
+    _need(x.dim() == 2 and w.dim() == 2 and y.dim() == 2 and _is_f8(x) and _is_f8(w), "x [m, k] and w [n, k] in e4m3")
+    (m, k), n = x.shape, w.shape[0]
+    _need(w.shape[1] == k and tuple(y.shape) == (m, n), "y [m, n] of x [m, k] and w [n, k]")
+    device = _same_device(x, x_scale, w, w_scale, y, bias)
+    _f32(x_scale, (-(-k // 128), m), "x_scale")
+    _f32(w_scale, (-(-n // 128), -(-k // 128)), "w_scale")
+    _inner(x, "x"), _inner(w, "w"), _inner(y, "y")
+    if bias is not None:
+        _f32(bias, (n,), "bias")
+        _inner(bias, "bias")
+    pitch = lambda t: _row(t) if t.shape[0] > 1 else -(-t.shape[1] // 16) * 16      # noqa: E731  (a single row has no pitch)
+    status = _status_word(device)
+    a = tt_dense_quantized_args(x=x.data_ptr(), w=w.data_ptr(), x_scale=x_scale.data_ptr(), w_scale=w_scale.data_ptr(),
+                         bias=None if bias is None else bias.data_ptr(), y=y.data_ptr(), status=status.data_ptr(), x_row=pitch(x), w_row=pitch(w),
+                         y_row=_row(y), xs_row=x_scale.stride(1), xs_block=x_scale.stride(0), ws_row=w_scale.stride(0), ws_block=w_scale.stride(1),
+                         y_type=_type_of(y), m=m, nn=n, kk=k, act=act)
+    return Call("tt_dense_quantized", a, (x, x_scale, w, w_scale, y, bias), device, status)
+
+
+def rotary_frequencies(rot, base=10000.0, scaling=None, factor=1.0, context=4096, slow=1.0, fast=32.0):
+    """Angles per position, in radians, of the rot / 2 pairs: base^(-2i / rot), scaled for contexts `factor` times as long as the one that the
+    weights were trained on.  scaling: None, "linear" (all positions divided by the factor), "base" (a larger base, so that the slowest
+    pair slows down by the factor and the fastest keeps its pace) or "by_parts" (pairs that turn less than `slow` times over the training
+    context are divided, those that turn more than `fast` times are kept, the ones between are blended)."""
+    _need(rot >= 0 and rot % 2 == 0 and base > 0 and factor > 0 and scaling in (None, "linear", "base", "by_parts") and fast > slow, "rotary_frequencies")
+    if scaling == "base" and rot > 2:
+        base = base * factor ** (rot / (rot - 2))
+    f = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        return [v / factor for v in f]
+    if scaling == "by_parts":
+        keep = [min(1.0, max(0.0, (context * v / 6.283185307179586 - slow) / (fast - slow))) for v in f]
+        return [v * k + v / factor * (1.0 - k) for v, k in zip(f, keep)]
+    return f
+
+
+def rotary_table(frequencies, device=None):
+    """tt_rotary_turns: angles per position (radians; a sequence or a float64 tensor) -> the int64 tensor that rotary takes, on `device` (default:
+    the tensor's, or the current GPU)."""
+    torch = _import_torch()
+    if isinstance(frequencies, torch.Tensor):
+        device = device if device is not None else frequencies.device
+        frequencies = frequencies.double().tolist()
+    n = len(frequencies)
+    values, turns = (C.c_double * max(n, 1))(*frequencies), (C.c_uint64 * max(n, 1))()
+    _check(lib().tt_rotary_turns(values, n, turns), "tt_rotary_turns")
+    signed = [v - (1 << 64) if v >> 63 else v for v in list(turns)[:n]]
+    return torch.tensor(signed, dtype=torch.int64, device=device if device is not None else "cuda")
+
+
+def rotary(x, positions, table, y=None, interleaved=False, factor=1.0, inverse=False) -> Call:
+    """tt_rotary: one tensor [tokens, heads, d] or two (queries and keys) turned by positions [tokens] (int32 or int64) times the frequencies of
+    `table` [rot / 2] (rotary_table) into y (default: in place).  inverse turns back, which is the gradient of the call."""
+    xs = list(x) if isinstance(x, (list, tuple)) else [x]
+    ys = xs if y is None else list(y) if isinstance(y, (list, tuple)) else [y]
+    torch = _import_torch()
+    _need(1 <= len(xs) <= 2 and len(ys) == len(xs) and all(t.dim() == 3 for t in xs), "one or two tensors [tokens, heads, d]")
+    tokens, _, d = xs[0].shape
+    _need(all(u.shape == t.shape and u.dtype == t.dtype == xs[0].dtype and t.shape[0] == tokens and t.shape[2] == d for t, u in zip(xs, ys)), "tensors of the same tokens, head size and type")
+    _need(positions.dtype in (torch.int32, torch.int64) and tuple(positions.shape) == (tokens,) and (tokens <= 1 or positions.stride(0) == 1), "positions [tokens]")
+    _need(table.dtype == torch.int64 and table.dim() == 1 and (table.numel() <= 1 or table.stride(0) == 1) and 2 * table.numel() <= d, "table [rot / 2] of rotary_table")
+    device = _same_device(xs[0], *xs, *ys, positions, table)
+    a = tt_rotary_args(positions=positions.data_ptr(), turns=table.data_ptr(), type=_type_of(xs[0]), position_bits=32 if positions.dtype == torch.int32 else 64,
+                       tokens=tokens, d=d, rot=2 * table.numel(), interleaved=int(bool(interleaved)), inverse=int(bool(inverse)), factor=factor)
+    for i, (t, u) in enumerate(zip(xs, ys)):
+        _inner(t, "x"), _inner(u, "y")
+        a.x[i], a.y[i], a.heads[i] = t.data_ptr(), u.data_ptr(), t.shape[1]
+        a.x_token[i], a.x_head[i], a.y_token[i], a.y_head[i] = t.stride(0), t.stride(1), u.stride(0), u.stride(1)
+    return Call("tt_rotary", a, (xs, ys, positions, table), device)
+
+
+class Cache:
+    """A paged e4m3 cache (tt_cache): k and v [pages, heads, block, d] (any strides that are multiples of 16, the last axis contiguous), k_scale and
+    v_scale [pages, heads] float32, table [batch, pages of a sequence] int32."""
+
+    def __init__(self, k, v, k_scale, v_scale, table):
+        torch = _import_torch()
+        _need(k.dim() == 4 and v.shape == k.shape and _is_f8(k) and _is_f8(v), "k and v [pages, heads, block, d] in e4m3")
+        pages, heads, block, d = k.shape
+        _need(table.dtype == torch.int32 and table.dim() == 2, "table [batch, pages of a sequence] int32")
+        self.device = _same_device(k, v, k_scale, v_scale, table)
+        c = tt_cache(table=table.data_ptr(), table_row=_row(table), pages=pages, heads=heads, block=block, d=d, batch=table.shape[0], max_pages=table.shape[1])
+        for i, (t, s) in enumerate(((k, k_scale), (v, v_scale))):
+            _f32(s, (pages, heads), "scales")
+            _inner(t, "k and v")
+            c.data[i], c.scale[i] = t.data_ptr(), s.data_ptr()
+            c.page[i], c.head[i], c.token[i] = t.stride(0), t.stride(1), t.stride(2)
+            c.s_page[i], c.s_head[i] = s.stride(0), s.stride(1)
+        _inner(table, "table")
+        self.c, self.keep = c, (k, v, k_scale, v_scale, table)
+
+    def _batch(self, starts, lengths):
+        torch = _torch
+        _need(starts.dtype == lengths.dtype == torch.int32 and starts.is_contiguous() and lengths.is_contiguous(), "starts and lengths are int32")
+        _need(tuple(starts.shape) == (self.c.batch + 1,) and tuple(lengths.shape) == (self.c.batch,), "starts [batch + 1], lengths [batch]")
+
+
+def cache_append(cache, k, v, starts, lengths) -> Call:
+    """tt_cache_append: new keys and values [tokens, heads, d] (float32, float16 or bfloat16) of a batch into their pages.  Sequence b has the tokens
+    starts[b] .. starts[b + 1] - 1 (int32, on the device), the last of its lengths[b] tokens."""
+    _need(k.dim() == 3 and v.shape == k.shape and v.dtype == k.dtype and tuple(k.shape[1:]) == (cache.c.heads, cache.c.d), "k and v [tokens, heads, d] of the cache")
+    cache._batch(starts, lengths)
+    device = _same_device(k, v, starts, lengths, *cache.keep)
+    _inner(k, "k"), _inner(v, "v")
+    status = _status_word(device)
+    a = tt_cache_append_args(cache=cache.c, starts=starts.data_ptr(), lengths=lengths.data_ptr(), status=status.data_ptr(), type=_type_of(k), tokens=k.shape[0])
+    for i, t in enumerate((k, v)):
+        a.x[i], a.x_token[i], a.x_head[i] = t.data_ptr(), t.stride(0), t.stride(1)
+    return Call("tt_cache_append", a, (cache, k, v, starts, lengths), device, status)
+
+
+def cache_attention(cache, q, y, starts, lengths, scale, causal=True, window=0, max_count=0, max_length=0) -> Call:
+    """tt_cache_attention: y [tokens, heads_q, d] of the queries q [tokens, heads_q, d] (float16 or bfloat16) over the cache, batched as in
+    cache_append.  max_count and max_length: bounds on a sequence's queries and on the lengths, where the program knows them."""
+    _need(q.dim() == 3 and y.shape == q.shape and y.dtype == q.dtype and q.shape[2] == cache.c.d, "q and y [tokens, heads_q, d] of the cache")
+    cache._batch(starts, lengths)
+    device = _same_device(q, y, starts, lengths, *cache.keep)
+    _inner(q, "q"), _inner(y, "y")
+    status = _status_word(device)
+    a = tt_cache_attention_args(cache=cache.c, q=q.data_ptr(), y=y.data_ptr(), q_token=q.stride(0), q_head=q.stride(1), y_token=y.stride(0),
+                                y_head=y.stride(1), starts=starts.data_ptr(), lengths=lengths.data_ptr(), status=status.data_ptr(), type=_type_of(q),
+                                tokens=q.shape[0], heads_q=q.shape[1], causal=int(bool(causal)), window=window, max_count=max_count,
+                                max_length=max_length, scale=scale)
+    n = i64()
+    _check(lib().tt_cache_attention_workspace(C.byref(a), C.byref(n)), "tt_cache_attention")
+    workspace = _device_words(device, n.value)
+    a.workspace, a.workspace_bytes = workspace.data_ptr(), n.value
+    return Call("tt_cache_attention", a, (cache, q, y, starts, lengths, workspace), device, status)
 
 
 def transfer_tune(workloads, tensor_sets, pool, opts: tt_tune_opts | None = None):

@@ -1,0 +1,673 @@
+// A paged cache of keys and values in e4m3, a scale for each page and head: new tokens into it, and attention over it.
+#include <cuda_runtime.h>
+#include <cstring>
+#include "tt_ptx.cuh"
+#include "tt_f8.cuh"
+
+namespace tt {
+
+__device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(status, 0u, (unsigned)TT_ERR_INVALID_ARG); }
+
+// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] / per + extra * b and up (as many as it can need
+// at most), so a unit finds its sequence by bisection.
+__device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
+    int lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (starts[mid] * mul / per + (long long)extra * mid <= unit) lo = mid; else hi = mid - 1;
+    }
+    first = starts[lo] * mul / per + (long long)extra * lo;
+    return lo;
+}
+
+// ---- append ---------------------------------------------------------------------------------------------------------------
+//
+// A CTA has the new tokens of one page and head, of the keys or of the values: their maximum first, then (the second reading comes from the
+// caches) their conversion; where the page holds tokens already and the scale has to rise, those are brought to it.
+template <int TYPE, bool WIDE>
+__global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_append_args a) {
+    __shared__ float warp_most[8];
+    typedef typename Element<TYPE>::type T;
+    pdl_allow_next();
+    pdl_wait_prev();
+    const tt_cache& c = a.cache;
+    const int head = (int)blockIdx.y >> 1, w = (int)blockIdx.y & 1;
+    long long first_unit;
+    const int b = sequence_of(a.starts, c.batch, 1, c.block, 2, blockIdx.x, first_unit);
+    const int start = a.starts[b], count = a.starts[b + 1] - start, length = a.lengths[b];
+    if (count == 0) return;
+    if (count < 0 || start < 0 || start + (long long)count > a.tokens || length < count || length > (long long)c.max_pages * c.block) {
+        if (threadIdx.x == 0) report_invalid(a.status);
+        return;
+    }
+    const int first = length - count;                       // position of the first new token
+    const long long index = first / c.block + ((long long)blockIdx.x - first_unit);
+    if (index * c.block >= length) return;
+    const int page = c.table[b * c.table_row + index];
+    if (page < 0 || page >= c.pages) {
+        if (threadIdx.x == 0) report_invalid(a.status);
+        return;
+    }
+    const int lo = max(first, (int)index * c.block), hi = min(length, (int)index * c.block + c.block);
+    const int held = lo - (int)index * c.block;             // tokens that the page holds already
+    constexpr int kPiece = WIDE ? 8 : 1;                    // values a thread takes at a time
+    const int pieces = c.d / kPiece, total = (hi - lo) * pieces;
+    const T* x = static_cast<const T*>(a.x[w]) + (long long)(start + (lo - first)) * a.x_token[w] + (long long)head * a.x_head[w];
+    float most = 0.f;
+    for (int e = threadIdx.x; e < total; e += blockDim.x) {
+        const int t = e / pieces, i = (e - t * pieces) * kPiece;
+        float v[kPiece];
+        if constexpr (WIDE) load_wide<TYPE, kPiece>(x + t * a.x_token[w] + i, v);
+        else v[0] = Element<TYPE>::up(x[t * a.x_token[w] + i]);
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) most = finite_max(most, v[j]);
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    float* scale = c.scale[w] + page * c.s_page[w] + head * c.s_head[w];
+    const float old = held > 0 ? *scale : 0.f;
+    if (blockDim.x > 32) {
+        if ((threadIdx.x & 31) == 0) warp_most[threadIdx.x >> 5] = most;
+        __syncthreads();                                    // (and every thread has read the old scale)
+        for (int i = 0; i < (int)blockDim.x >> 5; ++i) most = fmaxf(most, warp_most[i]);
+    } else {
+        __syncwarp();
+    }
+    float s = power_scale(most);
+    if (held > 0 && old >= s) s = old;
+    if (threadIdx.x == 0 && (held == 0 || s != old)) *scale = s;
+    uint8_t* data = static_cast<uint8_t*>(c.data[w]) + page * c.page[w] + head * c.head[w];
+    if (held > 0 && s != old) {
+        // (a ratio of powers of two as the calls here leave them; a scale of another origin is taken as it is)
+        const float ratio = __fdiv_rn(old, s);
+        const int words = c.d / 4;
+        for (int e = threadIdx.x; e < held * words; e += blockDim.x) {
+            const int t = e / words;
+            uint32_t* p = reinterpret_cast<uint32_t*>(data + t * c.token[w]) + (e - t * words);
+            const uint32_t q = *p;
+            *p = to_e4m3x4(float_of_e4m3(q) * ratio, float_of_e4m3(q >> 8) * ratio, float_of_e4m3(q >> 16) * ratio, float_of_e4m3(q >> 24) * ratio);
+        }
+    }
+    const bool power = (__float_as_int(s) & 0x7fffff) == 0 && s >= 1.17549435e-38f && s <= 1.329227996e36f;      // 2^-126 .. 2^120
+    const float inv = power ? power_inverse(s) : 0.f;
+    for (int e = threadIdx.x; e < total; e += blockDim.x) {
+        const int t = e / pieces, i = (e - t * pieces) * kPiece;
+        float v[kPiece];
+        if constexpr (WIDE) load_wide<TYPE, kPiece>(x + t * a.x_token[w] + i, v);
+        else v[0] = Element<TYPE>::up(x[t * a.x_token[w] + i]);
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) v[j] = power ? v[j] * inv : __fdiv_rn(v[j], s);
+        uint8_t* q = data + (long long)(held + t) * c.token[w] + i;
+        if constexpr (WIDE) *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3x4(v[0], v[1], v[2], v[3]), to_e4m3x4(v[4], v[5], v[6], v[7]));
+        else *q = (uint8_t)to_e4m3x4(v[0], 0.f, 0.f, 0.f);
+    }
+}
+
+// ---- attention ------------------------------------------------------------------------------------------------------------
+//
+// One pass over the visible keys and values with a running maximum and sum of each row (a query of one head).  The heads that share a key
+// head are rows of one tile, so a key is read once for all of them.
+//
+// Tiles of 16 or 32 rows: the cache's bytes are the bound.  A warp takes runs of 64 tokens, 16 at a time.  Its lanes fetch just the
+// bytes that they multiply: the order of the reduction is free as long as both factors have it, so lane (g, c) of an m16n8k16 product takes
+// 16 bytes in a row of the key g, and of four values 16 bytes in a row of columns, and nothing is exchanged through shared
+// memory.  It is only the buffer of the copies under way, each lane's its own, so there is no barrier in the loop.
+//   e4m3 -> 16-bit floating point is exact, and so is a row of queries: brought to a maximum of 2^14..2^15 by a power of two, which the
+// scores' factor takes back.  Probabilities are rounded to 11 bits, times 2^15 and the page's scale over the largest so far, so that what is
+// 2^-29 of the largest still has all of them; sums are in 32 bits.
+//   The keys of a sequence are split over CTAs, of which the last to finish adds up what all have left in the workspace, in their order.
+
+constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it
+constexpr int kRun = 64;                    // tokens that a warp takes in a row
+constexpr int kAttendWarps = 4;
+
+struct Attend {
+    tt_cache_attention_args a;
+    int group, rows;                        // query heads of a key head; rows of a tile
+    int chunk, splits, max_length;          // tokens of a split, most splits
+    float scale_log2;                       // the scale times log2(e)
+    unsigned* counters; float* partial;
+};
+
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <int N>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void read_shared(uint32_t addr, uint32_t (&v)[N / 4]) {
+    if constexpr (N == 16) asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr) : "memory");
+    else if constexpr (N == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v[0]), "=r"(v[1]) : "r"(addr) : "memory");
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[0]) : "r"(addr) : "memory");
+}
+constexpr int widest(int bytes) { return bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : 4; }
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xffffffffu, v, 1);
+    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+}
+// A non-zero byte for each e4m3 byte of the word that is NaN.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+template <int D, int MT>
+struct AttendShape {
+    static constexpr int kKey = widest(D / 4), kKeyPieces = D / 4 / kKey;           // bytes of a key that a lane fetches at a time, and how often
+    static constexpr int kVal = widest(D / 8), kValPieces = D / 8 / kVal;
+    static constexpr int kRows = 16 * MT;
+    static constexpr uint32_t kKeyBytes = 2u * kKeyPieces * 32u * kKey, kStage = kKeyBytes + 4u * kValPieces * 32u * kVal + 256u;      // 16 tokens, and each lane's copy of two scales
+    static constexpr int kStages = D <= 64 ? 6 : D <= 128 ? 4 : 3;
+    static constexpr uint32_t kQuery = MT * (D / 16) * 512u;                         // the queries' fragments
+    static constexpr uint32_t kRing = kAttendWarps * kStages * kStage;
+    static constexpr uint32_t kJoin = kAttendWarps * kRows * (D + 4) * 4u;           // the warps' results (over the ring)
+    static constexpr uint32_t kBytes = kQuery + (kRing > kJoin ? kRing : kJoin);
+};
+
+template <int D, int MT>
+__global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const Attend g) {
+    typedef AttendShape<D, MT> S;
+    extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int last_one;
+    pdl_allow_next();
+    pdl_wait_prev();
+    const tt_cache& c = g.a.cache;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, cq = lane & 3, head = blockIdx.y;
+    long long first_unit;
+    const int b = sequence_of(g.a.starts, c.batch, g.group, S::kRows, 1, blockIdx.x, first_unit);
+    const int start = g.a.starts[b], count = g.a.starts[b + 1] - start;
+    int length = g.a.lengths[b];
+    if (count == 0) return;
+    if (count < 0 || start < 0 || start + (long long)count > g.a.tokens || length < 0 || length > g.max_length) {
+        if (threadIdx.x == 0) report_invalid(g.a.status);
+        return;
+    }
+    const long long row0 = ((long long)blockIdx.x - first_unit) * S::kRows, all_rows = (long long)count * g.group;
+    if (row0 >= all_rows) return;
+    const int rows = (int)min((long long)S::kRows, all_rows - row0);
+    // what the tile's first and last row see: tokens seen0 .. up to hi
+    const int t0 = (int)(row0 / g.group), t1 = (int)((row0 + rows - 1) / g.group);
+    const int before = length - count;                      // (negative: the first queries see nothing)
+    const int lo = g.a.window > 0 ? max(0, before + t0 + 1 - g.a.window) : 0;
+    const int hi = g.a.causal ? max(0, min(length, before + t1 + 1)) : length;
+    const int base = lo / kRun * kRun;
+    const int active = hi > lo ? (hi - base + g.chunk - 1) / g.chunk : 1;
+    if ((int)blockIdx.z >= active) return;
+    const int from = base + (int)blockIdx.z * g.chunk, to = min(hi, from + g.chunk);
+    // tokens that every row sees: whole_lo .. whole_hi - 1
+    const int whole_lo = g.a.window > 0 ? max(0, before + t1 + 1 - g.a.window) : 0;
+    const int whole_hi = g.a.causal ? max(0, min(length, before + t0 + 1)) : length;
+
+    const uint32_t query = smem_u32(smem), ring = query + S::kQuery + (uint32_t)warp * S::kStages * S::kStage;
+    // ---- the copies of a step: 16 tokens of one page ----
+    const int steps = [&] {                                  // of this warp
+        const int runs = to > from ? (to - from + kRun - 1) / kRun : 0;
+        if (warp >= runs) return 0;
+        const int mine = (runs - warp + kAttendWarps - 1) / kAttendWarps;
+        const int last = from + ((mine - 1) * kAttendWarps + warp) * kRun;
+        return (mine - 1) * (kRun / kStep) + (min(kRun, to - last) + kStep - 1) / kStep;
+    }();
+    const auto token_of = [&](int step) { return from + ((step >> 2) * kAttendWarps + warp) * kRun + (step & 3) * kStep; };
+    const int* table = c.table + b * c.table_row;
+    const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0];
+    const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1];
+    bool bad = false;
+    const int shift = 31 - __clz(c.block);
+    const auto page_of = [&](int step) { return step < steps ? table[token_of(step) >> shift] : 0; };
+    const auto fetch = [&](int step, int page) {
+        if (step < steps) {
+            if ((unsigned)page >= (unsigned)c.pages) { bad = true; page = 0; }
+            const uint32_t slot = ring + (uint32_t)(step % S::kStages) * S::kStage;
+            const int t = token_of(step) & (c.block - 1);
+            const uint8_t* k = keys + page * c.page[0] + t * c.token[0];
+            const uint8_t* v = vals + page * c.page[1] + t * c.token[1];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int p = 0; p < S::kKeyPieces; ++p)
+                    copy_async<S::kKey>(slot + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k + (8 * n + gq) * c.token[0] + p * 4 * S::kKey + cq * S::kKey);
+#pragma unroll
+            for (int n = 0; n < 4; ++n)                      // tokens 2c, 2c + 1, 2c + 8, 2c + 9
+#pragma unroll
+                for (int p = 0; p < S::kValPieces; ++p)
+                    copy_async<S::kVal>(slot + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal,
+                                        v + (2 * cq + (n & 1) + 8 * (n >> 1)) * c.token[1] + p * 8 * S::kVal + gq * S::kVal);
+            copy_async<4>(slot + S::kStage - 256u + (uint32_t)lane * 8u, c.scale[0] + page * c.s_page[0] + head * c.s_head[0]);
+            copy_async<4>(slot + S::kStage - 252u + (uint32_t)lane * 8u, c.scale[1] + page * c.s_page[1] + head * c.s_head[1]);
+        }
+        cp_async_commit();
+    };
+    int next_page = page_of(0);
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; ++i) {
+        const int page = next_page;
+        next_page = page_of(i + 1);
+        fetch(i, page);
+    }
+
+    // ---- queries: the rows of the tile as fragments, in shared memory (each lane reads back what it wrote, but for the other warps') ----
+    const auto row_head = [&](int r) { return head * g.group + (int)((row0 + r) % g.group); };
+    const auto row_token = [&](int r) { return start + (int)((row0 + r) / g.group); };
+    float factor[2 * MT];                                    // of the rows gq, gq + 8, ... : what turns a product into a score in powers of two
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) {
+        const int r = gq + 8 * i;
+        float most = 0.f;
+        const long long at = r < rows ? (long long)row_token(r) * g.a.q_token + (long long)row_head(r) * g.a.q_head : 0;
+        if (r < rows)
+            for (int p = 0; p < S::kKeyPieces; ++p)
+                for (int e = 0; e < S::kKey; ++e) most = finite_max(most, load_one(g.a.q, at + p * 4 * S::kKey + cq * S::kKey + e, g.a.type));
+        most = quad_max(most);
+        const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14;          // (a subnormal: 0, as good as 1)
+        const float up = __int_as_float((min(254, max(1, 127 + 14 + 127 - ex))) << 23);
+        factor[i] = g.scale_log2 / up;
+        if (warp == i % kAttendWarps) {
+#pragma unroll
+            for (int p = 0; p < S::kKeyPieces; ++p)
+#pragma unroll
+                for (int s = 0; s < S::kKey / 4; ++s) {
+                    float v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = r < rows ? load_one(g.a.q, at + p * 4 * S::kKey + cq * S::kKey + 4 * s + e, g.a.type) * up : 0.f;
+                    const int step = p * (S::kKey / 4) + s;
+                    // a fragment's registers: (row, k), (row + 8, k), (row, k + 8), (row + 8, k + 8)
+                    const uint32_t to_ = query + (uint32_t)((((i >> 1) * (D / 16) + step) * 32 + lane) * 16 + (i & 1) * 4);
+                    st_shared_u32(to_, down2<TT_TYPE_F16>(v[0], v[1]));
+                    st_shared_u32(to_ + 8u, down2<TT_TYPE_F16>(v[2], v[3]));
+                }
+        }
+    }
+    __syncthreads();
+
+    float o[MT][D / 8][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[m][j][e] = 0.f;
+    float top[2 * MT], sum[2 * MT], ref = 0.f;               // ref: the largest scale of values so far, the unit of o
+#pragma unroll
+    for (int i = 0; i < 2 * MT; ++i) { top[i] = -INFINITY; sum[i] = 0.f; }
+
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+        {
+            const int page = next_page;
+            next_page = page_of(step + S::kStages);
+            fetch(step + S::kStages - 1, page);
+        }
+        cp_async_wait<S::kStages - 1>();
+        const uint32_t slot = ring + (uint32_t)(step % S::kStages) * S::kStage;
+        uint32_t scales[2];
+        read_shared<8>(slot + S::kStage - 256u + (uint32_t)lane * 8u, scales);
+        const float ks = __uint_as_float(scales[0]), vs = __uint_as_float(scales[1]);
+        const int t = token_of(step);
+        const bool whole = t >= whole_lo && t + kStep <= whole_hi;
+        // scores: rows x 16 tokens
+        float s[MT][2][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[m][n][e] = 0.f;
+#pragma unroll
+        for (int p = 0; p < S::kKeyPieces; ++p) {
+            uint32_t k[2][S::kKey / 4];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) read_shared<S::kKey>(slot + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k[n]);
+#pragma unroll
+            for (int w = 0; w < S::kKey / 4; ++w) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    uint32_t q[4];
+                    read_shared<16>(query + (uint32_t)((m * (D / 16) + p * (S::kKey / 4) + w) * 32 + lane) * 16u, q);
+#pragma unroll
+                    for (int n = 0; n < 2; ++n) mma_16x8x16(s[m][n], q, f16x2_of_e4m3(k[n][w]), f16x2_of_e4m3(k[n][w] >> 16));
+                }
+            }
+        }
+        // the running maximum, in powers of two
+        const float new_ref = fmaxf(ref, vs);
+        const float unit = vs > 0.f ? __fdividef(vs, new_ref) * 32768.f : 0.f;
+        const float shrink = ref < new_ref ? __fdividef(ref, new_ref) : 1.f;
+        bool moved = shrink != 1.f;
+        float alpha[2 * MT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = 2 * m + h;
+                float mx = -INFINITY;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float v = s[m][n][2 * h + e] * (factor[i] * ks);
+                        if (!whole) {
+                            const int tok = t + 8 * n + 2 * cq + e, pos = before + (int)((row0 + gq + 8 * i) / g.group);
+                            const bool seen = tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
+                            v = seen ? v : -INFINITY;
+                        }
+                        s[m][n][2 * h + e] = v;
+                        mx = fmaxf(mx, v);
+                    }
+                mx = fmaxf(top[i], quad_max(mx));
+                const float ref_max = mx == -INFINITY ? 0.f : mx;
+                alpha[i] = exp2f(top[i] - ref_max) * shrink;
+                const float keep = exp2f(top[i] - ref_max);
+                moved = moved || mx != top[i];
+                top[i] = mx;
+                float add = 0.f;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float p = exp2f(s[m][n][2 * h + e] - ref_max);
+                        add += p;
+                        s[m][n][2 * h + e] = p * unit;
+                    }
+                sum[i] = sum[i] * keep + add;
+            }
+        ref = new_ref;
+        if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[m][j][e] *= alpha[2 * m + (e >> 1)];
+        }
+        uint32_t pa[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            pa[m][0] = down2<TT_TYPE_F16>(s[m][0][0], s[m][0][1]);
+            pa[m][1] = down2<TT_TYPE_F16>(s[m][0][2], s[m][0][3]);
+            pa[m][2] = down2<TT_TYPE_F16>(s[m][1][0], s[m][1][1]);
+            pa[m][3] = down2<TT_TYPE_F16>(s[m][1][2], s[m][1][3]);
+        }
+        // values
+#pragma unroll
+        for (int p = 0; p < S::kValPieces; ++p) {
+            uint32_t v[4][S::kVal / 4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) read_shared<S::kVal>(slot + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal, v[n]);
+            if (!whole) {
+                // What no row of the tile sees is not multiplied (it may be anything), and a NaN that only some rows see reaches just those: it is
+                // replaced by 0 in the product, and another product counts for each row how many of a column's it sees.
+                uint32_t nans = 0u;
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const int tok = t + 2 * cq + (n & 1) + 8 * (n >> 1);
+                    const bool any = tok >= lo && tok < hi;
+#pragma unroll
+                    for (int w = 0; w < S::kVal / 4; ++w) {
+                        v[n][w] = any ? v[n][w] : 0u;
+                        nans |= nan_bytes(v[n][w]);
+                    }
+                }
+                if (__any_sync(0xffffffffu, nans != 0u)) {
+                    uint32_t see[MT][4];
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int pos = before + (int)((row0 + 16 * m + gq + 8 * (r & 1)) / g.group);
+                            uint32_t w = 0u;
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int tok = t + 8 * (r >> 1) + 2 * cq + e;
+                                const bool seen = tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
+                                w |= seen ? 0x3c00u << (16 * e) : 0u;
+                            }
+                            see[m][r] = w;
+                        }
+#pragma unroll
+                    for (int j = 0; j < S::kVal; ++j) {
+                        const auto is_nan = [&](int n) { return ((v[n][j >> 2] >> (8 * (j & 3))) & 0x7fu) == 0x7fu; };
+                        const uint32_t b0 = (is_nan(0) ? 0x3c00u : 0u) | (is_nan(1) ? 0x3c000000u : 0u), b1 = (is_nan(2) ? 0x3c00u : 0u) | (is_nan(3) ? 0x3c000000u : 0u);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            float hit[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_16x8x16(hit, see[m], b0, b1);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) if (hit[e] > 0.f) o[m][p * S::kVal + j][e] = __int_as_float(0x7fffffff);
+                        }
+                    }
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+#pragma unroll
+                        for (int w = 0; w < S::kVal / 4; ++w) v[n][w] &= ~((nan_bytes(v[n][w]) >> 7) * 0xffu);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < S::kVal; j += 2) {
+                // bytes j, j + 1 of two tokens side by side: the pairs of the reduction
+                const uint32_t sel = (j & 2) ? 0x7362u : 0x5140u;
+                const uint32_t x0 = __byte_perm(v[0][j >> 2], v[1][j >> 2], sel), x1 = __byte_perm(v[2][j >> 2], v[3][j >> 2], sel);
+                const uint32_t b0 = f16x2_of_e4m3(x0), b1 = f16x2_of_e4m3(x1), b2 = f16x2_of_e4m3(x0 >> 16), b3 = f16x2_of_e4m3(x1 >> 16);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    mma_16x8x16(o[m][p * S::kVal + j], pa[m], b0, b1);
+                    mma_16x8x16(o[m][p * S::kVal + j + 1], pa[m], b2, b3);
+                }
+            }
+        }
+    }
+    if (bad) report_invalid(g.a.status);
+
+    // ---- the warps' results together: maximum, sum and o of every row, through shared memory ----
+    cp_async_wait<0>();
+    __syncthreads();                                         // (the ring is idle)
+    constexpr int kLine = D + 4;                             // floats of a row: o, then maximum, sum
+    float* join = reinterpret_cast<float*>(smem + S::kQuery);
+    const float to_real = ref * 3.0517578125e-5f;            // 2^-15
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = 2 * m + h;
+            float* line = join + (warp * S::kRows + 16 * m + 8 * h + gq) * kLine;
+            const float total = quad_sum(sum[i]);
+#pragma unroll
+            for (int p = 0; p < S::kValPieces; ++p)
+#pragma unroll
+                for (int j = 0; j < S::kVal; ++j) {
+                    line[p * 8 * S::kVal + 2 * cq * S::kVal + j] = o[m][p * S::kVal + j][2 * h] * to_real;
+                    line[p * 8 * S::kVal + (2 * cq + 1) * S::kVal + j] = o[m][p * S::kVal + j][2 * h + 1] * to_real;
+                }
+            if (cq == 0) { line[D] = top[i]; line[D + 1] = total; }
+        }
+    __syncthreads();
+    const auto store = [&](int r, int i, float v) { store_one(g.a.y, (long long)row_token(r) * g.a.y_token + (long long)row_head(r) * g.a.y_head + i, g.a.type, v); };
+    const long long tile = (long long)blockIdx.x * c.heads + head;
+    float* left = g.partial + (tile * g.splits + blockIdx.z) * (S::kRows * (D + 2));
+    for (int e = threadIdx.x; e < rows * D; e += kAttendWarps * 32) {
+        const int r = e / D, i = e - r * D;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kAttendWarps; ++w) mx = fmaxf(mx, join[(w * S::kRows + r) * kLine + D]);
+        const float at = mx == -INFINITY ? 0.f : mx;
+        float v = 0.f, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttendWarps; ++w) {
+            const float* line = join + (w * S::kRows + r) * kLine;
+            const float k = exp2f(line[D] - at);
+            if (line[D + 1] != 0.f) { v += line[i] * k; l += line[D + 1] * k; }      // (a warp without tokens has nothing)
+        }
+        if (active == 1) store(r, i, l != 0.f ? v / l : 0.f);
+        else {
+            left[r * D + i] = v;
+            if (i == 0) { left[S::kRows * D + 2 * r] = mx; left[S::kRows * D + 2 * r + 1] = l; }
+        }
+    }
+    if (active == 1) return;
+
+    // ---- the splits together, by the last CTA of the tile ----
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last_one = atomicAdd(g.counters + tile, 1u) == (unsigned)active - 1u;
+    __syncthreads();
+    if (!last_one) return;
+    __threadfence();
+    const float* parts = g.partial + tile * g.splits * (S::kRows * (D + 2));
+    for (int e = threadIdx.x; e < rows * D; e += kAttendWarps * 32) {
+        const int r = e / D, i = e - r * D;
+        float mx = -INFINITY;
+        for (int z = 0; z < active; ++z) mx = fmaxf(mx, __ldcg(parts + (long long)z * (S::kRows * (D + 2)) + S::kRows * D + 2 * r));
+        const float at = mx == -INFINITY ? 0.f : mx;
+        float v = 0.f, l = 0.f;
+        for (int z = 0; z < active; ++z) {
+            const float* part = parts + (long long)z * (S::kRows * (D + 2));
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + S::kRows * D + 2 * r));
+            const float k = exp2f(ml.x - at);
+            if (ml.y != 0.f) { v += __ldcg(part + r * D + i) * k; l += ml.y * k; }
+        }
+        store(r, i, l != 0.f ? v / l : 0.f);
+    }
+    if (threadIdx.x == 0) g.counters[tile] = 0u;             // ready for the next call
+}
+
+// ---- host ----
+
+static tt_status check_cache(const tt_cache& c) {
+    if (c.pages < 0 || c.heads < 0 || c.batch < 0 || c.max_pages < 0 || c.d < 0 || c.block < 0) return TT_ERR_INVALID_ARG;
+    if (c.block != 16 && c.block != 32 && c.block != 64 && c.block != 128) return TT_ERR_NOT_IMPLEMENTED;
+    if (c.d == 0 || c.d % 32 || c.d > 256) return TT_ERR_NOT_IMPLEMENTED;
+    if (c.heads > 32767 || (long long)c.max_pages * c.block > 0x7fffff00ll || c.batch > (1 << 24)) return TT_ERR_INVALID_ARG;
+    return TT_OK;
+}
+static tt_status check_cache_memory(const tt_cache& c) {
+    if (!c.table || c.table_row < c.max_pages || reinterpret_cast<uintptr_t>(c.table) % 4) return TT_ERR_INVALID_ARG;
+    for (int w = 0; w < 2; ++w) {
+        if (!c.data[w] || !c.scale[w] || reinterpret_cast<uintptr_t>(c.scale[w]) % 4 || !on16(c.data[w])) return TT_ERR_INVALID_ARG;
+        if (c.page[w] < 0 || c.head[w] < 0 || c.token[w] < 0 || c.page[w] % 16 || c.head[w] % 16 || c.token[w] % 16 || c.s_page[w] < 0 || c.s_head[w] < 0) return TT_ERR_INVALID_ARG;
+    }
+    return TT_OK;
+}
+
+// The layout of an attention call: what is split over how many CTAs.
+static tt_status plan_attend(const tt_cache_attention_args& a, Attend& g, long long& units, long long& bytes) {
+    const tt_cache& c = a.cache;
+    g = Attend{};
+    g.a = a;
+    const tt_status s = check_cache(c);
+    if (s != TT_OK) return s;
+    if ((a.type != TT_TYPE_F16 && a.type != TT_TYPE_BF16) || a.tokens < 0 || a.heads_q < 0 || a.window < 0 || a.max_count < 0 || a.max_length < 0 || !(a.scale == a.scale)) return TT_ERR_INVALID_ARG;
+    if (c.heads == 0 ? a.heads_q != 0 : a.heads_q % c.heads) return TT_ERR_INVALID_ARG;
+    if (a.window > 0 && !a.causal) return TT_ERR_INVALID_ARG;
+    units = 0; bytes = 0;
+    if (a.tokens == 0 || a.heads_q == 0 || c.batch == 0) return TT_OK;
+    g.group = a.heads_q / c.heads;
+    const int count = a.max_count > 0 && a.max_count < a.tokens ? a.max_count : a.tokens;
+    // Two fragments of 16 rows a warp where the rows of a sequence need them: a key that is fetched and converted serves both.
+    g.rows = (long long)count * g.group > 16 && c.d <= 128 ? 32 : 16;
+    units = (long long)a.tokens * g.group / g.rows + c.batch;
+    if (units * c.heads > 0x7fffffffll) return TT_ERR_INVALID_ARG;
+    g.max_length = c.pages > 0 ? c.max_pages * c.block : 0;
+    if (a.max_length > 0 && a.max_length < g.max_length) g.max_length = a.max_length;
+    long long span = g.max_length;
+    if (a.window > 0 && a.window + (long long)(g.rows / g.group + 2) < span) span = a.window + (long long)(g.rows / g.group + 2);
+    span += kRun;
+    // Every SM is to have three CTAs at work, but a split is no shorter than what makes joining it cheap.
+    const long long tiles = units * c.heads;
+    constexpr int kLeast = 4 * kAttendWarps * kRun;
+    long long chunk = (span * tiles + 3 * kSms - 1) / (3 * kSms);
+    chunk = (chunk + kAttendWarps * kRun - 1) / (kAttendWarps * kRun) * (kAttendWarps * kRun);
+    if (chunk < kLeast) chunk = kLeast;
+    if (chunk > 2048) chunk = 2048;
+    while ((span + chunk - 1) / chunk > 65535 || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
+    g.chunk = (int)chunk;
+    g.splits = (int)((span + chunk - 1) / chunk);
+    if (g.splits > 1) bytes = (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (c.d + 2) * 4;
+    g.scale_log2 = a.scale * 1.4426950408889634f;
+    return TT_OK;
+}
+
+template <int D, int MT>
+static cudaError_t launch_attend(const Attend& g, long long units, void* stream) {
+    typedef AttendShape<D, MT> S;
+    static OncePerDevice raised;
+    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_few_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
+    if (ready != cudaSuccess) return ready;
+    return launch(tt_attend_few_kernel<D, MT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, g);
+}
+template <int D>
+static cudaError_t launch_attend_rows(const Attend& g, long long units, void* stream) {
+    if constexpr (D <= 128) if (g.rows == 32) return launch_attend<D, 2>(g, units, stream);
+    return launch_attend<D, 1>(g, units, stream);
+}
+
+}  // namespace tt
+
+using namespace tt;
+
+extern "C" tt_status tt_cache_append(const tt_cache_append_args* a, void* stream) {
+    if (!a || !known_type(a->type) || a->tokens < 0) return TT_ERR_INVALID_ARG;
+    const tt_cache& c = a->cache;
+    tt_status s = check_cache(c);
+    if (s != TT_OK) return s;
+    if (a->tokens == 0 || c.batch == 0 || c.heads == 0) return TT_OK;
+    s = check_cache_memory(c);
+    if (s != TT_OK) return s;
+    const int bytes = type_bytes(a->type);
+    if (!a->starts || !a->lengths || !a->status || reinterpret_cast<uintptr_t>(a->starts) % 4 || reinterpret_cast<uintptr_t>(a->lengths) % 4 || reinterpret_cast<uintptr_t>(a->status) % 4)
+        return TT_ERR_INVALID_ARG;
+    bool wide = true;
+    for (int w = 0; w < 2; ++w) {
+        if (!a->x[w] || reinterpret_cast<uintptr_t>(a->x[w]) % (uintptr_t)bytes || a->x_token[w] < 0 || a->x_head[w] < 0) return TT_ERR_INVALID_ARG;
+        wide = wide && on16(a->x[w]) && a->x_token[w] * bytes % 16 == 0 && a->x_head[w] * bytes % 16 == 0;
+    }
+    const long long units = a->tokens / c.block + 2ll * c.batch;
+    if (units > 0x7fffffff) return TT_ERR_INVALID_ARG;
+    // A warp has a page's tokens where there is hardly more than one of them, eight warps where there are many.
+    const long long values = (long long)(a->tokens / c.batch < c.block ? a->tokens / c.batch : c.block) * c.d;
+    const int threads = values <= 512 ? 32 : values <= 2048 ? 128 : 256;
+    const dim3 grid((unsigned)units, 2u * (unsigned)c.heads, 1);
+    const auto go = [&](auto kern) { return status_of(launch(kern, grid, threads, 0, 1, stream, *a)); };
+    if (a->type == TT_TYPE_F32) return wide ? go(tt_cache_append_kernel<TT_TYPE_F32, true>) : go(tt_cache_append_kernel<TT_TYPE_F32, false>);
+    if (a->type == TT_TYPE_F16) return wide ? go(tt_cache_append_kernel<TT_TYPE_F16, true>) : go(tt_cache_append_kernel<TT_TYPE_F16, false>);
+    return wide ? go(tt_cache_append_kernel<TT_TYPE_BF16, true>) : go(tt_cache_append_kernel<TT_TYPE_BF16, false>);
+}
+
+extern "C" tt_status tt_cache_attention_workspace(const tt_cache_attention_args* a, int64_t* bytes) {
+    if (!a || !bytes) return TT_ERR_INVALID_ARG;
+    Attend g;
+    long long units = 0, need = 0;
+    const tt_status s = plan_attend(*a, g, units, need);
+    *bytes = s == TT_OK ? need : 0;
+    return s;
+}
+
+extern "C" tt_status tt_cache_attention(const tt_cache_attention_args* a, void* stream) {
+    if (!a) return TT_ERR_INVALID_ARG;
+    Attend g;
+    long long units = 0, need = 0;
+    tt_status s = plan_attend(*a, g, units, need);
+    if (s != TT_OK || units == 0) return s;
+    const tt_cache& c = a->cache;
+    if (g.max_length > 0) s = check_cache_memory(c);
+    if (s != TT_OK) return s;
+    if (!a->q || !a->y || !a->starts || !a->lengths || !a->status || a->q_token < 0 || a->q_head < 0 || a->y_token < 0 || a->y_head < 0) return TT_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(a->q) % 2 || reinterpret_cast<uintptr_t>(a->y) % 2 || reinterpret_cast<uintptr_t>(a->starts) % 4 || reinterpret_cast<uintptr_t>(a->lengths) % 4 ||
+        reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
+    if (need > 0 && (!a->workspace || !on16(a->workspace) || a->workspace_bytes < need)) return TT_ERR_INVALID_ARG;
+    g.counters = static_cast<unsigned*>(a->workspace);
+    g.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + (units * c.heads * 4 + 15) / 16 * 16);
+    switch (c.d) {
+        case 32: return status_of(launch_attend_rows<32>(g, units, stream));
+        case 64: return status_of(launch_attend_rows<64>(g, units, stream));
+        case 96: return status_of(launch_attend_rows<96>(g, units, stream));
+        case 128: return status_of(launch_attend_rows<128>(g, units, stream));
+        case 160: return status_of(launch_attend_rows<160>(g, units, stream));
+        case 192: return status_of(launch_attend_rows<192>(g, units, stream));
+        case 224: return status_of(launch_attend_rows<224>(g, units, stream));
+        default: return status_of(launch_attend_rows<256>(g, units, stream));
+    }
+}

@@ -198,6 +198,20 @@ private:
 
 }  // namespace
 
+// A matrix of bytes [rows][cols], rows `pitch` bytes apart -> 2-D tensor map, box = [128, box_rows], 128-byte swizzle: K-major tiles of 8-bit
+// operands.
+tt_status encode_bytes(void* out, const void* base, long long cols, long long rows, long long pitch, int box_rows) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return TT_ERR_CUDA;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = fn(reinterpret_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? TT_OK : TT_ERR_CUDA;
+}
+
 // Forget what the workspace holds of re-packed filters, and the workspaces that passes captured under the record in force read.
 static void forget_filters(tt_workload* w) {
     for (void* p : w->kept) cudaFree(p);

@@ -1,0 +1,444 @@
+// e4m3 operands with a scale for each block of 128: their quantisation and the dense layer over them.
+#include <cuda_runtime.h>
+#include <cuda.h>
+#include <cstring>
+#include "tt_ptx.cuh"
+#include "tt_f8.cuh"
+
+namespace tt {
+
+// ---- quantisation ---------------------------------------------------------------------------------------------------------
+//
+// s = 2^ceil(log2(max |x| / 448)) comes from the bits of the maximum, x / s is a product with the power 1 / s, so the only rounding is the
+// one to e4m3.  Bound by memory: every value is read once and kept in registers between the maximum and the conversion.
+
+// Rows of activations: 16 lanes have a block of 128 columns, 8 values each; a warp has UNROLL * 256 columns of one row in flight.
+template <int TYPE, int UNROLL>
+__global__ void __launch_bounds__(256) tt_quantize_rows_kernel(const tt_quantize_args a, int pieces, long long tasks, int wide) {
+    pdl_allow_next();
+    pdl_wait_prev();
+    const int lane = threadIdx.x & 31;
+    const long long task = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (task >= tasks) return;
+    typedef typename Element<TYPE>::type T;
+    const long long row = task / pieces;
+    const int first = (int)(task - row * pieces) * (256 * UNROLL) + 8 * lane;
+    const T* x = static_cast<const T*>(a.x) + row * a.x_row;
+    uint8_t* q = static_cast<uint8_t*>(a.q) + row * a.q_row;
+    float v[UNROLL][8];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int c = first + 256 * u;
+        if (wide && c + 8 <= a.kk) load_wide<TYPE, 8>(x + c, v[u]);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[u][i] = c + i < a.kk ? Element<TYPE>::up(x[c + i]) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const int c = first + 256 * u;
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = finite_max(most, v[u][i]);
+#pragma unroll
+        for (int d = 8; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+        const float s = power_scale(most), inv = power_inverse(s);
+        if (c >= a.kk) continue;
+        const uint32_t lo = to_e4m3x4(v[u][0] * inv, v[u][1] * inv, v[u][2] * inv, v[u][3] * inv);
+        const uint32_t hi = to_e4m3x4(v[u][4] * inv, v[u][5] * inv, v[u][6] * inv, v[u][7] * inv);
+        if (wide && c + 8 <= a.kk) *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (c + i < a.kk) q[c + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+        }
+        if ((lane & 15) == 0) a.scales[(long long)(c >> 7) * a.s_block + row * a.s_row] = s;
+    }
+}
+
+// Blocks of 128 x 128: a CTA each, a thread has 8 columns of every sixteenth row.
+template <int TYPE>
+__global__ void __launch_bounds__(256) tt_quantize_blocks_kernel(const tt_quantize_args a, int blocks, int wide) {
+    __shared__ float warp_most[8];
+    pdl_allow_next();
+    pdl_wait_prev();
+    typedef typename Element<TYPE>::type T;
+    const int rb = (int)blockIdx.x / blocks, kb = (int)blockIdx.x - rb * blocks;
+    const int c = kb * 128 + 8 * ((int)threadIdx.x & 15), r0 = rb * 128 + ((int)threadIdx.x >> 4);
+    float v[8][8], most = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = r0 + 16 * j;
+        const T* x = static_cast<const T*>(a.x) + (long long)r * a.x_row;
+        if (r < a.m && wide && c + 8 <= a.kk) load_wide<TYPE, 8>(x + c, v[j]);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = r < a.m && c + i < a.kk ? Element<TYPE>::up(x[c + i]) : 0.f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = finite_max(most, v[j][i]);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+    if ((threadIdx.x & 31) == 0) warp_most[threadIdx.x >> 5] = most;
+    __syncthreads();
+    most = warp_most[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) most = fmaxf(most, warp_most[w]);
+    const float s = power_scale(most), inv = power_inverse(s);
+    if (threadIdx.x == 0) a.scales[(long long)kb * a.s_block + (long long)rb * a.s_row] = s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = r0 + 16 * j;
+        if (r >= a.m || c >= a.kk) continue;
+        uint8_t* q = static_cast<uint8_t*>(a.q) + (long long)r * a.q_row;
+        const uint32_t lo = to_e4m3x4(v[j][0] * inv, v[j][1] * inv, v[j][2] * inv, v[j][3] * inv);
+        const uint32_t hi = to_e4m3x4(v[j][4] * inv, v[j][5] * inv, v[j][6] * inv, v[j][7] * inv);
+        if (wide && c + 8 <= a.kk) *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
+        else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) if (c + i < a.kk) q[c + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+        }
+    }
+}
+
+// ---- the dense layer ------------------------------------------------------------------------------------------------------
+//
+// D[128 rows, TN] = A B^T by tcgen05.mma kind::f8f6f4 over one block of 128 columns at a time (four steps of 32), each block into the next of
+// the accumulators in tensor memory.  The read-out warps take a block's sums, multiply them by its scales and add them up in registers, in 32
+// bits, while the tensor core is at the following blocks: the scales may be any values, and no sum is longer than 128 before it
+// is added in full precision.
+//
+// Rows on the 128 lanes are the tokens, or (SWAP) the weights' rows where there are too few tokens to fill them.  `split` CTAs of
+// a cluster share a tile's blocks where there are fewer tiles than SMs, leave their sums in shared memory and add up a band of columns each,
+// in the order of the splits.
+
+struct DenseF8 {
+    const float* a_scale; long long as_row, as_block;     // of operand A's rows (normal: per row, SWAP: per 128 rows)
+    const float* b_scale; long long bs_row, bs_block;
+    const float* bias; void* y; long long y_row;
+    unsigned* status;
+    int rows_a, rows_b, blocks, blocks_per_split, split, stages, tiles_a;
+    int y_type, act, wide;
+    unsigned idesc;
+    unsigned long long wait_ns;
+};
+
+constexpr int kF8Threads = 320;                            // warp 0 TMA, warp 1 MMA + tensor memory, warps 2-9 read-out
+constexpr unsigned kF8TileA = 128 * 128;
+constexpr int kF8MaxStages = 8;
+
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr));
+}
+__device__ __forceinline__ float4 ld_cluster_v4f(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+template <int TN, bool SWAP>
+__global__ void __launch_bounds__(kF8Threads, 1)
+tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const DenseF8 g) {
+    constexpr int kBufs = 512 / TN < 4 ? 512 / TN : 4;     // accumulators
+    constexpr int kCols = TN / 2;                          // columns of a read-out warp
+    constexpr uint32_t kStage = kF8TileA + TN * 128u;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[kBufs], acc_empty[kBufs], drained;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    volatile int* abortp = &abort_flag;
+    pdl_allow_next();
+    const int tile_a = (int)blockIdx.x % g.tiles_a, tile_b = (int)blockIdx.x / g.tiles_a;
+    const int kb0 = (int)blockIdx.z * g.blocks_per_split, kb1 = min(g.blocks, kb0 + g.blocks_per_split);
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
+        for (int i = 0; i < kBufs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 8u); }
+        mbar_init(smem_u32(&drained), 1u);
+        abort_flag = 0;
+        fence_mbar_init();
+        fence_proxy_async_shared();
+    }
+    constexpr uint32_t kTmemCols = kBufs * TN < 32 ? 32 : kBufs * TN;
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *(volatile uint32_t*)&tmem_slot;
+    pdl_wait_prev();
+
+    float acc[kCols];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+    const int quad = warp & 3, half = (warp - 2) >> 2;      // a warp reads the lanes of its quadrant, one half of the columns
+    if (warp == 0) {
+        if (elect_one()) {
+            int st = 0, used = 0;
+            uint32_t ph = 0;
+            for (int kb = kb0; kb < kb1; ++kb) {
+                if (!mbar_wait(smem_u32(&empty_bar[st]), ph ^ 1u, abortp, g.status, 1u, g.wait_ns)) break;
+                const uint32_t bar = smem_u32(&full_bar[st]), dst = base + (uint32_t)st * kStage;
+                mbar_expect_tx(bar, kStage);
+                tma_load_2d(dst, &tmap_a, bar, kb * 128, tile_a * 128);
+                tma_load_2d(dst + kF8TileA, &tmap_b, bar, kb * 128, tile_b * TN);
+                ++used;
+                if (++st == g.stages) { st = 0; ph ^= 1u; }
+            }
+            // shared memory stays until the last copy into each stage has landed, also when somebody gave up (bounded)
+            const unsigned long long t0 = global_timer_ns();
+            for (int i = 0; i < g.stages && i < used; ++i) {
+                const uint32_t turn = (uint32_t)((used - 1 - i) / g.stages) & 1u;
+                while (!mbar_try_wait(smem_u32(&full_bar[i]), turn)) if (global_timer_ns() - t0 > g.wait_ns) break;
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (elect_one()) {
+            const uint64_t d0 = make_desc(0u, 128);
+            int st = 0, buf = 0;
+            uint32_t ph = 0, aph = 0;
+            bool ok = true;
+            for (int kb = kb0; kb < kb1 && ok; ++kb) {
+                ok = mbar_wait(smem_u32(&acc_empty[buf]), aph ^ 1u, abortp, g.status, 2u, g.wait_ns) &&
+                     mbar_wait(smem_u32(&full_bar[st]), ph, abortp, g.status, 3u, g.wait_ns);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t a = base + (uint32_t)st * kStage, b = a + kF8TileA;
+                const uint64_t da = d0 + (uint64_t)((a & 0x3FFFFu) >> 4), db = d0 + (uint64_t)((b & 0x3FFFFu) >> 4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f8(tmem_base + (uint32_t)(buf * TN), da + 2u * k, db + 2u * k, g.idesc, k > 0 ? 1u : 0u);
+                mma_commit(smem_u32(&empty_bar[st]));
+                mma_commit(smem_u32(&acc_full[buf]));
+                if (++st == g.stages) { st = 0; ph ^= 1u; }
+                if (++buf == kBufs) { buf = 0; aph ^= 1u; }
+            }
+            if (!ok) {                                      // nothing of what was issued is to run on behind this CTA (bounded)
+                mma_commit(smem_u32(&drained));
+                const unsigned long long t0 = global_timer_ns();
+                while (!mbar_try_wait(smem_u32(&drained), 0u)) if (global_timer_ns() - t0 > g.wait_ns) break;
+            }
+        }
+        __syncwarp();
+    } else {
+        // the scales of the next block are under way while this one's products are waited for
+        const int row = tile_a * 128 + quad * 32 + lane;
+        const int cb = min(tile_b * TN + half * kCols + lane % kCols, g.rows_b - 1);      // SWAP: the lane's column
+        const float* as = g.a_scale + (SWAP ? (long long)tile_a : (long long)min(row, g.rows_a - 1)) * g.as_row;
+        const float* bs = g.b_scale + (SWAP ? (long long)cb : (long long)((tile_b * TN) >> 7)) * g.bs_row;
+        int buf = 0;
+        uint32_t aph = 0;
+        float sa = 0.f, sb = 0.f;
+        if (kb0 < kb1) { sa = __ldg(as + kb0 * g.as_block); sb = __ldg(bs + kb0 * g.bs_block); }
+        for (int kb = kb0; kb < kb1; ++kb) {
+            const float s = sa * sb;
+            if (kb + 1 < kb1) { sa = __ldg(as + (kb + 1) * g.as_block); sb = __ldg(bs + (kb + 1) * g.bs_block); }
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&acc_full[buf]), aph, abortp, g.status, 4u, g.wait_ns))) break;
+            tc_fence_after();
+            const uint32_t t = tmem_base + (uint32_t)(buf * TN + half * kCols) + ((uint32_t)(quad * 32) << 16);
+            uint32_t r[kCols];
+            if constexpr (kCols >= 32) {
+#pragma unroll
+                for (int j = 0; j < kCols; j += 32) tmem_ld32(t + (uint32_t)j, *reinterpret_cast<uint32_t(*)[32]>(&r[j]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < kCols; j += 8) tmem_ld8(t + (uint32_t)j, &r[j]);
+            }
+            tmem_wait_ld();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&acc_empty[buf]));
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+                const float sj = SWAP ? __shfl_sync(0xffffffffu, s, j) : s;
+                acc[j] = fmaf(__uint_as_float(r[j]), sj, acc[j]);
+            }
+            if (++buf == kBufs) { buf = 0; aph ^= 1u; }
+        }
+    }
+
+    // ---- out: y[token][column of the weights] ----
+    const int first_col = tile_b * TN + half * kCols;
+    if (g.split == 1) {
+        if (warp >= 2 && !*abortp) {
+            const int row = tile_a * 128 + quad * 32 + lane;
+            if constexpr (SWAP) {
+                if (row < g.rows_a) {
+                    const float b = g.bias ? __ldg(g.bias + row) : 0.f;
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j)
+                        if (first_col + j < g.rows_b) store_one(g.y, (long long)(first_col + j) * g.y_row + row, g.y_type, apply_act(acc[j] + b, g.act));
+                }
+            } else if (row < g.rows_a) {
+                const long long at = (long long)row * g.y_row + first_col;
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) {
+                    const float b = g.bias && first_col + j < g.rows_b ? __ldg(g.bias + first_col + j) : 0.f;
+                    acc[j] = apply_act(acc[j] + b, g.act);
+                }
+                if (g.wide && first_col + kCols <= g.rows_b) {
+                    if (g.y_type == TT_TYPE_F32) store_wide<TT_TYPE_F32, kCols>(static_cast<float*>(g.y) + at, acc);
+                    else if (g.y_type == TT_TYPE_F16) store_wide<TT_TYPE_F16, kCols>(static_cast<__half*>(g.y) + at, acc);
+                    else store_wide<TT_TYPE_BF16, kCols>(static_cast<__nv_bfloat16*>(g.y) + at, acc);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) if (first_col + j < g.rows_b) store_one(g.y, at + j, g.y_type, acc[j]);
+                }
+            }
+        }
+    } else {
+        // partial sums to shared memory (the pipeline is idle: the last block's products are done with it), SWAP: [column][128 rows], else
+        // [row][TN + 4]
+        constexpr uint32_t kLine = SWAP ? 512u : (TN + 4) * 4u;
+        __syncthreads();
+        if (warp >= 2) {
+            const uint32_t r = (uint32_t)(quad * 32 + lane);
+            if constexpr (SWAP) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) st_shared_f32(base + (uint32_t)(half * kCols + j) * kLine + r * 4u, acc[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kCols; j += 4) st_shared_v4(base + r * kLine + (uint32_t)(half * kCols + j) * 4u, acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+            }
+        }
+        cluster_arrive();
+        cluster_wait();
+        if (warp >= 2 && !*abortp) {
+            // a band of lines for each CTA of the cluster, four values at a time
+            constexpr int kLines = SWAP ? TN : 128, kQuads = SWAP ? 32 : TN / 4;
+            const int per = (kLines + g.split - 1) / g.split, l0 = (int)blockIdx.z * per, l1 = min(kLines, l0 + per);
+            for (int e = (int)threadIdx.x - 64 + l0 * kQuads; e < l1 * kQuads; e += 256) {
+                const int line = e / kQuads, c = 4 * (e - line * kQuads);
+                const int token = (SWAP ? tile_b * TN : tile_a * 128) + line, col = (SWAP ? tile_a * 128 : tile_b * TN) + c;
+                const int tokens = SWAP ? g.rows_b : g.rows_a, cols = SWAP ? g.rows_a : g.rows_b;
+                if (token >= tokens || col >= cols) continue;
+                float v[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int p = 0; p < g.split; ++p) {
+                    const float4 f = ld_cluster_v4f(map_to_peer(base + (uint32_t)line * kLine + (uint32_t)c * 4u, (uint32_t)p));
+                    v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
+                }
+                const long long at = (long long)token * g.y_row + col;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float b = g.bias && col + i < cols ? __ldg(g.bias + col + i) : 0.f;
+                    v[i] = apply_act(v[i] + b, g.act);
+                }
+                if (g.wide && col + 4 <= cols) {
+                    if (g.y_type == TT_TYPE_F32) *reinterpret_cast<float4*>(static_cast<float*>(g.y) + at) = make_float4(v[0], v[1], v[2], v[3]);
+                    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.y) + at) =
+                        g.y_type == TT_TYPE_F16 ? make_uint2(down2<TT_TYPE_F16>(v[0], v[1]), down2<TT_TYPE_F16>(v[2], v[3]))
+                                                : make_uint2(down2<TT_TYPE_BF16>(v[0], v[1]), down2<TT_TYPE_BF16>(v[2], v[3]));
+                } else {
+                    for (int i = 0; i < 4 && col + i < cols; ++i) store_one(g.y, at + i, g.y_type, v[i]);
+                }
+            }
+        }
+        cluster_arrive();                                   // nobody leaves while its sums may still be read
+        cluster_wait();
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem_base, kTmemCols);
+    }
+}
+
+template <int TN, bool SWAP>
+static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb, DenseF8 g, void* stream) {
+    constexpr int kStageBytes = (int)kF8TileA + TN * 128;
+    static OncePerDevice raised;
+    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_dense_f8_kernel<TN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemLimit); });
+    if (ready != cudaSuccess) return ready;
+    const int fits = (kDynSmemLimit - 1024) / kStageBytes;
+    g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
+    const int tiles_b = (g.rows_b + TN - 1) / TN;
+    return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes, g.split, stream, ta, tb, g);
+}
+
+}  // namespace tt
+
+using namespace tt;
+
+extern "C" tt_status tt_quantize(const tt_quantize_args* a, void* stream) {
+    if (!a || !known_type(a->x_type) || a->m < 0 || a->kk < 0 || (a->block_rows != 1 && a->block_rows != kF8Block)) return TT_ERR_INVALID_ARG;
+    if (a->m == 0 || a->kk == 0) return TT_OK;
+    const int64_t bytes = type_bytes(a->x_type);
+    if (!a->x || !a->q || !a->scales || a->x_row < a->kk || a->q_row < a->kk || a->s_row < 0 || a->s_block < 0) return TT_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(a->x) % (uintptr_t)bytes || reinterpret_cast<uintptr_t>(a->scales) % 4) return TT_ERR_INVALID_ARG;
+    const int wide = on16(a->x) && a->x_row * bytes % 16 == 0 && reinterpret_cast<uintptr_t>(a->q) % 8 == 0 && a->q_row % 8 == 0;
+    const int blocks = (a->kk + kF8Block - 1) / kF8Block;
+    if (a->block_rows == kF8Block) {
+        const long long grid = (long long)blocks * ((a->m + kF8Block - 1) / kF8Block);
+        if (grid > 0x7fffffff) return TT_ERR_INVALID_ARG;
+        const auto kern = a->x_type == TT_TYPE_F32 ? tt_quantize_blocks_kernel<TT_TYPE_F32> : a->x_type == TT_TYPE_F16 ? tt_quantize_blocks_kernel<TT_TYPE_F16> : tt_quantize_blocks_kernel<TT_TYPE_BF16>;
+        return status_of(launch(kern, dim3((unsigned)grid, 1, 1), 256, 0, 1, stream, *a, blocks, wide));
+    }
+    // Four loads in flight per lane, where that leaves every SM some warps; few rows are spread over as many warps as they have.
+    const bool deep = (long long)a->m * a->kk >= (1 << 21);
+    const int step = deep ? 1024 : 256, pieces = (a->kk + step - 1) / step, threads = deep ? 256 : 64;
+    const long long tasks = (long long)a->m * pieces, grid = (tasks + threads / 32 - 1) / (threads / 32);
+    if (grid > 0x7fffffff) return TT_ERR_INVALID_ARG;
+    const auto kern = deep ? (a->x_type == TT_TYPE_F32 ? tt_quantize_rows_kernel<TT_TYPE_F32, 4> : a->x_type == TT_TYPE_F16 ? tt_quantize_rows_kernel<TT_TYPE_F16, 4> : tt_quantize_rows_kernel<TT_TYPE_BF16, 4>)
+                           : (a->x_type == TT_TYPE_F32 ? tt_quantize_rows_kernel<TT_TYPE_F32, 1> : a->x_type == TT_TYPE_F16 ? tt_quantize_rows_kernel<TT_TYPE_F16, 1> : tt_quantize_rows_kernel<TT_TYPE_BF16, 1>);
+    return status_of(launch(kern, dim3((unsigned)grid, 1, 1), threads, 0, 1, stream, *a, pieces, tasks, wide));
+}
+
+extern "C" tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* stream) {
+    if (!a || !known_type(a->y_type) || a->m < 0 || a->nn < 0 || a->kk < 0 || a->act < TT_ACT_NONE || a->act > TT_ACT_GELU_ERF) return TT_ERR_INVALID_ARG;
+    if (a->m == 0 || a->nn == 0) return TT_OK;
+    if (a->kk == 0) return TT_ERR_INVALID_ARG;             // (there is no sum to take)
+    if (!a->x || !a->w || !a->x_scale || !a->w_scale || !a->y || !a->status) return TT_ERR_INVALID_ARG;
+    if (a->x_row < a->kk || a->w_row < a->kk || a->y_row < a->nn || a->xs_row < 0 || a->xs_block < 0 || a->ws_row < 0 || a->ws_block < 0) return TT_ERR_INVALID_ARG;
+    if (!on16(a->x) || !on16(a->w) || a->x_row % 16 || a->w_row % 16) return TT_ERR_INVALID_ARG;
+    const int64_t bytes = type_bytes(a->y_type);
+    if (reinterpret_cast<uintptr_t>(a->y) % (uintptr_t)bytes || reinterpret_cast<uintptr_t>(a->x_scale) % 4 || reinterpret_cast<uintptr_t>(a->w_scale) % 4 ||
+        reinterpret_cast<uintptr_t>(a->bias) % 4 || reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
+    DenseF8 g{};
+    g.bias = a->bias; g.y = a->y; g.y_row = a->y_row; g.status = a->status; g.y_type = a->y_type; g.act = a->act;
+    g.wide = on16(a->y) && a->y_row * bytes % 16 == 0;
+    g.blocks = (a->kk + kF8Block - 1) / kF8Block;
+    g.wait_ns = 1000000000ull;
+    // Up to 64 tokens: the weights' rows take the 128 lanes, and the tokens a tile of 16, 32 or 64 columns.
+    const bool swap = a->m <= 64;
+    const int tn = swap ? (a->m <= 16 ? 16 : a->m <= 32 ? 32 : 64) : 128;
+    g.rows_a = swap ? a->nn : a->m; g.rows_b = swap ? a->m : a->nn;
+    g.tiles_a = (g.rows_a + 127) / 128;
+    const long long tiles = (long long)g.tiles_a * ((g.rows_b + tn - 1) / tn);
+    if (tiles > 0x7fffffff) return TT_ERR_INVALID_ARG;
+    g.split = 1;
+    while (g.split < 8 && tiles * g.split * 2 <= kSms && g.split * 4 <= g.blocks) g.split *= 2;
+    g.blocks_per_split = (g.blocks + g.split - 1) / g.split;
+    g.idesc = (1u << 4) | ((unsigned)(tn >> 3) << 17) | ((unsigned)(kHwTileM >> 4) << 24);
+    CUtensorMap tx, tw;
+    tt_status s = encode_bytes(&tx, a->x, a->kk, a->m, a->x_row, swap ? tn : 128);
+    if (s == TT_OK) s = encode_bytes(&tw, a->w, a->kk, a->nn, a->w_row, swap ? 128 : tn);
+    if (s != TT_OK) return s;
+    if (swap) {
+        g.a_scale = a->w_scale; g.as_row = a->ws_row; g.as_block = a->ws_block; g.b_scale = a->x_scale; g.bs_row = a->xs_row; g.bs_block = a->xs_block;
+        return status_of(tn == 16 ? launch_dense_f8<16, true>(tw, tx, g, stream) : tn == 32 ? launch_dense_f8<32, true>(tw, tx, g, stream) : launch_dense_f8<64, true>(tw, tx, g, stream));
+    }
+    g.a_scale = a->x_scale; g.as_row = a->xs_row; g.as_block = a->xs_block; g.b_scale = a->w_scale; g.bs_row = a->ws_row; g.bs_block = a->ws_block;
+    return status_of(launch_dense_f8<128, false>(tx, tw, g, stream));
+}

@@ -272,4 +272,5 @@ size_t tensor_elems(const tt_workload* w, int which);   // 0 x, 1 w, 2 bias, 3 r
 tt_status bind_device(tt_workload* w);                          // workspace + status word
 tt_status launch(tt_workload* w, const tt_tensors* t, void* stream);
 void release_device(tt_workload* w);
+tt_status encode_bytes(void* out, const void* base, long long cols, long long rows, long long pitch, int box_rows);   // of 8-bit operands
 }  // namespace tt

@@ -54,6 +54,23 @@ PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyLong_FromLong((long)s);
 }
 
+// call(function, arguments, stream) -> status: an entry point of the 8-bit operators, its arguments a ctypes structure that the caller keeps
+// alive and that has the size the entry point takes (the binding makes both).
+PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != 3) { PyErr_SetString(PyExc_TypeError, "call(function, arguments, stream)"); return nullptr; }
+    typedef tt_status (*Fn)(const void*, void*);
+    const Fn fn = reinterpret_cast<Fn>(PyLong_AsVoidPtr(args[0]));
+    void* stream = PyLong_AsVoidPtr(args[2]);
+    Py_buffer view;
+    if (PyErr_Occurred() || PyObject_GetBuffer(args[1], &view, PyBUF_SIMPLE) != 0) return nullptr;
+    tt_status s;
+    Py_BEGIN_ALLOW_THREADS
+    s = fn(view.buf, stream);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&view);
+    return PyLong_FromLong((long)s);
+}
+
 bool long_attr(PyObject* o, PyObject* name, void** as_ptr, long* as_long) {
     PyObject* v = PyObject_GetAttr(o, name);
     if (!v) return false;
@@ -186,6 +203,7 @@ PyObject* query(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef kMethods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, "bind(tt_run, tt_run_chain): addresses of the library's entry points"},
     {"run", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(run)), METH_FASTCALL, "run(handle, tensors, stream) -> tt_status"},
+    {"call", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call)), METH_FASTCALL, "call(function, arguments, stream) -> tt_status"},
     {"run_chain", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(run_chain)), METH_FASTCALL,
      "run_chain(workloads, steps, tensors, plan, streams) -> (tt_status, index of the failing node or -1)"},
     {"query_chain", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(query)), METH_FASTCALL,
