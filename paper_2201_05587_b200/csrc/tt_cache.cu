@@ -108,10 +108,11 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
 // One pass over the visible keys and values with a running maximum and sum of each row (a query of one head).  The heads that share a key
 // head are rows of one tile, so a key is read once for all of them.
 //
-// Tiles of 16 or 32 rows: the cache's bytes are the bound.  A warp takes runs of 64 tokens, 16 at a time.  Its lanes fetch just the
-// bytes that they multiply: the order of the reduction is free as long as both factors have it, so lane (g, c) of an m16n8k16 product takes
-// 16 bytes in a row of the key g, and of four values 16 bytes in a row of columns, and nothing is exchanged through shared
-// memory.  It is only the buffer of the copies under way, each lane's its own, so there is no barrier in the loop.
+// Tiles of 8 to 32 rows: the cache's bytes are the bound.  A warp takes runs of 64 tokens, 16 at a time, as the 16 rows of m16n8k16
+// products: scores^T = K Q^T and o^T = V^T P^T, so eight query rows cost half of what they would as rows.  Its lanes fetch just the bytes that they
+// multiply: the order of the reduction is free as long as both factors have it, so lane (g, c) takes 16 bytes in a row of the keys g and
+// g + 8, and of four values 16 bytes in a row of columns, and nothing is exchanged through shared memory.  It is only the buffer of the
+// copies under way, each lane's its own, so there is no barrier in the loop.
 //   e4m3 -> 16-bit floating point is exact, and so is a row of queries: brought to a maximum of 2^14..2^15 by a power of two, which the
 // scores' factor takes back.  Probabilities are rounded to 11 bits, times 2^15 and the page's scale over the largest so far, so that what is
 // 2^-29 of the largest still has all of them; sums are in 32 bits.
@@ -120,18 +121,31 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
 constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it
 constexpr int kRun = 64;                    // tokens that a warp takes in a row
 constexpr int kAttendWarps = 4;
+constexpr int kMostSplits = 256;            // of a sequence: the last CTA has the maxima and sums of all of them in shared memory
 
 struct Attend {
     tt_cache_attention_args a;
     int group, rows;                        // query heads of a key head; rows of a tile
     int chunk, splits, max_length;          // tokens of a split, most splits
+    int q_wide, y_wide;                     // four values of q, of y at a time
     float scale_log2;                       // the scale times log2(e)
     unsigned* counters; float* partial;
 };
 
-__device__ __forceinline__ void mma_16x8x16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// An 8 x 8 matrix of 16-bit values, a row's pair in lane (row, pair), transposed.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+    uint32_t t;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
+    return t;
+}
+__device__ __forceinline__ float exp2_fast(float x) {      // 2^x to two units in the last place; 0 below 2^-126
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 template <int N>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
@@ -145,33 +159,63 @@ __device__ __forceinline__ void read_shared(uint32_t addr, uint32_t (&v)[N / 4])
     else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v[0]) : "r"(addr) : "memory");
 }
 constexpr int widest(int bytes) { return bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : 4; }
-__device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+// Over the eight lanes that have the same pair of rows.
+__device__ __forceinline__ float octet_max(float v) {
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
 }
-__device__ __forceinline__ float quad_sum(float v) {
-    v += __shfl_xor_sync(0xffffffffu, v, 1);
-    return v + __shfl_xor_sync(0xffffffffu, v, 2);
+__device__ __forceinline__ float octet_sum(float v) {
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
 }
 // A non-zero byte for each e4m3 byte of the word that is NaN.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Four values of a 16-bit type.
+__device__ __forceinline__ void load_four(const void* p, long long i, int type, int wide, float (&v)[4]) {
+    if (wide) {
+        const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+        const float2 a = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.x) : up2<TT_TYPE_BF16>(u.x), b = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.y) : up2<TT_TYPE_BF16>(u.y);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = load_one(p, i + e, type);
+    }
+}
+__device__ __forceinline__ void store_four(void* p, long long i, int type, int wide, const float (&v)[4]) {
+    if (wide) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+            type == TT_TYPE_F16 ? make_uint2(down2<TT_TYPE_F16>(v[0], v[1]), down2<TT_TYPE_F16>(v[2], v[3])) : make_uint2(down2<TT_TYPE_BF16>(v[0], v[1]), down2<TT_TYPE_BF16>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_one(p, i + e, type, v[e]);
+    }
+}
 
-template <int D, int MT>
+// CTAs that their registers leave room for on an SM.
+constexpr int attend_ctas(int d, int nt) { return nt <= 2 && nt * d <= 128 ? 4 : nt * d <= 128 || (nt <= 2 && nt * d <= 256) ? 3 : 2; }
+
+template <int D, int NT>
 struct AttendShape {
     static constexpr int kKey = widest(D / 4), kKeyPieces = D / 4 / kKey;           // bytes of a key that a lane fetches at a time, and how often
     static constexpr int kVal = widest(D / 8), kValPieces = D / 8 / kVal;
-    static constexpr int kRows = 16 * MT;
+    static constexpr int kRows = 8 * NT;
+    static constexpr bool kQueryRegs = NT == 1 || NT * D <= 128;                     // the queries' fragments stay in registers
     static constexpr uint32_t kKeyBytes = 2u * kKeyPieces * 32u * kKey, kStage = kKeyBytes + 4u * kValPieces * 32u * kVal + 256u;      // 16 tokens, and each lane's copy of two scales
-    static constexpr int kStages = D <= 64 ? 6 : D <= 128 ? 4 : 3;
-    static constexpr uint32_t kQuery = MT * (D / 16) * 512u;                         // the queries' fragments
+    static constexpr int kStages = D <= 64 ? 6 : D <= 128 ? 3 : 2;
+    static constexpr uint32_t kQuery = kQueryRegs ? 0u : NT * (D / 16) * 256u;
     static constexpr uint32_t kRing = kAttendWarps * kStages * kStage;
     static constexpr uint32_t kJoin = kAttendWarps * kRows * (D + 4) * 4u;           // the warps' results (over the ring)
-    static constexpr uint32_t kBytes = kQuery + (kRing > kJoin ? kRing : kJoin);
+    static constexpr uint32_t kLists = kMostSplits * kRows * 8u;                     // ... the splits' maxima and sums
+    static constexpr uint32_t kMore = kRing > kJoin ? (kRing > kLists ? kRing : kLists) : (kJoin > kLists ? kJoin : kLists);
+    static constexpr uint32_t kBytes = kQuery + kMore;
+    static constexpr int kCtas = attend_ctas(D, NT);
 };
 
-template <int D, int MT>
-__global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const Attend g) {
-    typedef AttendShape<D, MT> S;
+template <int D, int NT>
+__global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)) tt_attend_few_kernel(const __grid_constant__ Attend g) {
+    typedef AttendShape<D, NT> S;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int last_one;
     pdl_allow_next();
@@ -181,7 +225,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     long long first_unit;
     const int b = sequence_of(g.a.starts, c.batch, g.group, S::kRows, 1, blockIdx.x, first_unit);
     const int start = g.a.starts[b], count = g.a.starts[b + 1] - start;
-    int length = g.a.lengths[b];
+    const int length = g.a.lengths[b];
     if (count == 0) return;
     if (count < 0 || start < 0 || start + (long long)count > g.a.tokens || length < 0 || length > g.max_length) {
         if (threadIdx.x == 0) report_invalid(g.a.status);
@@ -190,8 +234,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     const long long row0 = ((long long)blockIdx.x - first_unit) * S::kRows, all_rows = (long long)count * g.group;
     if (row0 >= all_rows) return;
     const int rows = (int)min((long long)S::kRows, all_rows - row0);
-    // what the tile's first and last row see: tokens seen0 .. up to hi
-    const int t0 = (int)(row0 / g.group), t1 = (int)((row0 + rows - 1) / g.group);
+    // what the tile's first and last row see: tokens lo .. hi - 1
+    const int t0 = (int)(row0 / g.group), h0 = (int)(row0 - (long long)t0 * g.group), t1 = t0 + (h0 + rows - 1) / g.group;
     const int before = length - count;                      // (negative: the first queries see nothing)
     const int lo = g.a.window > 0 ? max(0, before + t0 + 1 - g.a.window) : 0;
     const int hi = g.a.causal ? max(0, min(length, before + t1 + 1)) : length;
@@ -214,31 +258,36 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     }();
     const auto token_of = [&](int step) { return from + ((step >> 2) * kAttendWarps + warp) * kRun + (step & 3) * kStep; };
     const int* table = c.table + b * c.table_row;
-    const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0];
-    const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1];
+    const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + gq * c.token[0] + cq * S::kKey;
+    const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + 2 * cq * c.token[1] + gq * S::kVal;
+    const float* kscale = c.scale[0] + head * c.s_head[0];
+    const float* vscale = c.scale[1] + head * c.s_head[1];
     bool bad = false;
     const int shift = 31 - __clz(c.block);
     const auto page_of = [&](int step) { return step < steps ? table[token_of(step) >> shift] : 0; };
-    const auto fetch = [&](int step, int page) {
+    const auto fetch = [&](int step, int page, uint32_t slot) {
         if (step < steps) {
             if ((unsigned)page >= (unsigned)c.pages) { bad = true; page = 0; }
-            const uint32_t slot = ring + (uint32_t)(step % S::kStages) * S::kStage;
+            slot += (uint32_t)lane * 16u;                    // (a piece of 16 bytes has a line of 512 for the warp, a smaller one its share)
             const int t = token_of(step) & (c.block - 1);
-            const uint8_t* k = keys + page * c.page[0] + t * c.token[0];
-            const uint8_t* v = vals + page * c.page[1] + t * c.token[1];
+            const uint8_t* k = keys + (page * c.page[0] + t * c.token[0]);
+            const uint8_t* v = vals + (page * c.page[1] + t * c.token[1]);
+            const uint32_t ks = slot - (uint32_t)lane * (16u - S::kKey), vs = slot + S::kKeyBytes - (uint32_t)lane * (16u - S::kVal);
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int n = 0; n < 2; ++n) {
 #pragma unroll
-                for (int p = 0; p < S::kKeyPieces; ++p)
-                    copy_async<S::kKey>(slot + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k + (8 * n + gq) * c.token[0] + p * 4 * S::kKey + cq * S::kKey);
+                for (int p = 0; p < S::kKeyPieces; ++p) copy_async<S::kKey>(ks + (uint32_t)((n * S::kKeyPieces + p) * 32 * S::kKey), k + p * 4 * S::kKey);
+                k += 8 * c.token[0];
+            }
 #pragma unroll
-            for (int n = 0; n < 4; ++n)                      // tokens 2c, 2c + 1, 2c + 8, 2c + 9
+            for (int n = 0; n < 4; ++n) {                    // tokens 2c, 2c + 1, 2c + 8, 2c + 9
 #pragma unroll
-                for (int p = 0; p < S::kValPieces; ++p)
-                    copy_async<S::kVal>(slot + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal,
-                                        v + (2 * cq + (n & 1) + 8 * (n >> 1)) * c.token[1] + p * 8 * S::kVal + gq * S::kVal);
-            copy_async<4>(slot + S::kStage - 256u + (uint32_t)lane * 8u, c.scale[0] + page * c.s_page[0] + head * c.s_head[0]);
-            copy_async<4>(slot + S::kStage - 252u + (uint32_t)lane * 8u, c.scale[1] + page * c.s_page[1] + head * c.s_head[1]);
+                for (int p = 0; p < S::kValPieces; ++p) copy_async<S::kVal>(vs + (uint32_t)((n * S::kValPieces + p) * 32 * S::kVal), v + p * 8 * S::kVal);
+                v += n == 1 ? 7 * c.token[1] : c.token[1];
+            }
+            const uint32_t at = slot - (uint32_t)lane * 8u + S::kStage - 256u;
+            copy_async<4>(at, kscale + page * c.s_page[0]);
+            copy_async<4>(at + 4u, vscale + page * c.s_page[1]);
         }
         cp_async_commit();
     };
@@ -247,157 +296,174 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     for (int i = 0; i < S::kStages - 1; ++i) {
         const int page = next_page;
         next_page = page_of(i + 1);
-        fetch(i, page);
+        fetch(i, page, ring + (uint32_t)i * S::kStage);
     }
 
-    // ---- queries: the rows of the tile as fragments, in shared memory (each lane reads back what it wrote, but for the other warps') ----
-    const auto row_head = [&](int r) { return head * g.group + (int)((row0 + r) % g.group); };
-    const auto row_token = [&](int r) { return start + (int)((row0 + r) / g.group); };
-    float factor[2 * MT];                                    // of the rows gq, gq + 8, ... : what turns a product into a score in powers of two
+    // ---- queries: lane (g, c) has of rows g, g + 8, ... what it has of the keys ----
+    const auto q_row = [&](int r) { const int t = (h0 + r) / g.group; return make_int2(start + t0 + t, head * g.group + (h0 + r - t * g.group)); };
+    uint32_t q[S::kQueryRegs ? NT : 1][D / 16][2];
+    float factor[NT][2];                                     // of the rows 2c, 2c + 1: what turns a product into a score in powers of two
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
-        const int r = gq + 8 * i;
-        float most = 0.f;
-        const long long at = r < rows ? (long long)row_token(r) * g.a.q_token + (long long)row_head(r) * g.a.q_head : 0;
-        if (r < rows)
-            for (int p = 0; p < S::kKeyPieces; ++p)
-                for (int e = 0; e < S::kKey; ++e) most = finite_max(most, load_one(g.a.q, at + p * 4 * S::kKey + cq * S::kKey + e, g.a.type));
-        most = quad_max(most);
-        const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14;          // (a subnormal: 0, as good as 1)
-        const float up = __int_as_float((min(254, max(1, 127 + 14 + 127 - ex))) << 23);
-        factor[i] = g.scale_log2 / up;
-        if (warp == i % kAttendWarps) {
+    for (int n = 0; n < NT; ++n) {
+        const int r = 8 * n + gq;
+        float f = 0.f;
+        if (S::kQueryRegs || warp == n % kAttendWarps) {
+            float v[D / 16][4], most = 0.f;
+            if (r < rows) {
+                const int2 at = q_row(r);
+                const long long first = at.x * g.a.q_token + at.y * g.a.q_head + cq * S::kKey;
 #pragma unroll
-            for (int p = 0; p < S::kKeyPieces; ++p)
+                for (int i = 0; i < D / 16; ++i) load_four(g.a.q, first + i / (S::kKey / 4) * 4 * S::kKey + i % (S::kKey / 4) * 4, g.a.type, g.q_wide, v[i]);
+            } else {
 #pragma unroll
-                for (int s = 0; s < S::kKey / 4; ++s) {
-                    float v[4];
+                for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = r < rows ? load_one(g.a.q, at + p * 4 * S::kKey + cq * S::kKey + 4 * s + e, g.a.type) * up : 0.f;
-                    const int step = p * (S::kKey / 4) + s;
-                    // a fragment's registers: (row, k), (row + 8, k), (row, k + 8), (row + 8, k + 8)
-                    const uint32_t to_ = query + (uint32_t)((((i >> 1) * (D / 16) + step) * 32 + lane) * 16 + (i & 1) * 4);
-                    st_shared_u32(to_, down2<TT_TYPE_F16>(v[0], v[1]));
-                    st_shared_u32(to_ + 8u, down2<TT_TYPE_F16>(v[2], v[3]));
+                    for (int e = 0; e < 4; ++e) v[i][e] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = finite_max(most, v[i][e]);
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14;      // (a subnormal: 0, as good as 1)
+            const float up = __int_as_float((min(254, max(1, 127 + 14 + 127 - ex))) << 23);
+            f = g.scale_log2 / up;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+                const uint32_t x = down2<TT_TYPE_F16>(v[i][0] * up, v[i][1] * up), y = down2<TT_TYPE_F16>(v[i][2] * up, v[i][3] * up);
+                if constexpr (S::kQueryRegs) { q[n][i][0] = x; q[n][i][1] = y; }
+                else {
+                    const uint32_t at = query + (uint32_t)(((n * (D / 16) + i) * 32 + lane) * 8);
+                    st_shared_u32(at, x);
+                    st_shared_u32(at + 4u, y);
                 }
+            }
+        }
+        if constexpr (!S::kQueryRegs) {
+            // (the warp that has the rows tells the others, through the place that the join takes later)
+            __shared__ float factors[S::kRows];
+            if (warp == n % kAttendWarps && cq == 0) factors[8 * n + gq] = f;
+            if (n == NT - 1) {
+                __syncthreads();
+#pragma unroll
+                for (int m = 0; m < NT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) factor[m][e] = factors[8 * m + 2 * cq + e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) factor[n][e] = __shfl_sync(0xffffffffu, f, 4 * (2 * cq + e));
         }
     }
-    __syncthreads();
 
-    float o[MT][D / 8][4];
+    float o[NT][D / 16][4];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j)
+        for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[m][j][e] = 0.f;
-    float top[2 * MT], sum[2 * MT], ref = 0.f;               // ref: the largest scale of values so far, the unit of o
+            for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
+    float top[NT][2], sum[NT][2], ref = 0.f;                 // ref: the largest scale of values so far, the unit of o
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) { top[i] = -INFINITY; sum[i] = 0.f; }
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { top[n][e] = -INFINITY; sum[n][e] = 0.f; }
+    const auto sees = [&](int r, int tok) {
+        const int pos = before + t0 + (h0 + r) / g.group;
+        return tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
+    };
 
+    uint32_t slot = ring, ahead = ring + (uint32_t)(S::kStages - 1) * S::kStage;      // of this step, of the one that is fetched
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
         {
             const int page = next_page;
             next_page = page_of(step + S::kStages);
-            fetch(step + S::kStages - 1, page);
+            fetch(step + S::kStages - 1, page, ahead);
+            ahead = ahead + S::kStage == ring + S::kStages * S::kStage ? ring : ahead + S::kStage;
         }
         cp_async_wait<S::kStages - 1>();
-        const uint32_t slot = ring + (uint32_t)(step % S::kStages) * S::kStage;
+        const uint32_t at = slot;
+        slot = slot + S::kStage == ring + S::kStages * S::kStage ? ring : slot + S::kStage;
         uint32_t scales[2];
-        read_shared<8>(slot + S::kStage - 256u + (uint32_t)lane * 8u, scales);
+        read_shared<8>(at + S::kStage - 256u + (uint32_t)lane * 8u, scales);
         const float ks = __uint_as_float(scales[0]), vs = __uint_as_float(scales[1]);
         const int t = token_of(step);
         const bool whole = t >= whole_lo && t + kStep <= whole_hi;
-        // scores: rows x 16 tokens
-        float s[MT][2][4];
+        // scores of 16 tokens x rows: tokens g, g + 8 and rows 2c, 2c + 1 of each eight
+        float s[NT][2][4];                                   // (two sums each: a chain of products half as long)
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[m][n][e] = 0.f;
+            for (int e = 0; e < 4; ++e) s[n][0][e] = s[n][1][e] = 0.f;
 #pragma unroll
         for (int p = 0; p < S::kKeyPieces; ++p) {
             uint32_t k[2][S::kKey / 4];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) read_shared<S::kKey>(slot + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k[n]);
+            for (int n = 0; n < 2; ++n) read_shared<S::kKey>(at + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k[n]);
 #pragma unroll
             for (int w = 0; w < S::kKey / 4; ++w) {
+                uint32_t a0, a1, a2, a3;
+                f16_pairs_of_e4m3(k[0][w], a0, a2);
+                f16_pairs_of_e4m3(k[1][w], a1, a3);
+                const int i = p * (S::kKey / 4) + w;
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    uint32_t q[4];
-                    read_shared<16>(query + (uint32_t)((m * (D / 16) + p * (S::kKey / 4) + w) * 32 + lane) * 16u, q);
-#pragma unroll
-                    for (int n = 0; n < 2; ++n) mma_16x8x16(s[m][n], q, f16x2_of_e4m3(k[n][w]), f16x2_of_e4m3(k[n][w] >> 16));
+                for (int n = 0; n < NT; ++n) {
+                    if constexpr (S::kQueryRegs) mma_16x8x16(s[n][i & 1], a0, a1, a2, a3, q[n][i][0], q[n][i][1]);
+                    else {
+                        uint32_t qq[2];
+                        read_shared<8>(query + (uint32_t)(((n * (D / 16) + i) * 32 + lane) * 8), qq);
+                        mma_16x8x16(s[n][i & 1], a0, a1, a2, a3, qq[0], qq[1]);
+                    }
                 }
             }
         }
         // the running maximum, in powers of two
         const float new_ref = fmaxf(ref, vs);
-        const float unit = vs > 0.f ? __fdividef(vs, new_ref) * 32768.f : 0.f;
-        const float shrink = ref < new_ref ? __fdividef(ref, new_ref) : 1.f;
+        const float unit = vs == new_ref ? 32768.f : __fdividef(vs, new_ref) * 32768.f;
+        const float shrink = ref == new_ref ? 1.f : __fdividef(ref, new_ref);
         bool moved = shrink != 1.f;
-        float alpha[2 * MT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int i = 2 * m + h;
-                float mx = -INFINITY;
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float v = s[m][n][2 * h + e] * (factor[i] * ks);
-                        if (!whole) {
-                            const int tok = t + 8 * n + 2 * cq + e, pos = before + (int)((row0 + gq + 8 * i) / g.group);
-                            const bool seen = tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
-                            v = seen ? v : -INFINITY;
-                        }
-                        s[m][n][2 * h + e] = v;
-                        mx = fmaxf(mx, v);
-                    }
-                mx = fmaxf(top[i], quad_max(mx));
-                const float ref_max = mx == -INFINITY ? 0.f : mx;
-                alpha[i] = exp2f(top[i] - ref_max) * shrink;
-                const float keep = exp2f(top[i] - ref_max);
-                moved = moved || mx != top[i];
-                top[i] = mx;
-                float add = 0.f;
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float p = exp2f(s[m][n][2 * h + e] - ref_max);
-                        add += p;
-                        s[m][n][2 * h + e] = p * unit;
-                    }
-                sum[i] = sum[i] * keep + add;
-            }
         ref = new_ref;
+        float alpha[NT][2];
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = (s[n][0][e] + s[n][1][e]) * (factor[n][e & 1] * ks);
+                if (!whole) v[e] = sees(8 * n + 2 * cq + (e & 1), t + gq + 8 * (e >> 1)) ? v[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float mx = fmaxf(top[n][e], octet_max(fmaxf(v[e], v[e + 2])));
+                const float ref_max = mx == -INFINITY ? 0.f : mx;
+                const float keep = exp2_fast(top[n][e] - ref_max);
+                moved = moved || mx != top[n][e];
+                top[n][e] = mx;
+                v[e] = exp2_fast(v[e] - ref_max);
+                v[e + 2] = exp2_fast(v[e + 2] - ref_max);
+                sum[n][e] = fmaf(sum[n][e], keep, v[e] + v[e + 2]);
+                alpha[n][e] = keep * shrink;
+            }
+            pb[n][0] = transpose_8x8(down2<TT_TYPE_F16>(v[0] * unit, v[1] * unit));
+            pb[n][1] = transpose_8x8(down2<TT_TYPE_F16>(v[2] * unit, v[3] * unit));
+        }
         if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < D / 8; ++j)
+                for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[m][j][e] *= alpha[2 * m + (e >> 1)];
-        }
-        uint32_t pa[MT][4];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            pa[m][0] = down2<TT_TYPE_F16>(s[m][0][0], s[m][0][1]);
-            pa[m][1] = down2<TT_TYPE_F16>(s[m][0][2], s[m][0][3]);
-            pa[m][2] = down2<TT_TYPE_F16>(s[m][1][0], s[m][1][1]);
-            pa[m][3] = down2<TT_TYPE_F16>(s[m][1][2], s[m][1][3]);
+                    for (int e = 0; e < 4; ++e) o[n][j][e] *= alpha[n][e & 1];
         }
         // values
 #pragma unroll
         for (int p = 0; p < S::kValPieces; ++p) {
             uint32_t v[4][S::kVal / 4];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) read_shared<S::kVal>(slot + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal, v[n]);
+            for (int n = 0; n < 4; ++n) read_shared<S::kVal>(at + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal, v[n]);
             if (!whole) {
                 // What no row of the tile sees is not multiplied (it may be anything), and a NaN that only some rows see reaches just those: it is
                 // replaced by 0 in the product, and another product counts for each row how many of a column's it sees.
@@ -413,31 +479,22 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
                     }
                 }
                 if (__any_sync(0xffffffffu, nans != 0u)) {
-                    uint32_t see[MT][4];
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t see[2];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const int pos = before + (int)((row0 + 16 * m + gq + 8 * (r & 1)) / g.group);
-                            uint32_t w = 0u;
+                        for (int r = 0; r < 2; ++r)
+                            see[r] = (sees(8 * n + gq, t + 8 * r + 2 * cq) ? 0x3c00u : 0u) | (sees(8 * n + gq, t + 8 * r + 2 * cq + 1) ? 0x3c000000u : 0u);
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int tok = t + 8 * (r >> 1) + 2 * cq + e;
-                                const bool seen = tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
-                                w |= seen ? 0x3c00u << (16 * e) : 0u;
-                            }
-                            see[m][r] = w;
-                        }
+                        for (int j = 0; j < S::kVal; j += 2) {
+                            const auto is_nan = [&](int m, int i) { return ((v[m][i >> 2] >> (8 * (i & 3))) & 0x7fu) == 0x7fu; };
+                            uint32_t a[4];
 #pragma unroll
-                    for (int j = 0; j < S::kVal; ++j) {
-                        const auto is_nan = [&](int n) { return ((v[n][j >> 2] >> (8 * (j & 3))) & 0x7fu) == 0x7fu; };
-                        const uint32_t b0 = (is_nan(0) ? 0x3c00u : 0u) | (is_nan(1) ? 0x3c000000u : 0u), b1 = (is_nan(2) ? 0x3c00u : 0u) | (is_nan(3) ? 0x3c000000u : 0u);
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) {
+                            for (int r = 0; r < 4; ++r) a[r] = (is_nan(r & 2, j + (r & 1)) ? 0x3c00u : 0u) | (is_nan((r & 2) + 1, j + (r & 1)) ? 0x3c000000u : 0u);
                             float hit[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_16x8x16(hit, see[m], b0, b1);
+                            mma_16x8x16(hit, a[0], a[1], a[2], a[3], see[0], see[1]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) if (hit[e] > 0.f) o[m][p * S::kVal + j][e] = __int_as_float(0x7fffffff);
+                            for (int e = 0; e < 4; ++e) if (hit[e] > 0.f) o[n][(p * S::kVal + j) / 2][e] = __int_as_float(0x7fffffff);
                         }
                     }
 #pragma unroll
@@ -448,15 +505,13 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
             }
 #pragma unroll
             for (int j = 0; j < S::kVal; j += 2) {
-                // bytes j, j + 1 of two tokens side by side: the pairs of the reduction
+                // bytes j, j + 1 of two tokens side by side: the pairs of the reduction, two columns of them
                 const uint32_t sel = (j & 2) ? 0x7362u : 0x5140u;
-                const uint32_t x0 = __byte_perm(v[0][j >> 2], v[1][j >> 2], sel), x1 = __byte_perm(v[2][j >> 2], v[3][j >> 2], sel);
-                const uint32_t b0 = f16x2_of_e4m3(x0), b1 = f16x2_of_e4m3(x1), b2 = f16x2_of_e4m3(x0 >> 16), b3 = f16x2_of_e4m3(x1 >> 16);
+                uint32_t a0, a1, a2, a3;
+                f16_pairs_of_e4m3(__byte_perm(v[0][j >> 2], v[1][j >> 2], sel), a0, a1);
+                f16_pairs_of_e4m3(__byte_perm(v[2][j >> 2], v[3][j >> 2], sel), a2, a3);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    mma_16x8x16(o[m][p * S::kVal + j], pa[m], b0, b1);
-                    mma_16x8x16(o[m][p * S::kVal + j + 1], pa[m], b2, b3);
-                }
+                for (int n = 0; n < NT; ++n) mma_16x8x16(o[n][(p * S::kVal + j) / 2], a0, a1, a2, a3, pb[n][0], pb[n][1]);
             }
         }
     }
@@ -469,42 +524,54 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     float* join = reinterpret_cast<float*>(smem + S::kQuery);
     const float to_real = ref * 3.0517578125e-5f;            // 2^-15
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int i = 2 * m + h;
-            float* line = join + (warp * S::kRows + 16 * m + 8 * h + gq) * kLine;
-            const float total = quad_sum(sum[i]);
+        for (int e = 0; e < 2; ++e) {
+            float* line = join + (warp * S::kRows + 8 * n + 2 * cq + e) * kLine;
+            const float total = octet_sum(sum[n][e]);
 #pragma unroll
             for (int p = 0; p < S::kValPieces; ++p)
 #pragma unroll
-                for (int j = 0; j < S::kVal; ++j) {
-                    line[p * 8 * S::kVal + 2 * cq * S::kVal + j] = o[m][p * S::kVal + j][2 * h] * to_real;
-                    line[p * 8 * S::kVal + (2 * cq + 1) * S::kVal + j] = o[m][p * S::kVal + j][2 * h + 1] * to_real;
-                }
-            if (cq == 0) { line[D] = top[i]; line[D + 1] = total; }
+                for (int j = 0; j < S::kVal; j += 2)
+                    *reinterpret_cast<float2*>(line + (p * 8 + gq) * S::kVal + j) = make_float2(o[n][(p * S::kVal + j) / 2][e] * to_real, o[n][(p * S::kVal + j) / 2][e + 2] * to_real);
+            if (gq == 0) *reinterpret_cast<float2*>(line + D) = make_float2(top[n][e], total);
         }
     __syncthreads();
-    const auto store = [&](int r, int i, float v) { store_one(g.a.y, (long long)row_token(r) * g.a.y_token + (long long)row_head(r) * g.a.y_head + i, g.a.type, v); };
+    const auto store = [&](int r, int i, const float (&v)[4]) {
+        const int2 at_ = q_row(r);
+        store_four(g.a.y, at_.x * g.a.y_token + at_.y * g.a.y_head + i, g.a.type, g.y_wide, v);
+    };
     const long long tile = (long long)blockIdx.x * c.heads + head;
-    float* left = g.partial + (tile * g.splits + blockIdx.z) * (S::kRows * (D + 2));
-    for (int e = threadIdx.x; e < rows * D; e += kAttendWarps * 32) {
-        const int r = e / D, i = e - r * D;
+    constexpr int kPart = S::kRows * (D + 2);
+    float* left = g.partial + (tile * g.splits + blockIdx.z) * kPart;
+    for (int e = threadIdx.x; e < rows * (D / 4); e += kAttendWarps * 32) {
+        const int r = e / (D / 4), i = 4 * (e - r * (D / 4));
+        float2 ml[kAttendWarps];
         float mx = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kAttendWarps; ++w) mx = fmaxf(mx, join[(w * S::kRows + r) * kLine + D]);
-        const float at = mx == -INFINITY ? 0.f : mx;
-        float v = 0.f, l = 0.f;
+        for (int w = 0; w < kAttendWarps; ++w) {
+            ml[w] = *reinterpret_cast<const float2*>(join + (w * S::kRows + r) * kLine + D);
+            mx = fmaxf(mx, ml[w].x);
+        }
+        const float ref_max = mx == -INFINITY ? 0.f : mx;
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
 #pragma unroll
         for (int w = 0; w < kAttendWarps; ++w) {
-            const float* line = join + (w * S::kRows + r) * kLine;
-            const float k = exp2f(line[D] - at);
-            if (line[D + 1] != 0.f) { v += line[i] * k; l += line[D + 1] * k; }      // (a warp without tokens has nothing)
+            const float k = exp2_fast(ml[w].x - ref_max);
+            if (ml[w].y != 0.f) {                            // (a warp without tokens has nothing)
+                const float4 f = *reinterpret_cast<const float4*>(join + (w * S::kRows + r) * kLine + i);
+                v[0] += f.x * k; v[1] += f.y * k; v[2] += f.z * k; v[3] += f.w * k;
+                l += ml[w].y * k;
+            }
         }
-        if (active == 1) store(r, i, l != 0.f ? v / l : 0.f);
-        else {
-            left[r * D + i] = v;
-            if (i == 0) { left[S::kRows * D + 2 * r] = mx; left[S::kRows * D + 2 * r + 1] = l; }
+        if (active == 1) {
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] *= inv;
+            store(r, i, v);
+        } else {
+            *reinterpret_cast<float4*>(left + r * D + i) = make_float4(v[0], v[1], v[2], v[3]);
+            if (i == 0) *reinterpret_cast<float2*>(left + S::kRows * D + 2 * r) = make_float2(mx, l);
         }
     }
     if (active == 1) return;
@@ -516,20 +583,42 @@ __global__ void __launch_bounds__(kAttendWarps * 32) tt_attend_few_kernel(const 
     __syncthreads();
     if (!last_one) return;
     __threadfence();
-    const float* parts = g.partial + tile * g.splits * (S::kRows * (D + 2));
-    for (int e = threadIdx.x; e < rows * D; e += kAttendWarps * 32) {
-        const int r = e / D, i = e - r * D;
-        float mx = -INFINITY;
-        for (int z = 0; z < active; ++z) mx = fmaxf(mx, __ldcg(parts + (long long)z * (S::kRows * (D + 2)) + S::kRows * D + 2 * r));
-        const float at = mx == -INFINITY ? 0.f : mx;
-        float v = 0.f, l = 0.f;
-        for (int z = 0; z < active; ++z) {
-            const float* part = parts + (long long)z * (S::kRows * (D + 2));
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(part + S::kRows * D + 2 * r));
-            const float k = exp2f(ml.x - at);
-            if (ml.y != 0.f) { v += __ldcg(part + r * D + i) * k; l += ml.y * k; }
+    const float* parts = g.partial + tile * g.splits * kPart;
+    float2* lists = reinterpret_cast<float2*>(join);         // [split][row]: maximum and sum, then the split's share
+    for (int e = threadIdx.x; e < active * rows; e += kAttendWarps * 32) {
+        const int z = e / rows, r = e - z * rows;
+        lists[z * S::kRows + r] = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + S::kRows * D + 2 * r));
+    }
+    __syncthreads();
+    for (int r = warp; r < rows; r += kAttendWarps) {
+        float mx = -INFINITY, l = 0.f;
+        for (int z = lane; z < active; z += 32) mx = fmaxf(mx, lists[z * S::kRows + r].x);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+        const float ref_max = mx == -INFINITY ? 0.f : mx;
+        for (int z = lane; z < active; z += 32) {
+            const float2 ml = lists[z * S::kRows + r];
+            if (ml.y != 0.f) l += ml.y * exp2_fast(ml.x - ref_max);
         }
-        store(r, i, l != 0.f ? v / l : 0.f);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        for (int z = lane; z < active; z += 32) {
+            const float2 ml = lists[z * S::kRows + r];
+            lists[z * S::kRows + r].x = ml.y != 0.f ? exp2_fast(ml.x - ref_max) * inv : 0.f;
+        }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * (D / 4); e += kAttendWarps * 32) {
+        const int r = e / (D / 4), i = 4 * (e - r * (D / 4));
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int z = 0; z < active; ++z) {
+            const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + r * D + i));
+            const float w = lists[z * S::kRows + r].x;
+            v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
+        }
+        store(r, i, v);
     }
     if (threadIdx.x == 0) g.counters[tile] = 0u;             // ready for the next call
 }
@@ -566,42 +655,46 @@ static tt_status plan_attend(const tt_cache_attention_args& a, Attend& g, long l
     if (a.tokens == 0 || a.heads_q == 0 || c.batch == 0) return TT_OK;
     g.group = a.heads_q / c.heads;
     const int count = a.max_count > 0 && a.max_count < a.tokens ? a.max_count : a.tokens;
-    // Two fragments of 16 rows a warp where the rows of a sequence need them: a key that is fetched and converted serves both.
-    g.rows = (long long)count * g.group > 16 && c.d <= 128 ? 32 : 16;
+    // As many rows as a sequence has, up to what the registers hold: a key that is fetched and converted serves all of them.
+    const long long most_rows = (long long)count * g.group;
+    g.rows = most_rows <= 8 ? 8 : most_rows <= 16 || c.d > 128 ? 16 : 32;
     units = (long long)a.tokens * g.group / g.rows + c.batch;
     if (units * c.heads > 0x7fffffffll) return TT_ERR_INVALID_ARG;
     g.max_length = c.pages > 0 ? c.max_pages * c.block : 0;
     if (a.max_length > 0 && a.max_length < g.max_length) g.max_length = a.max_length;
     long long span = g.max_length;
-    if (a.window > 0 && a.window + (long long)(g.rows / g.group + 2) < span) span = a.window + (long long)(g.rows / g.group + 2);
-    span += kRun;
-    // Every SM is to have three CTAs at work, but a split is no shorter than what makes joining it cheap.
-    const long long tiles = units * c.heads;
-    constexpr int kLeast = 4 * kAttendWarps * kRun;
-    long long chunk = (span * tiles + 3 * kSms - 1) / (3 * kSms);
-    chunk = (chunk + kAttendWarps * kRun - 1) / (kAttendWarps * kRun) * (kAttendWarps * kRun);
-    if (chunk < kLeast) chunk = kLeast;
-    if (chunk > 2048) chunk = 2048;
-    while ((span + chunk - 1) / chunk > 65535 || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
-    g.chunk = (int)chunk;
+    const long long tile_tokens = g.rows / g.group + 2;
+    if (a.window > 0 && a.window + tile_tokens < span) span = a.window + tile_tokens;
+    span += kRun;                                          // (splits begin at multiples of it)
+    // One sequence: a share for each CTA that the SMs hold at once.  Several, of lengths that only the device knows: a quarter of that, so that
+    // long and short ones even out.  No split is shorter than what makes joining it cheap.
+    const long long tiles = units * c.heads, slots = (long long)kSms * attend_ctas(c.d, g.rows / 8) * (c.batch > 1 ? 4 : 1);
+    constexpr int kGrain = kAttendWarps * kRun;
+    long long chunk = ((span - kRun) * tiles + slots - 1) / slots;
+    chunk = (chunk + kGrain - 1) / kGrain * kGrain;
+    if (chunk < 2 * kGrain) chunk = 2 * kGrain;
+    if (c.batch > 1 && chunk > 8 * kGrain) chunk = 8 * kGrain;
+    while ((span + chunk - 1) / chunk > kMostSplits || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
+    g.chunk = (int)(chunk < span ? chunk : span);
     g.splits = (int)((span + chunk - 1) / chunk);
     if (g.splits > 1) bytes = (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (c.d + 2) * 4;
     g.scale_log2 = a.scale * 1.4426950408889634f;
     return TT_OK;
 }
 
-template <int D, int MT>
+template <int D, int NT>
 static cudaError_t launch_attend(const Attend& g, long long units, void* stream) {
-    typedef AttendShape<D, MT> S;
+    typedef AttendShape<D, NT> S;
     static OncePerDevice raised;
-    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_few_kernel<D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
+    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
     if (ready != cudaSuccess) return ready;
-    return launch(tt_attend_few_kernel<D, MT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, g);
+    return launch(tt_attend_few_kernel<D, NT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, g);
 }
 template <int D>
 static cudaError_t launch_attend_rows(const Attend& g, long long units, void* stream) {
-    if constexpr (D <= 128) if (g.rows == 32) return launch_attend<D, 2>(g, units, stream);
-    return launch_attend<D, 1>(g, units, stream);
+    if (g.rows == 8) return launch_attend<D, 1>(g, units, stream);
+    if constexpr (D <= 128) if (g.rows == 32) return launch_attend<D, 4>(g, units, stream);
+    return launch_attend<D, 2>(g, units, stream);
 }
 
 }  // namespace tt
@@ -658,6 +751,8 @@ extern "C" tt_status tt_cache_attention(const tt_cache_attention_args* a, void* 
     if (reinterpret_cast<uintptr_t>(a->q) % 2 || reinterpret_cast<uintptr_t>(a->y) % 2 || reinterpret_cast<uintptr_t>(a->starts) % 4 || reinterpret_cast<uintptr_t>(a->lengths) % 4 ||
         reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
     if (need > 0 && (!a->workspace || !on16(a->workspace) || a->workspace_bytes < need)) return TT_ERR_INVALID_ARG;
+    g.q_wide = reinterpret_cast<uintptr_t>(a->q) % 8 == 0 && a->q_token % 4 == 0 && a->q_head % 4 == 0;
+    g.y_wide = reinterpret_cast<uintptr_t>(a->y) % 8 == 0 && a->y_token % 4 == 0 && a->y_head % 4 == 0;
     g.counters = static_cast<unsigned*>(a->workspace);
     g.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + (units * c.heads * 4 + 15) / 16 * 16);
     switch (c.d) {

@@ -124,6 +124,10 @@ __device__ __forceinline__ uint32_t f16x2_of_e4m3(uint32_t two) {
     asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(h) : "r"(two));
     return h;
 }
+// ... and those of a whole word, two pairs.
+__device__ __forceinline__ void f16_pairs_of_e4m3(uint32_t four, uint32_t& first, uint32_t& second) {
+    asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\tcvt.rn.f16x2.e4m3x2 %1, hi;\n\t}" : "=r"(first), "=r"(second) : "r"(four));
+}
 __device__ __forceinline__ float float_of_e4m3(uint32_t byte) {
     const uint32_t h = f16x2_of_e4m3(byte & 0xffu);
     return __half2float(__ushort_as_half((unsigned short)(h & 0xffffu)));
