@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtt.so")
-SOURCES = ["tt_host.cpp", "tt_kernels.cu", "tt_conv.cu", "tt_attention.cu", "tt_f8.cu", "tt_rotary.cu", "tt_cache.cu", "tt_device.cu"]
-HEADERS = [os.path.join(CSRC, "tt_internal.h"), os.path.join(CSRC, "tt_ptx.cuh"), os.path.join(CSRC, "tt_f8.cuh"), os.path.join(ROOT, "include", "tt.h")]
+SOURCES = ["tt_host.cpp", "tt_kernels.cu", "tt_conv.cu", "tt_attention.cu", "tt_f8.cu", "tt_rotary.cu", "tt_cache.cu", "tt_prompt.cu", "tt_device.cu"]
+HEADERS = [os.path.join(CSRC, "tt_internal.h"), os.path.join(CSRC, "tt_ptx.cuh"), os.path.join(CSRC, "tt_f8.cuh"), os.path.join(CSRC, "tt_cache.cuh"), os.path.join(ROOT, "include", "tt.h")]
 CALL_LIB = os.path.join(HERE, "_ttcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 CALL_SOURCE = os.path.join(CSRC, "tt_pycall.cpp")
 

@@ -1,24 +1,9 @@
 // A paged cache of keys and values in e4m3, a scale for each page and head: new tokens into it, and attention over it.
 #include <cuda_runtime.h>
 #include <cstring>
-#include "tt_ptx.cuh"
-#include "tt_f8.cuh"
+#include "tt_cache.cuh"
 
 namespace tt {
-
-__device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(status, 0u, (unsigned)TT_ERR_INVALID_ARG); }
-
-// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] / per + extra * b and up (as many as it can need
-// at most), so a unit finds its sequence by bisection.
-__device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
-    int lo = 0, hi = batch - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (starts[mid] * mul / per + (long long)extra * mid <= unit) lo = mid; else hi = mid - 1;
-    }
-    first = starts[lo] * mul / per + (long long)extra * lo;
-    return lo;
-}
 
 // ---- append ---------------------------------------------------------------------------------------------------------------
 //
@@ -118,19 +103,10 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
 // 2^-29 of the largest still has all of them; sums are in 32 bits.
 //   The keys of a sequence are split over CTAs, of which the last to finish adds up what all have left in the workspace, in their order.
 
-constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it
 constexpr int kRun = 64;                    // tokens that a warp takes in a row
 constexpr int kAttendWarps = 4;
+constexpr int kFewRows = 32;                // rows of a tile at most
 constexpr int kMostSplits = 256;            // of a sequence: the last CTA has the maxima and sums of all of them in shared memory
-
-struct Attend {
-    tt_cache_attention_args a;
-    int group, rows;                        // query heads of a key head; rows of a tile
-    int chunk, splits, max_length;          // tokens of a split, most splits
-    int q_wide, y_wide;                     // four values of q, of y at a time
-    float scale_log2;                       // the scale times log2(e)
-    unsigned* counters; float* partial;
-};
 
 __device__ __forceinline__ void mma_16x8x16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -141,11 +117,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     uint32_t t;
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
     return t;
-}
-__device__ __forceinline__ float exp2_fast(float x) {      // 2^x to two units in the last place; 0 below 2^-126
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
 }
 template <int N>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
@@ -170,29 +141,6 @@ __device__ __forceinline__ float octet_sum(float v) {
     for (int d = 4; d < 32; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
-// A non-zero byte for each e4m3 byte of the word that is NaN.
-__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-// Four values of a 16-bit type.
-__device__ __forceinline__ void load_four(const void* p, long long i, int type, int wide, float (&v)[4]) {
-    if (wide) {
-        const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-        const float2 a = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.x) : up2<TT_TYPE_BF16>(u.x), b = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.y) : up2<TT_TYPE_BF16>(u.y);
-        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = load_one(p, i + e, type);
-    }
-}
-__device__ __forceinline__ void store_four(void* p, long long i, int type, int wide, const float (&v)[4]) {
-    if (wide) {
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
-            type == TT_TYPE_F16 ? make_uint2(down2<TT_TYPE_F16>(v[0], v[1]), down2<TT_TYPE_F16>(v[2], v[3])) : make_uint2(down2<TT_TYPE_BF16>(v[0], v[1]), down2<TT_TYPE_BF16>(v[2], v[3]));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) store_one(p, i + e, type, v[e]);
-    }
-}
-
 // CTAs that their registers leave room for on an SM.
 constexpr int attend_ctas(int d, int nt) { return nt <= 2 && nt * d <= 128 ? 4 : nt * d <= 128 || (nt <= 2 && nt * d <= 256) ? 3 : 2; }
 
@@ -222,30 +170,13 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     pdl_wait_prev();
     const tt_cache& c = g.a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, cq = lane & 3, head = blockIdx.y;
-    long long first_unit;
-    const int b = sequence_of(g.a.starts, c.batch, g.group, S::kRows, 1, blockIdx.x, first_unit);
-    const int start = g.a.starts[b], count = g.a.starts[b + 1] - start;
-    const int length = g.a.lengths[b];
-    if (count == 0) return;
-    if (count < 0 || start < 0 || start + (long long)count > g.a.tokens || length < 0 || length > g.max_length) {
-        if (threadIdx.x == 0) report_invalid(g.a.status);
-        return;
-    }
-    const long long row0 = ((long long)blockIdx.x - first_unit) * S::kRows, all_rows = (long long)count * g.group;
-    if (row0 >= all_rows) return;
-    const int rows = (int)min((long long)S::kRows, all_rows - row0);
-    // what the tile's first and last row see: tokens lo .. hi - 1
-    const int t0 = (int)(row0 / g.group), h0 = (int)(row0 - (long long)t0 * g.group), t1 = t0 + (h0 + rows - 1) / g.group;
-    const int before = length - count;                      // (negative: the first queries see nothing)
-    const int lo = g.a.window > 0 ? max(0, before + t0 + 1 - g.a.window) : 0;
-    const int hi = g.a.causal ? max(0, min(length, before + t1 + 1)) : length;
+    TileView view;
+    if (!view_tile(g, S::kRows, blockIdx.x, view)) return;
+    const int b = view.b, start = view.start, rows = view.rows, t0 = view.t0, h0 = view.h0, before = view.before, lo = view.lo, hi = view.hi;
     const int base = lo / kRun * kRun;
     const int active = hi > lo ? (hi - base + g.chunk - 1) / g.chunk : 1;
     if ((int)blockIdx.z >= active) return;
     const int from = base + (int)blockIdx.z * g.chunk, to = min(hi, from + g.chunk);
-    // tokens that every row sees: whole_lo .. whole_hi - 1
-    const int whole_lo = g.a.window > 0 ? max(0, before + t1 + 1 - g.a.window) : 0;
-    const int whole_hi = g.a.causal ? max(0, min(length, before + t0 + 1)) : length;
 
     const uint32_t query = smem_u32(smem), ring = query + S::kQuery + (uint32_t)warp * S::kStages * S::kStage;
     // ---- the copies of a step: 16 tokens of one page ----
@@ -390,7 +321,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         read_shared<8>(at + S::kStage - 256u + (uint32_t)lane * 8u, scales);
         const float ks = __uint_as_float(scales[0]), vs = __uint_as_float(scales[1]);
         const int t = token_of(step);
-        const bool whole = t >= whole_lo && t + kStep <= whole_hi;
+        const bool whole = t >= view.whole_lo && t + kStep <= view.whole_hi;
         // scores of 16 tokens x rows: tokens g, g + 8 and rows 2c, 2c + 1 of each eight
         float s[NT][2][4];                                   // (two sums each: a chain of products half as long)
 #pragma unroll
@@ -641,45 +572,96 @@ static tt_status check_cache_memory(const tt_cache& c) {
     return TT_OK;
 }
 
-// The layout of an attention call: what is split over how many CTAs.
-static tt_status plan_attend(const tt_cache_attention_args& a, Attend& g, long long& units, long long& bytes) {
+// The layout of an attention call: the kernels that it takes and what they split over how many CTAs.
+struct AttendPlan {
+    Attend few{}, prompt{};
+    long long few_units = 0, prompt_units = 0;              // 0: the kernel is not needed
+    long long bytes = 0, prompt_at = 0;                     // of the workspace; where the second one's part begins
+};
+static long long workspace_part(const Attend& g, long long units) {
+    const long long tiles = units * g.a.cache.heads;
+    return g.splits > 1 ? (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (g.a.cache.d + 2) * 4 : 0;
+}
+static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan) {
     const tt_cache& c = a.cache;
-    g = Attend{};
-    g.a = a;
+    plan = AttendPlan{};
     const tt_status s = check_cache(c);
     if (s != TT_OK) return s;
     if ((a.type != TT_TYPE_F16 && a.type != TT_TYPE_BF16) || a.tokens < 0 || a.heads_q < 0 || a.window < 0 || a.max_count < 0 || a.max_length < 0 || !(a.scale == a.scale)) return TT_ERR_INVALID_ARG;
     if (c.heads == 0 ? a.heads_q != 0 : a.heads_q % c.heads) return TT_ERR_INVALID_ARG;
     if (a.window > 0 && !a.causal) return TT_ERR_INVALID_ARG;
-    units = 0; bytes = 0;
     if (a.tokens == 0 || a.heads_q == 0 || c.batch == 0) return TT_OK;
+    Attend g{};
+    g.a = a;
     g.group = a.heads_q / c.heads;
-    const int count = a.max_count > 0 && a.max_count < a.tokens ? a.max_count : a.tokens;
-    // As many rows as a sequence has, up to what the registers hold: a key that is fetched and converted serves all of them.
-    const long long most_rows = (long long)count * g.group;
-    g.rows = most_rows <= 8 ? 8 : most_rows <= 16 || c.d > 128 ? 16 : 32;
-    units = (long long)a.tokens * g.group / g.rows + c.batch;
-    if (units * c.heads > 0x7fffffffll) return TT_ERR_INVALID_ARG;
+    g.least = 1; g.most = 0x7fffffff;
+    g.scale_log2 = a.scale * 1.4426950408889634f;
     g.max_length = c.pages > 0 ? c.max_pages * c.block : 0;
     if (a.max_length > 0 && a.max_length < g.max_length) g.max_length = a.max_length;
-    long long span = g.max_length;
-    const long long tile_tokens = g.rows / g.group + 2;
-    if (a.window > 0 && a.window + tile_tokens < span) span = a.window + tile_tokens;
-    span += kRun;                                          // (splits begin at multiples of it)
-    // One sequence: a share for each CTA that the SMs hold at once.  Several, of lengths that only the device knows: a quarter of that, so that
-    // long and short ones even out.  No split is shorter than what makes joining it cheap.
-    const long long tiles = units * c.heads, slots = (long long)kSms * attend_ctas(c.d, g.rows / 8) * (c.batch > 1 ? 4 : 1);
-    constexpr int kGrain = kAttendWarps * kRun;
-    long long chunk = ((span - kRun) * tiles + slots - 1) / slots;
-    chunk = (chunk + kGrain - 1) / kGrain * kGrain;
-    if (chunk < 2 * kGrain) chunk = 2 * kGrain;
-    if (c.batch > 1 && chunk > 8 * kGrain) chunk = 8 * kGrain;
-    while ((span + chunk - 1) / chunk > kMostSplits || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
-    g.chunk = (int)(chunk < span ? chunk : span);
-    g.splits = (int)((span + chunk - 1) / chunk);
-    if (g.splits > 1) bytes = (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (c.d + 2) * 4;
-    g.scale_log2 = a.scale * 1.4426950408889634f;
+    g.q_wide = reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.q_token % 4 == 0 && a.q_head % 4 == 0;
+    g.y_wide = reinterpret_cast<uintptr_t>(a.y) % 8 == 0 && a.y_token % 4 == 0 && a.y_head % 4 == 0;
+    const int count = c.batch > 1 && a.max_count > 0 && a.max_count < a.tokens ? a.max_count : a.tokens;
+    const long long most_rows = (long long)count * g.group;
+    if (most_rows > 0x7fffffff) return TT_ERR_INVALID_ARG;
+    const auto span_of = [&](int rows) {
+        const long long span = g.max_length, tokens = rows / g.group + 2;
+        return a.window > 0 && a.window + tokens < span ? a.window + tokens : span;
+    };
+    // More than kFewRows rows of a sequence are a prompt's: its tiles take the tensor cores, whose minimum is 128 rows.  (A window must be longer than
+    // what a tile's rows and a step span, so that no step is at both ends of it.)
+    const bool prompts = most_rows > kFewRows && prompt_built_for(c.d) && (a.window == 0 || a.window > kPromptRows / g.group + 2 * kPromptTokens + 2);
+    const bool few = !prompts || c.batch > 1;
+    if (few) {
+        Attend& f = plan.few;
+        f = g;
+        // As many rows as a sequence has, up to what the registers hold: a key that is fetched and converted serves all of them.
+        f.rows = most_rows <= 8 ? 8 : most_rows <= 16 || c.d > 128 ? 16 : 32;
+        f.by_sequence = prompts;
+        if (prompts) f.most = kFewRows;
+        plan.few_units = f.by_sequence ? c.batch : (long long)a.tokens * g.group / f.rows + c.batch;
+        const long long tiles = plan.few_units * c.heads, span = span_of(f.rows) + kRun;      // (splits begin at multiples of kRun)
+        if (tiles > 0x7fffffffll) return TT_ERR_INVALID_ARG;
+        // One sequence: a share for each CTA that the SMs hold at once.  Several, of lengths that only the device knows: a quarter of that, so
+        // that long and short ones even out.  No split is shorter than what makes joining it cheap.
+        const long long slots = (long long)kSms * attend_ctas(c.d, f.rows / 8) * (c.batch > 1 ? 4 : 1);
+        constexpr int kGrain = kAttendWarps * kRun;
+        long long chunk = ((span - kRun) * tiles + slots - 1) / slots;
+        chunk = (chunk + kGrain - 1) / kGrain * kGrain;
+        if (chunk < 2 * kGrain) chunk = 2 * kGrain;
+        if (c.batch > 1 && chunk > 8 * kGrain) chunk = 8 * kGrain;
+        while ((span + chunk - 1) / chunk > kMostSplits || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
+        f.chunk = (int)(chunk < span ? chunk : span);
+        f.splits = (int)((span + chunk - 1) / chunk);
+        plan.bytes = workspace_part(f, plan.few_units);
+    }
+    if (prompts) {
+        Attend& p = plan.prompt;
+        p = g;
+        p.rows = kPromptRows;
+        if (few) p.least = kFewRows + 1;
+        plan.prompt_units = (long long)a.tokens * g.group / kPromptRows + c.batch;
+        const long long tiles = plan.prompt_units * c.heads, span = span_of(kPromptRows) + kPromptTokens;
+        if (tiles > 0x7fffffffll) return TT_ERR_INVALID_ARG;
+        // Fewer tiles than SMs: the keys are split as well, into shares of 1024 tokens at least.
+        long long chunk = span;
+        if (tiles < kSms) {
+            const long long shares = kSms / tiles;
+            chunk = (span + shares - 1) / shares;
+            chunk = (chunk + kPromptTokens - 1) / kPromptTokens * kPromptTokens;
+            if (chunk < 1024) chunk = 1024;
+            while ((span + chunk - 1) / chunk > kPromptSplits) chunk += kPromptTokens;
+        }
+        p.chunk = (int)(chunk < span ? chunk : (span + kPromptTokens - 1) / kPromptTokens * kPromptTokens);
+        p.splits = (int)((span + p.chunk - 1) / p.chunk);
+        plan.prompt_at = plan.bytes = (plan.bytes + 15) / 16 * 16;
+        plan.bytes += workspace_part(p, plan.prompt_units);
+    }
     return TT_OK;
+}
+static void place(Attend& g, long long units, void* workspace, long long at) {
+    uint8_t* w = static_cast<uint8_t*>(workspace) + (g.splits > 1 ? at : 0);
+    g.counters = reinterpret_cast<unsigned*>(w);
+    g.partial = reinterpret_cast<float*>(w + (units * g.a.cache.heads * 4 + 15) / 16 * 16);
 }
 
 template <int D, int NT>
@@ -731,30 +713,32 @@ extern "C" tt_status tt_cache_append(const tt_cache_append_args* a, void* stream
 
 extern "C" tt_status tt_cache_attention_workspace(const tt_cache_attention_args* a, int64_t* bytes) {
     if (!a || !bytes) return TT_ERR_INVALID_ARG;
-    Attend g;
-    long long units = 0, need = 0;
-    const tt_status s = plan_attend(*a, g, units, need);
-    *bytes = s == TT_OK ? need : 0;
+    AttendPlan plan;
+    const tt_status s = plan_attend(*a, plan);
+    *bytes = s == TT_OK ? plan.bytes : 0;
     return s;
 }
 
 extern "C" tt_status tt_cache_attention(const tt_cache_attention_args* a, void* stream) {
     if (!a) return TT_ERR_INVALID_ARG;
-    Attend g;
-    long long units = 0, need = 0;
-    tt_status s = plan_attend(*a, g, units, need);
-    if (s != TT_OK || units == 0) return s;
+    AttendPlan plan;
+    tt_status s = plan_attend(*a, plan);
+    if (s != TT_OK || (plan.few_units == 0 && plan.prompt_units == 0)) return s;
     const tt_cache& c = a->cache;
-    if (g.max_length > 0) s = check_cache_memory(c);
+    if (c.pages > 0 && c.max_pages > 0) s = check_cache_memory(c);
     if (s != TT_OK) return s;
     if (!a->q || !a->y || !a->starts || !a->lengths || !a->status || a->q_token < 0 || a->q_head < 0 || a->y_token < 0 || a->y_head < 0) return TT_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(a->q) % 2 || reinterpret_cast<uintptr_t>(a->y) % 2 || reinterpret_cast<uintptr_t>(a->starts) % 4 || reinterpret_cast<uintptr_t>(a->lengths) % 4 ||
         reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
-    if (need > 0 && (!a->workspace || !on16(a->workspace) || a->workspace_bytes < need)) return TT_ERR_INVALID_ARG;
-    g.q_wide = reinterpret_cast<uintptr_t>(a->q) % 8 == 0 && a->q_token % 4 == 0 && a->q_head % 4 == 0;
-    g.y_wide = reinterpret_cast<uintptr_t>(a->y) % 8 == 0 && a->y_token % 4 == 0 && a->y_head % 4 == 0;
-    g.counters = static_cast<unsigned*>(a->workspace);
-    g.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(a->workspace) + (units * c.heads * 4 + 15) / 16 * 16);
+    if (plan.bytes > 0 && (!a->workspace || !on16(a->workspace) || a->workspace_bytes < plan.bytes)) return TT_ERR_INVALID_ARG;
+    if (plan.prompt_units > 0) {
+        place(plan.prompt, plan.prompt_units, a->workspace, plan.prompt_at);
+        s = status_of(launch_attend_prompt(plan.prompt, plan.prompt_units, stream));
+        if (s != TT_OK || plan.few_units == 0) return s;
+    }
+    const Attend& g = plan.few;
+    const long long units = plan.few_units;
+    place(plan.few, units, a->workspace, 0);
     switch (c.d) {
         case 32: return status_of(launch_attend_rows<32>(g, units, stream));
         case 64: return status_of(launch_attend_rows<64>(g, units, stream));

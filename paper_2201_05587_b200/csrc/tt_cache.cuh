@@ -1,0 +1,102 @@
+// The paged e4m3 cache: what its kernels share.
+#pragma once
+#include "tt_ptx.cuh"
+#include "tt_f8.cuh"
+
+namespace tt {
+
+__device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(status, 0u, (unsigned)TT_ERR_INVALID_ARG); }
+
+// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] / per + extra * b and up (as many as it can need
+// at most), so a unit finds its sequence by bisection.
+__device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
+    int lo = 0, hi = batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (starts[mid] * mul / per + (long long)extra * mid <= unit) lo = mid; else hi = mid - 1;
+    }
+    first = starts[lo] * mul / per + (long long)extra * lo;
+    return lo;
+}
+
+constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it
+
+// An attention call, as one of its kernels takes it.
+struct Attend {
+    tt_cache_attention_args a;
+    int group, rows;                        // query heads of a key head; rows of a tile
+    int chunk, splits, max_length;          // tokens of a split, most splits
+    int least, most;                        // rows of the sequences that the kernel takes
+    int by_sequence;                        // no more than one tile each: tile b is sequence b's
+    int q_wide, y_wide;                     // four values of q, of y at a time
+    float scale_log2;                       // the scale times log2(e)
+    unsigned* counters; float* partial;
+};
+constexpr int kPromptRows = 256;            // rows of a tile of tt_attend_prompt_kernel
+constexpr int kPromptSplits = 32;           // its most splits of a sequence
+constexpr int kPromptTokens = 128;          // tokens of a step of it
+bool prompt_built_for(int d);
+cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream);
+
+// What a tile of rows has to do with the tokens of its sequence: false if there is nothing (or an error, which is reported).
+struct TileView {
+    int b, start, rows;                     // sequence, its first token in the batch, the tile's rows
+    int t0, h0;                             // the first row: token (of the new ones) and head (of the group)
+    int before;                             // tokens in front of the new ones (negative: the first queries see nothing)
+    int lo, hi;                             // tokens that any row sees
+    int whole_lo, whole_hi;                 // tokens that every row sees
+};
+__device__ __forceinline__ bool view_tile(const Attend& g, int tile_rows, long long unit, TileView& v) {
+    const tt_cache& c = g.a.cache;
+    long long first_unit = unit;
+    v.b = g.by_sequence ? (int)unit : sequence_of(g.a.starts, c.batch, g.group, tile_rows, 1, unit, first_unit);
+    v.start = g.a.starts[v.b];
+    const int count = g.a.starts[v.b + 1] - v.start, length = g.a.lengths[v.b];
+    if (count == 0) return false;
+    if (count < 0 || v.start < 0 || v.start + (long long)count > g.a.tokens || length < 0 || length > g.max_length) {
+        if (threadIdx.x == 0) report_invalid(g.a.status);
+        return false;
+    }
+    const long long row0 = (unit - first_unit) * tile_rows, all = (long long)count * g.group;
+    if (row0 >= all || all < g.least || all > g.most) return false;
+    v.rows = (int)min((long long)tile_rows, all - row0);
+    v.t0 = (int)(row0 / g.group);
+    v.h0 = (int)(row0 - (long long)v.t0 * g.group);
+    const int t1 = v.t0 + (v.h0 + v.rows - 1) / g.group;
+    v.before = length - count;
+    v.lo = g.a.window > 0 ? max(0, v.before + v.t0 + 1 - g.a.window) : 0;
+    v.hi = g.a.causal ? max(0, min(length, v.before + t1 + 1)) : length;
+    v.whole_lo = g.a.window > 0 ? max(0, v.before + t1 + 1 - g.a.window) : 0;
+    v.whole_hi = g.a.causal ? max(0, min(length, v.before + v.t0 + 1)) : length;
+    return true;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {      // 2^x to two units in the last place; 0 below 2^-126
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// A non-zero byte for each e4m3 byte of the word that is NaN.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// Four values of a 16-bit type.
+__device__ __forceinline__ void load_four(const void* p, long long i, int type, int wide, float (&v)[4]) {
+    if (wide) {
+        const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+        const float2 a = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.x) : up2<TT_TYPE_BF16>(u.x), b = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.y) : up2<TT_TYPE_BF16>(u.y);
+        v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = load_one(p, i + e, type);
+    }
+}
+__device__ __forceinline__ void store_four(void* p, long long i, int type, int wide, const float (&v)[4]) {
+    if (wide) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+            type == TT_TYPE_F16 ? make_uint2(down2<TT_TYPE_F16>(v[0], v[1]), down2<TT_TYPE_F16>(v[2], v[3])) : make_uint2(down2<TT_TYPE_BF16>(v[0], v[1]), down2<TT_TYPE_BF16>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) store_one(p, i + e, type, v[e]);
+    }
+}
+
+}  // namespace tt

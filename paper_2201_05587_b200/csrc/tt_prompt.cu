@@ -1,0 +1,495 @@
+// Attention of prompts over the paged e4m3 cache: many rows (queries of the heads that share a key head) for each key, so the products and the
+// exponentials are the bound, not the cache's bytes.
+//
+// A CTA has two tiles of 128 rows and walks the keys 128 at a time.  Four warps bring keys and values from the pages, turn them into 16-bit floating
+// point (exactly) and leave them as operand tiles, which serve both tiles of rows.  S = Q K^T goes to tensor memory; a thread of the softmax warps
+// has one row of it, takes its maximum, and leaves P = 2^(s - m) in S's place as the first operand of O += P V, whose sums stay
+// in tensor memory.  While one tile's softmax runs, the tensor core is at the other tile's products.
+//   O is multiplied only when a maximum has grown by more than 2^8 since it was last: P may be up to 2^8 times what it
+// would be, which 16 bits have room for (it is brought to 2^15 at most), and the row's sum has the same factor.  A page's scale of values is in
+// P too, as the part of the exponent, over the largest scale so far.
+//   NaN in values that only some rows of the tile see (the steps at the edge of what is visible) are taken out of the product and put into
+// the outputs of the rows that do: a column's first such token (at the upper edge; its last one at the lower) decides.
+#include <cuda_runtime.h>
+#include <climits>
+#include "tt_cache.cuh"
+
+namespace tt {
+
+constexpr int kPromptThreads = 512;         // warps 0-3 and 4-7 softmax of a tile each, 8-11 keys and values, 12 MMA and tensor memory
+constexpr uint32_t kAtom = 128u * 128u;     // 128 rows of 64 values
+
+__device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+__device__ __forceinline__ uint4 ld_once(const void* p) {                          // (read by this CTA once)
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+// What the softmax needs to know of a step's eight groups of 16 tokens.
+struct StepScales { float key[8], shift[8], back[8]; float ref; };
+
+template <int D>
+struct PromptShape {
+    static constexpr int kAtoms = D / 64;
+    static constexpr uint32_t kTile = kAtoms * kAtom;                    // bytes of 128 rows of queries, keys or values
+    static constexpr uint32_t kBytes = 1024u + 6u * kTile;               // two of each
+    static constexpr uint32_t kScores = 0, kOut = 256;                   // columns of tensor memory: S (and P) of both tiles, O of both
+};
+
+template <int D>
+__global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(const __grid_constant__ Attend g) {
+    typedef PromptShape<D> S;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_done[2], drained;
+    __shared__ StepScales scales[4];
+    __shared__ int nan_first[D], nan_last[D];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag, last_one;
+    constexpr unsigned long long kWait = 1000000000ull;
+
+    const tt_cache& c = g.a.cache;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, head = blockIdx.y;
+    volatile int* abortp = &abort_flag;
+    pdl_allow_next();
+    pdl_wait_prev();
+    TileView view;
+    const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most)
+    if (!view_tile(g, kPromptRows, unit, view)) return;
+    const int base_token = view.lo / kPromptTokens * kPromptTokens;
+    const int active = view.hi > view.lo ? (view.hi - base_token + g.chunk - 1) / g.chunk : 1;
+    if ((int)blockIdx.z >= active) return;
+    const int from = base_token + (int)blockIdx.z * g.chunk, to = min(view.hi, from + g.chunk);
+    const int steps = to > from ? (to - from + kPromptTokens - 1) / kPromptTokens : 0;
+    const int tiles = view.rows > 128 ? 2 : 1;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_s = base, k_s = base + 2u * S::kTile, v_s = base + 4u * S::kTile;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&q_full), 8u);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&k_full[i]), 4u); mbar_init(smem_u32(&v_full[i]), 4u);
+            mbar_init(smem_u32(&k_empty[i]), 1u); mbar_init(smem_u32(&v_empty[i]), 1u);
+            mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i]), 4u); mbar_init(smem_u32(&o_done[i]), 1u);
+        }
+        mbar_init(smem_u32(&drained), 1u);
+        abort_flag = 0;
+        fence_mbar_init();
+        fence_proxy_async_shared();
+    }
+    if ((int)threadIdx.x < D) { nan_first[threadIdx.x] = INT_MAX; nan_last[threadIdx.x] = INT_MIN; }
+    if (warp == 12) {
+        tmem_alloc(smem_u32(&tmem_slot), 512u);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
+
+    // a softmax thread's row
+    const int tile = warp >> 2, r = (int)threadIdx.x & 255;
+    const bool mine = warp < 8 && r < view.rows;
+    const int row_t = view.t0 + (view.h0 + r) / g.group, row_h = head * g.group + (view.h0 + r) % g.group;
+    float top = -INFINITY, used = 0.f, sum = 0.f, ref = 0.f;              // maximum; the one that O and the sum are relative to; the unit of O
+    bool fine = true;
+
+    if (warp < 8) {
+        // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
+        const int lr = r & 127;
+        const long long at = (view.start + (long long)row_t) * g.a.q_token + (long long)row_h * g.a.q_head;
+        float most = 0.f;
+        if (mine) {
+#pragma unroll 8
+            for (int i = 0; i < D; i += 4) {
+                float v[4];
+                load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) most = finite_max(most, v[e]);
+            }
+        }
+        const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14;
+        const float size = __int_as_float((min(254, max(1, 127 + 14 + 127 - ex))) << 23);
+        const float up = g.scale_log2 < 0.f ? -size : size;               // (the factor of the scores is positive: their maximum is the products')
+        const float factor = fabsf(g.scale_log2) / size;
+        const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)lr * 128u;
+#pragma unroll 8
+        for (int i = 0; i < D; i += 4) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (mine) load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
+            const uint32_t to_ = line + (uint32_t)(i >> 6) * kAtom + ((((uint32_t)(i & 63) >> 3) ^ (uint32_t)(lr & 7)) << 4) + (uint32_t)(i & 4) * 2u;
+            st_shared_u32(to_, down2<TT_TYPE_F16>(v[0] * up, v[1] * up));
+            st_shared_u32(to_ + 4u, down2<TT_TYPE_F16>(v[2] * up, v[3] * up));
+        }
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&q_full));
+
+        // ---------------- softmax ----------------
+        if (tile < tiles) {
+            const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
+            const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
+            const int pos = view.before + row_t;
+            const int row_hi = g.a.causal ? min(view.hi, pos + 1) : view.hi, row_lo = g.a.window > 0 ? pos + 1 - g.a.window : 0;
+            for (int i = 0; i < steps; ++i) {
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[tile]), (uint32_t)i & 1u, abortp, g.a.status, 31u, kWait))) { fine = false; break; }
+                tc_fence_after();
+                const int t = from + i * kPromptTokens;
+                const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
+                const int j_lo = row_lo - t, j_hi = row_hi - t;           // the row sees columns j_lo .. j_hi - 1
+                const StepScales& sc = scales[i & 3];
+                float mx = top;
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t v[32];
+                    tmem_ld32(s_t + 32u * h, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int gr = 0; gr < 2; ++gr) {
+                        float m = -INFINITY;
+                        if (whole) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) m = fmaxf(m, __uint_as_float(v[16 * gr + j]));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const int col = 32 * h + 16 * gr + j;
+                                m = col >= j_lo && col < j_hi ? fmaxf(m, __uint_as_float(v[16 * gr + j])) : m;
+                            }
+                        }
+                        mx = m == -INFINITY ? mx : fmaxf(mx, m * (factor * sc.key[2 * h + gr]));
+                    }
+                }
+                top = mx;
+                // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
+                const float new_ref = sc.ref;
+                const bool move = top > used + 8.f || (i == 0 || sum == 0.f ? top != used : false) || ref != new_ref;
+                if (__any_sync(0xffffffffu, move)) {
+                    const float now = top == -INFINITY ? 0.f : top;
+                    const float alpha = sum != 0.f ? exp2_fast(used - now) : 0.f;
+                    const float scale_o = ref == new_ref ? alpha : alpha * __fdividef(ref, new_ref);
+                    used = now;
+                    sum *= alpha;
+                    ref = new_ref;
+                    if (i > 0) {
+                        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&o_done[tile]), (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kWait))) { fine = false; break; }
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int h = 0; h < D; h += 32) {
+                            uint32_t v[32];
+                            tmem_ld32(o_t + (uint32_t)h, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * scale_o);
+#pragma unroll
+                            for (int j = 0; j < 32; j += 8) tmem_st8u(o_t + (uint32_t)(h + j), v + j);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    uint32_t v[32], p[16];
+                    tmem_ld32(s_t + 32u * h, v);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int gr = 0; gr < 2; ++gr) {
+                        const float f = factor * sc.key[2 * h + gr], add = sc.shift[2 * h + gr] - used;
+                        float part = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const int col = 32 * h + 16 * gr + j;
+                            float a = fmaf(__uint_as_float(v[16 * gr + j]), f, add), b = fmaf(__uint_as_float(v[16 * gr + j + 1]), f, add);
+                            if (!whole) {
+                                a = col >= j_lo && col < j_hi ? a : -INFINITY;
+                                b = col + 1 >= j_lo && col + 1 < j_hi ? b : -INFINITY;
+                            }
+                            a = exp2_fast(a);
+                            b = exp2_fast(b);
+                            part += a + b;
+                            p[8 * gr + (j >> 1)] = down2<TT_TYPE_F16>(a, b);
+                        }
+                        sum = fmaf(part, sc.back[2 * h + gr], sum);
+                    }
+                    tmem_st8u(s_t + 16u * h, p);
+                    tmem_st8u(s_t + 16u * h + 8u, p + 8);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile]));
+            }
+        }
+    } else if (warp < 12) {
+        // ---------------- keys and values: pages -> operand tiles ----------------
+        constexpr int kPieces = D / 16, kTokens = 128 / kPieces;          // 16-byte pieces of a token; tokens of a pass of the four warps
+        const int dt = (int)threadIdx.x - 256, piece = dt % kPieces, sub = dt / kPieces;
+        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + 16 * piece;
+        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + 16 * piece;
+        const int* table = c.table + view.b * c.table_row;
+        const int shift = 31 - __clz(c.block);
+        float most = 0.f;                                                 // the largest scale of values so far
+        const uint32_t swap = piece >= 4 ? 1u : 0u;                       // (half of the lanes begin with the second half: all banks at once)
+        const auto put = [&](uint32_t tile_s, int token, const uint4& raw) {
+            uint32_t h[8];
+            f16_pairs_of_e4m3(raw.x, h[0], h[1]);
+            f16_pairs_of_e4m3(raw.y, h[2], h[3]);
+            f16_pairs_of_e4m3(raw.z, h[4], h[5]);
+            f16_pairs_of_e4m3(raw.w, h[6], h[7]);
+            const uint32_t line = tile_s + (uint32_t)(piece >> 2) * kAtom + (uint32_t)token * 128u, c0 = 2u * ((uint32_t)piece & 3u), x = (uint32_t)token & 7u;
+            const auto half = [&](uint32_t w) {
+                const uint32_t at = line + (((c0 + w) ^ x) << 4);
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w ? h[4] : h[0]), "r"(w ? h[5] : h[1]), "r"(w ? h[6] : h[2]), "r"(w ? h[7] : h[3]) : "memory");
+            };
+            half(swap);
+            half(swap ^ 1u);
+        };
+        // lane g of the first eight has the page of the next step's group g
+        const auto page_of = [&](int i) {
+            const int t = from + i * kPromptTokens + 16 * (lane & 7);
+            return i < steps && t + 15 >= view.lo && t < to ? table[t >> shift] : -1;
+        };
+        int page = page_of(0);
+        for (int i = 0; i < steps; ++i) {
+            const int t = from + i * kPromptTokens, buf = i & 1;
+            const int group_t = t + 16 * (lane & 7);
+            const bool held = group_t + 15 >= view.lo && group_t < to;
+            const bool good = held && (unsigned)page < (unsigned)c.pages;
+            if (held && !good) report_invalid(g.a.status);
+            const float ks = good ? c.scale[0][page * c.s_page[0] + head * c.s_head[0]] : 0.f, vs = good ? c.scale[1][page * c.s_page[1] + head * c.s_head[1]] : 0.f;
+            const int pages = good ? page : -1;
+            page = page_of(i + 1);
+            uint4 kr[kPieces], vr[kPieces];
+            const auto fetch = [&](const uint8_t* from_, int w, uint4 (&to_)[kPieces]) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    const int token = p * kTokens + sub, pg = __shfl_sync(0xffffffffu, pages, token >> 4), tok = t + token;
+                    to_[p] = make_uint4(0u, 0u, 0u, 0u);
+                    if (pg >= 0 && tok >= view.lo && tok < to) to_[p] = ld_once(from_ + pg * c.page[w] + (tok & (c.block - 1)) * c.token[w]);
+                }
+            };
+            fetch(keys, 0, kr);
+            fetch(vals, 1, vr);
+            // the scales, before the keys report: two steps back everybody has read what lies here
+            if (warp == 8) {
+                float m = vs;
+#pragma unroll
+                for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                most = fmaxf(most, m);
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&k_empty[buf]), ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u, kWait))) break;
+            if (warp == 8 && lane < 8) {
+                StepScales& sc = scales[i & 3];
+                // (a share of less than 2^-40 of the largest scale is taken as that)
+                const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
+                sc.key[lane] = ks;
+                sc.shift[lane] = lg + 7.f;
+                sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
+                if (lane == 0) sc.ref = most;
+            }
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) put(k_s + (uint32_t)buf * S::kTile, p * kTokens + sub, kr[p]);
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
+            const bool low = t < view.whole_lo, high = g.a.causal && t + kPromptTokens > view.whole_hi;
+            if (low || high) {
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    uint32_t w[4] = {vr[p].x, vr[p].y, vr[p].z, vr[p].w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t n = nan_bytes(w[q]);
+                        if (n == 0u) continue;
+                        for (int e = 0; e < 4; ++e)
+                            if ((n >> (8 * e)) & 0x80u) {
+                                if (high) atomicMin(&nan_first[16 * piece + 4 * q + e], t + p * kTokens + sub);
+                                else atomicMax(&nan_last[16 * piece + 4 * q + e], t + p * kTokens + sub);
+                            }
+                        w[q] &= ~((n >> 7) * 0xffu);
+                    }
+                    vr[p] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&v_empty[buf]), ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u, kWait))) break;
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) put(v_s + (uint32_t)buf * S::kTile, p * kTokens + sub, vr[p]);
+            fence_proxy_async_shared();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&v_full[buf]));
+        }
+    } else if (warp == 12) {
+        // ---------------- MMA issuer ----------------
+        if (steps > 0 && elect_one()) {
+            constexpr uint32_t kIdescS = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+            constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);     // values: the columns are the contiguous axis
+            const uint64_t dk = make_desc(0u, 128);
+            // an MN-major tile: groups of eight tokens 1024 bytes apart, the next 64 columns an atom's 16 KB further on
+            const uint64_t dv = (uint64_t)(kAtom >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
+            const auto at = [](uint32_t a) { return (uint64_t)((a & 0x3FFFFu) >> 4); };
+            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return mbar_wait(smem_u32(bar), parity, abortp, g.a.status, where, kWait); };
+            const auto scores = [&](int tl, int buf) {
+                const uint64_t a = dk + at(q_s + (uint32_t)tl * S::kTile), b = dk + at(k_s + (uint32_t)buf * S::kTile);
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_f16(tmem + S::kScores + (uint32_t)tl * 128u, a + (uint64_t)((k >> 2) * (kAtom >> 4) + 2 * (k & 3)), b + (uint64_t)((k >> 2) * (kAtom >> 4) + 2 * (k & 3)), kIdescS, k > 0 ? 1u : 0u);
+                mma_commit(smem_u32(&s_full[tl]));
+            };
+            bool ok = wait(&q_full, 0u, 35u) && wait(&k_full[0], 0u, 36u);
+            if (ok) {
+                tc_fence_after();
+                for (int tl = 0; tl < tiles; ++tl) scores(tl, 0);
+                mma_commit(smem_u32(&k_empty[0]));
+            }
+            for (int i = 0; i < steps && ok; ++i) {
+                const int buf = i & 1, next = (i + 1) & 1;
+                for (int tl = 0; tl < tiles && ok; ++tl) {
+                    ok = wait(&p_ready[tl], (uint32_t)i & 1u, 37u) && (tl > 0 || wait(&v_full[buf], (uint32_t)(i >> 1) & 1u, 38u));
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t b = dv + at(v_s + (uint32_t)buf * S::kTile);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        mma_f16_ta(tmem + S::kOut + (uint32_t)(tl * D), tmem + S::kScores + (uint32_t)(tl * 128 + 8 * k), b + (uint64_t)(128 * k), kIdescO, i > 0 || k > 0 ? 1u : 0u);
+                    mma_commit(smem_u32(&o_done[tl]));
+                    if (tl == tiles - 1) mma_commit(smem_u32(&v_empty[buf]));
+                    if (i + 1 < steps) {
+                        // the next scores take P's place, behind the product that reads it
+                        ok = tl > 0 || wait(&k_full[next], (uint32_t)((i + 1) >> 1) & 1u, 39u);
+                        if (!ok) break;
+                        tc_fence_after();
+                        scores(tl, next);
+                        if (tl == tiles - 1) mma_commit(smem_u32(&k_empty[next]));
+                    }
+                }
+            }
+            // nothing of what was issued is to run on behind this CTA, also when somebody gave up (bounded)
+            mma_commit(smem_u32(&drained));
+            const unsigned long long t0 = global_timer_ns();
+            while (!mbar_try_wait(smem_u32(&drained), 0u)) if (global_timer_ns() - t0 > kWait) break;
+        }
+        __syncwarp();
+    }
+
+    // ---------------- out ----------------
+    __syncthreads();                                                      // (every NaN of the steps at the edges has been noted)
+    const long long place = unit * c.heads + head;
+    constexpr int kPart = kPromptRows * (D + 2);
+    const auto store = [&](int rr, int i, const float (&v)[4]) {
+        const int tt = (view.h0 + rr) / g.group;
+        store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
+    };
+    if (warp < 8 && tile < tiles) {
+        if (steps > 0 && fine) fine = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_done[tile]), (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u, kWait));
+        tc_fence_after();
+        if (fine) {
+            const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
+            const int pos = view.before + row_t;
+            // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
+            const float unit_o = ref * 0.0078125f * (active == 1 ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
+            float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
+#pragma unroll 1
+            for (int h = 0; h < D; h += 32) {
+                uint32_t v[32];
+                if (steps > 0) {
+                    tmem_ld32(o_t + (uint32_t)h, v);
+                    tmem_wait_ld();
+                }
+                if (mine) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        float x[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            x[e] = steps > 0 && sum != 0.f ? __uint_as_float(v[j + e]) * unit_o : 0.f;
+                            const int col = h + j + e;
+                            if (nan_first[col] <= pos || (g.a.window > 0 && nan_last[col] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
+                        }
+                        if (active == 1) store(r, h + j, x);
+                        else *reinterpret_cast<float4*>(left + h + j) = make_float4(x[0], x[1], x[2], x[3]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, sum);
+        }
+    }
+    tc_fence_before();
+    if (active > 1) __threadfence();
+    __syncthreads();
+    if (warp == 12) {
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512u);
+    }
+    if (active == 1) return;
+
+    // ---------------- the splits together, by the last CTA of the tile ----------------
+    if (threadIdx.x == 0) last_one = atomicAdd(g.counters + place, 1u) == (unsigned)active - 1u;
+    __syncthreads();
+    if (!last_one) return;
+    __threadfence();
+    const float* parts = g.partial + place * g.splits * kPart;
+    float* share = reinterpret_cast<float*>(smem_raw);                   // [split][row]
+    if ((int)threadIdx.x < view.rows) {
+        const int rr = threadIdx.x;
+        float mx = -INFINITY, l = 0.f;
+        for (int z = 0; z < active; ++z) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * rr));
+            if (ml.y != 0.f) mx = fmaxf(mx, ml.x);
+        }
+        for (int z = 0; z < active; ++z) {
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * rr));
+            const float k = ml.y != 0.f ? exp2_fast(ml.x - mx) : 0.f;
+            if (ml.y != 0.f) l += ml.y * k;
+            share[z * kPromptRows + rr] = k;
+        }
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+        for (int z = 0; z < active; ++z) share[z * kPromptRows + rr] *= inv;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < view.rows * (D / 4); e += kPromptThreads) {
+        const int rr = e / (D / 4), i = 4 * (e - rr * (D / 4));
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int z = 0; z < active; ++z) {
+            const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (long long)rr * D + i));
+            const float w = share[z * kPromptRows + rr];
+            v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
+        }
+        store(rr, i, v);
+    }
+    if (threadIdx.x == 0) g.counters[place] = 0u;                       // ready for the next call
+}
+
+bool prompt_built_for(int d) { return d == 64 || d == 128; }
+
+template <int D>
+static cudaError_t launch_prompt(const Attend& g, long long units, void* stream) {
+    typedef PromptShape<D> S;
+    static OncePerDevice raised;
+    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
+    if (ready != cudaSuccess) return ready;
+    return launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, g);
+}
+cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream) {
+    return g.a.cache.d == 64 ? launch_prompt<64>(g, units, stream) : launch_prompt<128>(g, units, stream);
+}
+
+}  // namespace tt
