@@ -17,6 +17,7 @@
 namespace tt {
 
 constexpr int kPromptThreads = 512;         // warps 0-3 and 4-7 softmax of a tile each, 8-11 keys and values, 12 MMA and tensor memory
+constexpr unsigned long long kPromptWait = 1000000000ull;                    // nanoseconds that a wait takes at most
 constexpr uint32_t kAtom = 128u * 128u;     // 128 rows of 64 values
 
 __device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -37,11 +38,41 @@ __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
-__device__ __forceinline__ uint4 ld_once(const void* p) {                          // (read by this CTA once)
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+__device__ __forceinline__ void tmem_ld8u(uint32_t taddr, uint32_t* v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ uint2 ld_once(const void* p) {                          // (read by this CTA once)
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
     return v;
 }
+// Registers of a warpgroup from here on.  512 threads begin with 128 each (65536): 184 for the softmax's
+// two, 96 and 40 for the others make 64512.
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// mbar_wait without the call of a function (whose registers would be those of the launch, not of the warpgroup).
+__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* status, unsigned where) {
+    const uint32_t b = smem_u32(bar);
+    if (mbar_try_wait(b, parity)) return true;
+    const unsigned long long t0 = global_timer_ns();
+#pragma unroll 1
+    for (unsigned spins = 1; !mbar_try_wait(b, parity); ++spins) {
+        if ((spins & 31u) != 0u) continue;
+        if (*abort_flag) return false;
+        if (global_timer_ns() - t0 > kPromptWait) {
+            *abort_flag = 1;
+            atomicCAS(status, 0u, (unsigned)TT_ERR_TIMEOUT | (where << 8));
+            return false;
+        }
+    }
+    return true;
+}
+
+// Named barriers: 1 the softmax and the warps of keys and values, 2 the softmax and the MMA warp (at the end), 3 the softmax alone.
+__device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+__device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // What the softmax needs to know of a step's eight groups of 16 tokens.
 struct StepScales { float key[8], shift[8], back[8]; float ref; };
@@ -63,7 +94,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     __shared__ int nan_first[D], nan_last[D];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, last_one;
-    constexpr unsigned long long kWait = 1000000000ull;
 
     const tt_cache& c = g.a.cache;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, head = blockIdx.y;
@@ -112,6 +142,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     bool fine = true;
 
     if (warp < 8) {
+        registers_up<184>();
         // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
         const int lr = r & 127;
         const long long at = (view.start + (long long)row_t) * g.a.q_token + (long long)row_h * g.a.q_head;
@@ -149,33 +180,27 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const int pos = view.before + row_t;
             const int row_hi = g.a.causal ? min(view.hi, pos + 1) : view.hi, row_lo = g.a.window > 0 ? pos + 1 - g.a.window : 0;
             for (int i = 0; i < steps; ++i) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[tile]), (uint32_t)i & 1u, abortp, g.a.status, 31u, kWait))) { fine = false; break; }
+                if (!__all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u))) { fine = false; break; }
                 tc_fence_after();
                 const int t = from + i * kPromptTokens;
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
                 const int j_lo = row_lo - t, j_hi = row_hi - t;           // the row sees columns j_lo .. j_hi - 1
                 const StepScales& sc = scales[i & 3];
+                uint32_t v[128];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) tmem_ld32(s_t + 32u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
+                tmem_wait_ld();
+                if (!whole) {
+#pragma unroll
+                    for (int k = 0; k < 128; ++k) v[k] = k >= j_lo && k < j_hi ? v[k] : 0xff800000u;      // (-inf)
+                }
                 float mx = top;
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    uint32_t v[32];
-                    tmem_ld32(s_t + 32u * h, v);
-                    tmem_wait_ld();
+                for (int gr = 0; gr < 8; ++gr) {
+                    float m = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
 #pragma unroll
-                    for (int gr = 0; gr < 2; ++gr) {
-                        float m = -INFINITY;
-                        if (whole) {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) m = fmaxf(m, __uint_as_float(v[16 * gr + j]));
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const int col = 32 * h + 16 * gr + j;
-                                m = col >= j_lo && col < j_hi ? fmaxf(m, __uint_as_float(v[16 * gr + j])) : m;
-                            }
-                        }
-                        mx = m == -INFINITY ? mx : fmaxf(mx, m * (factor * sc.key[2 * h + gr]));
-                    }
+                    for (int k = 2; k < 16; k += 2) m = fmaxf(fmaxf(m, __uint_as_float(v[16 * gr + k])), __uint_as_float(v[16 * gr + k + 1]));
+                    mx = m == -INFINITY ? mx : fmaxf(mx, m * (factor * sc.key[gr]));
                 }
                 top = mx;
                 // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
@@ -189,46 +214,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     sum *= alpha;
                     ref = new_ref;
                     if (i > 0) {
-                        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&o_done[tile]), (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kWait))) { fine = false; break; }
+                        if (!__all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u))) { fine = false; break; }
                         tc_fence_after();
 #pragma unroll 1
-                        for (int h = 0; h < D; h += 32) {
-                            uint32_t v[32];
-                            tmem_ld32(o_t + (uint32_t)h, v);
+                        for (int h = 0; h < D; h += 16) {                 // (few at a time: the scores are in registers)
+                            uint32_t o[16];
+                            tmem_ld8u(o_t + (uint32_t)h, o);
+                            tmem_ld8u(o_t + (uint32_t)h + 8u, o + 8);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * scale_o);
-#pragma unroll
-                            for (int j = 0; j < 32; j += 8) tmem_st8u(o_t + (uint32_t)(h + j), v + j);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
+                            tmem_st8u(o_t + (uint32_t)h, o);
+                            tmem_st8u(o_t + (uint32_t)h + 8u, o + 8);
                         }
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 4; ++h) {
-                    uint32_t v[32], p[16];
-                    tmem_ld32(s_t + 32u * h, v);
-                    tmem_wait_ld();
+                for (int gr = 0; gr < 8; ++gr) {
+                    // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
+                    const float f = fmaxf(factor * sc.key[gr], 1.17549435e-38f), add = sc.shift[gr] - used;
+                    float2 part = make_float2(0.f, 0.f);
+                    uint32_t p[8];
 #pragma unroll
-                    for (int gr = 0; gr < 2; ++gr) {
-                        const float f = factor * sc.key[2 * h + gr], add = sc.shift[2 * h + gr] - used;
-                        float part = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const int col = 32 * h + 16 * gr + j;
-                            float a = fmaf(__uint_as_float(v[16 * gr + j]), f, add), b = fmaf(__uint_as_float(v[16 * gr + j + 1]), f, add);
-                            if (!whole) {
-                                a = col >= j_lo && col < j_hi ? a : -INFINITY;
-                                b = col + 1 >= j_lo && col + 1 < j_hi ? b : -INFINITY;
-                            }
-                            a = exp2_fast(a);
-                            b = exp2_fast(b);
-                            part += a + b;
-                            p[8 * gr + (j >> 1)] = down2<TT_TYPE_F16>(a, b);
-                        }
-                        sum = fmaf(part, sc.back[2 * h + gr], sum);
+                    for (int k = 0; k < 16; k += 2) {
+                        float2 e = fma_pair(make_float2(__uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1])), make_float2(f, f), make_float2(add, add));
+                        e.x = exp2_fast(e.x);
+                        e.y = exp2_fast(e.y);
+                        part = fma_pair(e, make_float2(1.f, 1.f), part);
+                        p[k >> 1] = down2<TT_TYPE_F16>(e.x, e.y);
                     }
-                    tmem_st8u(s_t + 16u * h, p);
-                    tmem_st8u(s_t + 16u * h + 8u, p + 8);
+                    sum = fmaf(part.x + part.y, sc.back[gr], sum);
+                    tmem_st8u(s_t + 8u * gr, p);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -236,29 +252,108 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile]));
             }
         }
+        // ---------------- out ----------------
+        named_sync(1, 384);                                               // (every NaN of the steps at the edges has been noted)
+        const long long place = unit * c.heads + head;
+        constexpr int kPart = kPromptRows * (D + 2);
+        const auto store = [&](int rr, int i, const float (&v)[4]) {
+            const int tt = (view.h0 + rr) / g.group;
+            store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
+        };
+        if (tile < tiles) {
+            if (steps > 0 && fine) fine = __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u));
+            tc_fence_after();
+            if (fine) {
+                const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
+                const int pos = view.before + row_t;
+                // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
+                const float unit_o = ref * 0.0078125f * (active == 1 ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
+                float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
+#pragma unroll 1
+                for (int h = 0; h < D; h += 32) {
+                    uint32_t v[32];
+                    if (steps > 0) {
+                        tmem_ld32(o_t + (uint32_t)h, v);
+                        tmem_wait_ld();
+                    }
+                    if (mine) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 4) {
+                            float x[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                x[e] = steps > 0 && sum != 0.f ? __uint_as_float(v[j + e]) * unit_o : 0.f;
+                                const int col = h + j + e;
+                                if (nan_first[col] <= pos || (g.a.window > 0 && nan_last[col] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
+                            }
+                            if (active == 1) store(r, h + j, x);
+                            else *reinterpret_cast<float4*>(left + h + j) = make_float4(x[0], x[1], x[2], x[3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, sum);
+            }
+        }
+        tc_fence_before();
+        __syncwarp();
+        named_arrive(2, 288);                                             // (the tensor memory has been read)
+        if (active == 1) return;
+
+        // ---------------- the splits together, by the last CTA of the tile ----------------
+        __threadfence();
+        named_sync(3, 256);
+        if (threadIdx.x == 0) last_one = atomicAdd(g.counters + place, 1u) == (unsigned)active - 1u;
+        named_sync(3, 256);
+        if (!last_one) return;
+        __threadfence();
+        const float* parts = g.partial + place * g.splits * kPart;
+        float* share = reinterpret_cast<float*>(smem_raw);               // [split][row]
+        if (mine) {
+            float mx = -INFINITY, l = 0.f;
+            for (int z = 0; z < active; ++z) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * r));
+                if (ml.y != 0.f) mx = fmaxf(mx, ml.x);
+            }
+            for (int z = 0; z < active; ++z) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * r));
+                const float k = ml.y != 0.f ? exp2_fast(ml.x - mx) : 0.f;
+                if (ml.y != 0.f) l += ml.y * k;
+                share[z * kPromptRows + r] = k;
+            }
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+            for (int z = 0; z < active; ++z) share[z * kPromptRows + r] *= inv;
+        }
+        named_sync(3, 256);
+        for (int e = threadIdx.x; e < view.rows * (D / 4); e += 256) {
+            const int rr = e / (D / 4), i = 4 * (e - rr * (D / 4));
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int z = 0; z < active; ++z) {
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (long long)rr * D + i));
+                const float w = share[z * kPromptRows + rr];
+                v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
+            }
+            store(rr, i, v);
+        }
+        if (threadIdx.x == 0) g.counters[place] = 0u;                    // ready for the next call
     } else if (warp < 12) {
+        registers_down<96>();
         // ---------------- keys and values: pages -> operand tiles ----------------
-        constexpr int kPieces = D / 16, kTokens = 128 / kPieces;          // 16-byte pieces of a token; tokens of a pass of the four warps
-        const int dt = (int)threadIdx.x - 256, piece = dt % kPieces, sub = dt / kPieces;
-        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + 16 * piece;
-        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + 16 * piece;
+        // Eight lanes have a token, eight values of each 64 of it (a 16-byte chunk of an operand's line: all banks at once); the four warps take the
+        // 16 tokens of a group at a time.
+        const int dt = (int)threadIdx.x - 256, piece = dt & 7, sub = dt >> 3;
+        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + sub * c.token[0] + 8 * piece;
+        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + sub * c.token[1] + 8 * piece;
         const int* table = c.table + view.b * c.table_row;
         const int shift = 31 - __clz(c.block);
         float most = 0.f;                                                 // the largest scale of values so far
-        const uint32_t swap = piece >= 4 ? 1u : 0u;                       // (half of the lanes begin with the second half: all banks at once)
-        const auto put = [&](uint32_t tile_s, int token, const uint4& raw) {
-            uint32_t h[8];
+        const uint32_t chunk = (uint32_t)sub * 128u + ((((uint32_t)piece) ^ ((uint32_t)sub & 7u)) << 4);
+        const auto put = [&](uint32_t tile_s, int group, int atom, const uint2& raw) {
+            uint32_t h[4];
             f16_pairs_of_e4m3(raw.x, h[0], h[1]);
             f16_pairs_of_e4m3(raw.y, h[2], h[3]);
-            f16_pairs_of_e4m3(raw.z, h[4], h[5]);
-            f16_pairs_of_e4m3(raw.w, h[6], h[7]);
-            const uint32_t line = tile_s + (uint32_t)(piece >> 2) * kAtom + (uint32_t)token * 128u, c0 = 2u * ((uint32_t)piece & 3u), x = (uint32_t)token & 7u;
-            const auto half = [&](uint32_t w) {
-                const uint32_t at = line + (((c0 + w) ^ x) << 4);
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w ? h[4] : h[0]), "r"(w ? h[5] : h[1]), "r"(w ? h[6] : h[2]), "r"(w ? h[7] : h[3]) : "memory");
-            };
-            half(swap);
-            half(swap ^ 1u);
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(tile_s + chunk + (uint32_t)atom * kAtom + (uint32_t)group * 2048u), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
         };
         // lane g of the first eight has the page of the next step's group g
         const auto page_of = [&](int i) {
@@ -275,13 +370,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const float ks = good ? c.scale[0][page * c.s_page[0] + head * c.s_head[0]] : 0.f, vs = good ? c.scale[1][page * c.s_page[1] + head * c.s_head[1]] : 0.f;
             const int pages = good ? page : -1;
             page = page_of(i + 1);
-            uint4 kr[kPieces], vr[kPieces];
-            const auto fetch = [&](const uint8_t* from_, int w, uint4 (&to_)[kPieces]) {
+            uint2 kr[8][S::kAtoms], vr[8][S::kAtoms];
+            const auto fetch = [&](const uint8_t* data, int w, uint2 (&to_)[8][S::kAtoms]) {
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) {
-                    const int token = p * kTokens + sub, pg = __shfl_sync(0xffffffffu, pages, token >> 4), tok = t + token;
-                    to_[p] = make_uint4(0u, 0u, 0u, 0u);
-                    if (pg >= 0 && tok >= view.lo && tok < to) to_[p] = ld_once(from_ + pg * c.page[w] + (tok & (c.block - 1)) * c.token[w]);
+                for (int p = 0; p < 8; ++p) {
+                    const int pg = __shfl_sync(0xffffffffu, pages, p), first = t + 16 * p, tok = first + sub;
+                    const uint8_t* at = data + pg * c.page[w] + (first & (c.block - 1)) * c.token[w];
+                    const bool any = pg >= 0 && tok >= view.lo && tok < to;
+#pragma unroll
+                    for (int a = 0; a < S::kAtoms; ++a) to_[p][a] = any ? ld_once(at + 64 * a) : make_uint2(0u, 0u);
                 }
             };
             fetch(keys, 0, kr);
@@ -293,7 +390,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 most = fmaxf(most, m);
             }
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&k_empty[buf]), ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u, kWait))) break;
+            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u))) break;
             if (warp == 8 && lane < 8) {
                 StepScales& sc = scales[i & 3];
                 // (a share of less than 2^-40 of the largest scale is taken as that)
@@ -304,46 +401,54 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 if (lane == 0) sc.ref = most;
             }
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) put(k_s + (uint32_t)buf * S::kTile, p * kTokens + sub, kr[p]);
+            for (int p = 0; p < 8; ++p)
+#pragma unroll
+                for (int a = 0; a < S::kAtoms; ++a) put(k_s + (uint32_t)buf * S::kTile, p, a, kr[p][a]);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
             const bool low = t < view.whole_lo, high = g.a.causal && t + kPromptTokens > view.whole_hi;
             if (low || high) {
 #pragma unroll
-                for (int p = 0; p < kPieces; ++p) {
-                    uint32_t w[4] = {vr[p].x, vr[p].y, vr[p].z, vr[p].w};
+                for (int p = 0; p < 8; ++p)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t n = nan_bytes(w[q]);
-                        if (n == 0u) continue;
-                        for (int e = 0; e < 4; ++e)
-                            if ((n >> (8 * e)) & 0x80u) {
-                                if (high) atomicMin(&nan_first[16 * piece + 4 * q + e], t + p * kTokens + sub);
-                                else atomicMax(&nan_last[16 * piece + 4 * q + e], t + p * kTokens + sub);
-                            }
-                        w[q] &= ~((n >> 7) * 0xffu);
+                    for (int a = 0; a < S::kAtoms; ++a) {
+                        uint32_t w[2] = {vr[p][a].x, vr[p][a].y};
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const uint32_t n = nan_bytes(w[q]);
+                            if (n == 0u) continue;
+                            for (int e = 0; e < 4; ++e)
+                                if ((n >> (8 * e)) & 0x80u) {
+                                    if (high) atomicMin(&nan_first[64 * a + 8 * piece + 4 * q + e], t + 16 * p + sub);
+                                    else atomicMax(&nan_last[64 * a + 8 * piece + 4 * q + e], t + 16 * p + sub);
+                                }
+                            w[q] &= ~((n >> 7) * 0xffu);
+                        }
+                        vr[p][a] = make_uint2(w[0], w[1]);
                     }
-                    vr[p] = make_uint4(w[0], w[1], w[2], w[3]);
-                }
             }
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&v_empty[buf]), ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u, kWait))) break;
+            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u))) break;
 #pragma unroll
-            for (int p = 0; p < kPieces; ++p) put(v_s + (uint32_t)buf * S::kTile, p * kTokens + sub, vr[p]);
+            for (int p = 0; p < 8; ++p)
+#pragma unroll
+                for (int a = 0; a < S::kAtoms; ++a) put(v_s + (uint32_t)buf * S::kTile, p, a, vr[p][a]);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&v_full[buf]));
         }
-    } else if (warp == 12) {
+        named_arrive(1, 384);
+    } else {
+        registers_down<40>();
         // ---------------- MMA issuer ----------------
-        if (steps > 0 && elect_one()) {
+        if (warp == 12 && steps > 0 && elect_one()) {
             constexpr uint32_t kIdescS = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
             constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);     // values: the columns are the contiguous axis
             const uint64_t dk = make_desc(0u, 128);
             // an MN-major tile: groups of eight tokens 1024 bytes apart, the next 64 columns an atom's 16 KB further on
             const uint64_t dv = (uint64_t)(kAtom >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
             const auto at = [](uint32_t a) { return (uint64_t)((a & 0x3FFFFu) >> 4); };
-            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return mbar_wait(smem_u32(bar), parity, abortp, g.a.status, where, kWait); };
+            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return bounded_wait(bar, parity, abortp, g.a.status, where); };
             const auto scores = [&](int tl, int buf) {
                 const uint64_t a = dk + at(q_s + (uint32_t)tl * S::kTile), b = dk + at(k_s + (uint32_t)buf * S::kTile);
 #pragma unroll
@@ -382,100 +487,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             // nothing of what was issued is to run on behind this CTA, also when somebody gave up (bounded)
             mma_commit(smem_u32(&drained));
             const unsigned long long t0 = global_timer_ns();
-            while (!mbar_try_wait(smem_u32(&drained), 0u)) if (global_timer_ns() - t0 > kWait) break;
+            while (!mbar_try_wait(smem_u32(&drained), 0u)) if (global_timer_ns() - t0 > kPromptWait) break;
         }
-        __syncwarp();
-    }
-
-    // ---------------- out ----------------
-    __syncthreads();                                                      // (every NaN of the steps at the edges has been noted)
-    const long long place = unit * c.heads + head;
-    constexpr int kPart = kPromptRows * (D + 2);
-    const auto store = [&](int rr, int i, const float (&v)[4]) {
-        const int tt = (view.h0 + rr) / g.group;
-        store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
-    };
-    if (warp < 8 && tile < tiles) {
-        if (steps > 0 && fine) fine = __all_sync(0xffffffffu, mbar_wait(smem_u32(&o_done[tile]), (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u, kWait));
-        tc_fence_after();
-        if (fine) {
-            const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
-            const int pos = view.before + row_t;
-            // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
-            const float unit_o = ref * 0.0078125f * (active == 1 ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
-            float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
-#pragma unroll 1
-            for (int h = 0; h < D; h += 32) {
-                uint32_t v[32];
-                if (steps > 0) {
-                    tmem_ld32(o_t + (uint32_t)h, v);
-                    tmem_wait_ld();
-                }
-                if (mine) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        float x[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            x[e] = steps > 0 && sum != 0.f ? __uint_as_float(v[j + e]) * unit_o : 0.f;
-                            const int col = h + j + e;
-                            if (nan_first[col] <= pos || (g.a.window > 0 && nan_last[col] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
-                        }
-                        if (active == 1) store(r, h + j, x);
-                        else *reinterpret_cast<float4*>(left + h + j) = make_float4(x[0], x[1], x[2], x[3]);
-                    }
-                }
-                __syncwarp();
-            }
-            if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, sum);
+        if (warp == 12) {
+            __syncwarp();
+            named_sync(2, 288);
+            tc_fence_after();
+            tmem_dealloc(tmem, 512u);
         }
     }
-    tc_fence_before();
-    if (active > 1) __threadfence();
-    __syncthreads();
-    if (warp == 12) {
-        __syncwarp();
-        tc_fence_after();
-        tmem_dealloc(tmem, 512u);
-    }
-    if (active == 1) return;
-
-    // ---------------- the splits together, by the last CTA of the tile ----------------
-    if (threadIdx.x == 0) last_one = atomicAdd(g.counters + place, 1u) == (unsigned)active - 1u;
-    __syncthreads();
-    if (!last_one) return;
-    __threadfence();
-    const float* parts = g.partial + place * g.splits * kPart;
-    float* share = reinterpret_cast<float*>(smem_raw);                   // [split][row]
-    if ((int)threadIdx.x < view.rows) {
-        const int rr = threadIdx.x;
-        float mx = -INFINITY, l = 0.f;
-        for (int z = 0; z < active; ++z) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * rr));
-            if (ml.y != 0.f) mx = fmaxf(mx, ml.x);
-        }
-        for (int z = 0; z < active; ++z) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * rr));
-            const float k = ml.y != 0.f ? exp2_fast(ml.x - mx) : 0.f;
-            if (ml.y != 0.f) l += ml.y * k;
-            share[z * kPromptRows + rr] = k;
-        }
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-        for (int z = 0; z < active; ++z) share[z * kPromptRows + rr] *= inv;
-    }
-    __syncthreads();
-    for (int e = threadIdx.x; e < view.rows * (D / 4); e += kPromptThreads) {
-        const int rr = e / (D / 4), i = 4 * (e - rr * (D / 4));
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-        for (int z = 0; z < active; ++z) {
-            const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (long long)rr * D + i));
-            const float w = share[z * kPromptRows + rr];
-            v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
-        }
-        store(rr, i, v);
-    }
-    if (threadIdx.x == 0) g.counters[place] = 0u;                       // ready for the next call
 }
 
 bool prompt_built_for(int d) { return d == 64 || d == 128; }
