@@ -36,16 +36,37 @@ __device__ __forceinline__ void mma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uin
 }
 __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]));
+}
+// 32 columns from here on.
+__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+                   "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+                   "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]));
+}
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float m;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
 }
 __device__ __forceinline__ void tmem_ld8u(uint32_t taddr, uint32_t* v) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ uint2 ld_once(const void* p) {                          // (read by this CTA once)
-    uint2 v;
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
-    return v;
+// N bytes to shared memory, or N zeros.
+template <int N>
+__device__ __forceinline__ void copy_async_or_zero(uint32_t dst, const void* src, bool copy) {
+    const int bytes = copy ? N : 0;
+    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(N) : "memory");
 }
 // Registers of a warpgroup from here on.  512 threads begin with 128 each (65536): 184 for the softmax's
 // two, 96 and 40 for the others make 64512.
@@ -75,13 +96,13 @@ __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("
 __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // What the softmax needs to know of a step's eight groups of 16 tokens.
-struct StepScales { float key[8], shift[8], back[8]; float ref; };
+struct alignas(16) StepScales { float key[8], shift[8], back[8]; float ref; };
 
 template <int D>
 struct PromptShape {
     static constexpr int kAtoms = D / 64;
     static constexpr uint32_t kTile = kAtoms * kAtom;                    // bytes of 128 rows of queries, keys or values
-    static constexpr uint32_t kBytes = 1024u + 6u * kTile;               // two of each
+    static constexpr uint32_t kBytes = 1024u + 7u * kTile;               // two of each, and the bytes of the next keys and values
     static constexpr uint32_t kScores = 0, kOut = 256;                   // columns of tensor memory: S (and P) of both tiles, O of both
 };
 
@@ -89,7 +110,7 @@ template <int D>
 __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(const __grid_constant__ Attend g) {
     typedef PromptShape<D> S;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2], o_done[2], drained;
+    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2], drained;
     __shared__ StepScales scales[4];
     __shared__ int nan_first[D], nan_last[D];
     __shared__ uint32_t tmem_slot;
@@ -117,7 +138,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&k_full[i]), 4u); mbar_init(smem_u32(&v_full[i]), 4u);
             mbar_init(smem_u32(&k_empty[i]), 1u); mbar_init(smem_u32(&v_empty[i]), 1u);
-            mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i]), 4u); mbar_init(smem_u32(&o_done[i]), 1u);
+            mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i][0]), 4u); mbar_init(smem_u32(&p_ready[i][1]), 4u); mbar_init(smem_u32(&o_done[i]), 1u);
         }
         mbar_init(smem_u32(&drained), 1u);
         abort_flag = 0;
@@ -165,7 +186,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         for (int i = 0; i < D; i += 4) {
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (mine) load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
-            const uint32_t to_ = line + (uint32_t)(i >> 6) * kAtom + ((((uint32_t)(i & 63) >> 3) ^ (uint32_t)(lr & 7)) << 4) + (uint32_t)(i & 4) * 2u;
+            const uint32_t to_ = line + (uint32_t)(i / 8 % S::kAtoms) * kAtom + (((uint32_t)(i / (8 * S::kAtoms)) ^ (uint32_t)(lr & 7)) << 4) + (uint32_t)(i & 4) * 2u;
             st_shared_u32(to_, down2<TT_TYPE_F16>(v[0] * up, v[1] * up));
             st_shared_u32(to_ + 4u, down2<TT_TYPE_F16>(v[2] * up, v[3] * up));
         }
@@ -174,18 +195,17 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         if (lane == 0) mbar_arrive(smem_u32(&q_full));
 
         // ---------------- softmax ----------------
+        const int row_pos = view.before + row_t;                          // the row sees tokens row_lo .. row_hi - 1
+        const int row_hi = g.a.causal ? min(view.hi, row_pos + 1) : view.hi, row_lo = g.a.window > 0 ? row_pos + 1 - g.a.window : 0;
         if (tile < tiles) {
             const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
             const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
-            const int pos = view.before + row_t;
-            const int row_hi = g.a.causal ? min(view.hi, pos + 1) : view.hi, row_lo = g.a.window > 0 ? pos + 1 - g.a.window : 0;
             for (int i = 0; i < steps; ++i) {
                 if (!__all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u))) { fine = false; break; }
                 tc_fence_after();
                 const int t = from + i * kPromptTokens;
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
                 const int j_lo = row_lo - t, j_hi = row_hi - t;           // the row sees columns j_lo .. j_hi - 1
-                const StepScales& sc = scales[i & 3];
                 uint32_t v[128];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) tmem_ld32(s_t + 32u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
@@ -194,21 +214,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 #pragma unroll
                     for (int k = 0; k < 128; ++k) v[k] = k >= j_lo && k < j_hi ? v[k] : 0xff800000u;      // (-inf)
                 }
-                float mx = top;
+                float key[8], shift[8], back[8];
+                const uint32_t info = smem_u32(&scales[i & 3]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float4 a = ld_shared_v4f(info + 16u * h), b = ld_shared_v4f(info + 32u + 16u * h), d = ld_shared_v4f(info + 64u + 16u * h);
+                    key[4 * h] = a.x; key[4 * h + 1] = a.y; key[4 * h + 2] = a.z; key[4 * h + 3] = a.w;
+                    shift[4 * h] = b.x; shift[4 * h + 1] = b.y; shift[4 * h + 2] = b.z; shift[4 * h + 3] = b.w;
+                    back[4 * h] = d.x; back[4 * h + 1] = d.y; back[4 * h + 2] = d.z; back[4 * h + 3] = d.w;
+                }
+                float mx = top, m[8];
+#pragma unroll
+                for (int gr = 0; gr < 8; ++gr) m[gr] = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
+#pragma unroll
+                for (int k = 2; k < 16; k += 2)
+#pragma unroll
+                    for (int gr = 0; gr < 8; ++gr) m[gr] = max_of(m[gr], __uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1]));
 #pragma unroll
                 for (int gr = 0; gr < 8; ++gr) {
-                    float m = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
-#pragma unroll
-                    for (int k = 2; k < 16; k += 2) m = fmaxf(fmaxf(m, __uint_as_float(v[16 * gr + k])), __uint_as_float(v[16 * gr + k + 1]));
-                    mx = m == -INFINITY ? mx : fmaxf(mx, m * (factor * sc.key[gr]));
+                    // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
+                    key[gr] = fmaxf(factor * key[gr], 1.17549435e-38f);
+                    mx = fmaxf(mx, m[gr] * key[gr]);
                 }
+                const float seen = top;
                 top = mx;
                 // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
-                const float new_ref = sc.ref;
-                const bool move = top > used + 8.f || (i == 0 || sum == 0.f ? top != used : false) || ref != new_ref;
+                const float new_ref = ld_shared_f32(info + 96u);
+                const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
+                const bool move = top > used + 8.f || first || ref != new_ref;
                 if (__any_sync(0xffffffffu, move)) {
                     const float now = top == -INFINITY ? 0.f : top;
-                    const float alpha = sum != 0.f ? exp2_fast(used - now) : 0.f;
+                    const float alpha = seen != -INFINITY ? exp2_fast(used - now) : 0.f;
                     const float scale_o = ref == new_ref ? alpha : alpha * __fdividef(ref, new_ref);
                     used = now;
                     sum *= alpha;
@@ -229,27 +265,37 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                         }
                     }
                 }
+                // exponentials of a group while the sums and the conversion of the one before are under way
+                float2 e[2][8];
+                uint32_t p[32];
 #pragma unroll
-                for (int gr = 0; gr < 8; ++gr) {
-                    // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
-                    const float f = fmaxf(factor * sc.key[gr], 1.17549435e-38f), add = sc.shift[gr] - used;
-                    float2 part = make_float2(0.f, 0.f);
-                    uint32_t p[8];
+                for (int gr = 0; gr < 9; ++gr) {
+                    if (gr < 8) {
+                        const float f = key[gr], add = shift[gr] - used;
 #pragma unroll
-                    for (int k = 0; k < 16; k += 2) {
-                        float2 e = fma_pair(make_float2(__uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1])), make_float2(f, f), make_float2(add, add));
-                        e.x = exp2_fast(e.x);
-                        e.y = exp2_fast(e.y);
-                        part = fma_pair(e, make_float2(1.f, 1.f), part);
-                        p[k >> 1] = down2<TT_TYPE_F16>(e.x, e.y);
+                        for (int k = 0; k < 8; ++k)
+                            e[gr & 1][k] = fma_pair(make_float2(__uint_as_float(v[16 * gr + 2 * k]), __uint_as_float(v[16 * gr + 2 * k + 1])), make_float2(f, f), make_float2(add, add));
                     }
-                    sum = fmaf(part.x + part.y, sc.back[gr], sum);
-                    tmem_st8u(s_t + 8u * gr, p);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (gr < 8) { e[gr & 1][k].x = exp2_fast(e[gr & 1][k].x); e[gr & 1][k].y = exp2_fast(e[gr & 1][k].y); }
+                        if (gr > 0) p[8 * ((gr - 1) & 3) + k] = down2<TT_TYPE_F16>(e[(gr - 1) & 1][k].x, e[(gr - 1) & 1][k].y);
+                    }
+                    if (gr > 0) {
+                        float2 (&d)[8] = e[(gr - 1) & 1];
+                        const float2 a = add_pair(add_pair(add_pair(d[0], d[1]), add_pair(d[2], d[3])), add_pair(add_pair(d[4], d[5]), add_pair(d[6], d[7])));
+                        sum = fmaf(a.x + a.y, back[gr - 1], sum);
+                    }
+                    if (gr == 4 || gr == 8) {
+                        constexpr int kHalf[9] = {0, 0, 0, 0, 0, 0, 0, 0, 1};
+                        const int h = kHalf[gr];
+                        tmem_st32u(s_t + 32u * h, p);
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile][h]));
+                    }
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile]));
             }
         }
         // ---------------- out ----------------
@@ -265,9 +311,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             tc_fence_after();
             if (fine) {
                 const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
-                const int pos = view.before + row_t;
+                const int pos = row_pos;
+                const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
                 // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
-                const float unit_o = ref * 0.0078125f * (active == 1 ? (sum != 0.f ? 1.f / sum : 0.f) : 1.f);
+                const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
                 float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
 #pragma unroll 1
                 for (int h = 0; h < D; h += 32) {
@@ -279,20 +326,20 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     if (mine) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
+                            const int n = h + j, first = n % 64 / 8 * 8 * S::kAtoms + n / 64 * 8 + n % 8;      // the place of column n in the head
                             float x[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
-                                x[e] = steps > 0 && sum != 0.f ? __uint_as_float(v[j + e]) * unit_o : 0.f;
-                                const int col = h + j + e;
-                                if (nan_first[col] <= pos || (g.a.window > 0 && nan_last[col] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
+                                x[e] = none ? 0.f : __uint_as_float(v[j + e]) * unit_o;
+                                if (nan_first[first + e] <= pos || (g.a.window > 0 && nan_last[first + e] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
                             }
-                            if (active == 1) store(r, h + j, x);
-                            else *reinterpret_cast<float4*>(left + h + j) = make_float4(x[0], x[1], x[2], x[3]);
+                            if (active == 1) store(r, first, x);
+                            else *reinterpret_cast<float4*>(left + first) = make_float4(x[0], x[1], x[2], x[3]);
                         }
                     }
                     __syncwarp();
                 }
-                if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, sum);
+                if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, none ? 0.f : sum);
             }
         }
         tc_fence_before();
@@ -340,103 +387,125 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     } else if (warp < 12) {
         registers_down<96>();
         // ---------------- keys and values: pages -> operand tiles ----------------
-        // Eight lanes have a token, eight values of each 64 of it (a 16-byte chunk of an operand's line: all banks at once); the four warps take the
-        // 16 tokens of a group at a time.
+        // Eight lanes have a token; the four warps take the 16 tokens of a group at a time.  A lane copies kPiece values a step ahead into a place of
+        // its own, and turns them into one 16-byte chunk of each atom's line (all banks at once): value kPiece * lane + 8 a + e of a head is
+        // value e of chunk `lane` of atom a, and the queries and the outputs are ordered alike.
+        constexpr int kPiece = 8 * S::kAtoms;
         const int dt = (int)threadIdx.x - 256, piece = dt & 7, sub = dt >> 3;
-        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + sub * c.token[0] + 8 * piece;
-        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + sub * c.token[1] + 8 * piece;
+        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + sub * c.token[0] + kPiece * piece;
+        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + sub * c.token[1] + kPiece * piece;
         const int* table = c.table + view.b * c.table_row;
         const int shift = 31 - __clz(c.block);
-        float most = 0.f;                                                 // the largest scale of values so far
+        const uint32_t raw = base + 6u * S::kTile + (uint32_t)(dt * kPiece);                     // (keys; the values' behind them)
+        constexpr uint32_t kGroup = 128u * kPiece;                                               // bytes of a group of 16 tokens there
         const uint32_t chunk = (uint32_t)sub * 128u + ((((uint32_t)piece) ^ ((uint32_t)sub & 7u)) << 4);
-        const auto put = [&](uint32_t tile_s, int group, int atom, const uint2& raw) {
-            uint32_t h[4];
-            f16_pairs_of_e4m3(raw.x, h[0], h[1]);
-            f16_pairs_of_e4m3(raw.y, h[2], h[3]);
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(tile_s + chunk + (uint32_t)atom * kAtom + (uint32_t)group * 2048u), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+        const auto put = [&](uint32_t tile_s, int group, const uint32_t (&w)[kPiece / 4]) {
+#pragma unroll
+            for (int a = 0; a < S::kAtoms; ++a) {
+                uint32_t h[4];
+                f16_pairs_of_e4m3(w[2 * a], h[0], h[1]);
+                f16_pairs_of_e4m3(w[2 * a + 1], h[2], h[3]);
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(tile_s + chunk + (uint32_t)a * kAtom + (uint32_t)group * 2048u), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+            }
         };
-        // lane g of the first eight has the page of the next step's group g
-        const auto page_of = [&](int i) {
-            const int t = from + i * kPromptTokens + 16 * (lane & 7);
-            return i < steps && t + 15 >= view.lo && t < to ? table[t >> shift] : -1;
-        };
-        int page = page_of(0);
-        for (int i = 0; i < steps; ++i) {
-            const int t = from + i * kPromptTokens, buf = i & 1;
-            const int group_t = t + 16 * (lane & 7);
-            const bool held = group_t + 15 >= view.lo && group_t < to;
-            const bool good = held && (unsigned)page < (unsigned)c.pages;
-            if (held && !good) report_invalid(g.a.status);
-            const float ks = good ? c.scale[0][page * c.s_page[0] + head * c.s_head[0]] : 0.f, vs = good ? c.scale[1][page * c.s_page[1] + head * c.s_head[1]] : 0.f;
-            const int pages = good ? page : -1;
-            page = page_of(i + 1);
-            uint2 kr[8][S::kAtoms], vr[8][S::kAtoms];
-            const auto fetch = [&](const uint8_t* data, int w, uint2 (&to_)[8][S::kAtoms]) {
+        const auto fetch = [&](int i, int pages, const uint8_t* data, int w) {
+            const int t = from + i * kPromptTokens;
+            if (i < steps) {
 #pragma unroll
                 for (int p = 0; p < 8; ++p) {
                     const int pg = __shfl_sync(0xffffffffu, pages, p), first = t + 16 * p, tok = first + sub;
-                    const uint8_t* at = data + pg * c.page[w] + (first & (c.block - 1)) * c.token[w];
-                    const bool any = pg >= 0 && tok >= view.lo && tok < to;
-#pragma unroll
-                    for (int a = 0; a < S::kAtoms; ++a) to_[p][a] = any ? ld_once(at + 64 * a) : make_uint2(0u, 0u);
+                    const bool any = pg >= 0 && tok >= view.lo && tok < to;                      // (else zeros)
+                    const uint8_t* at = any ? data + (pg * c.page[w] + (first & (c.block - 1)) * c.token[w]) : data;
+                    copy_async_or_zero<kPiece>(raw + (uint32_t)w * 8u * kGroup + (uint32_t)p * kGroup, at, any);
                 }
-            };
-            fetch(keys, 0, kr);
-            fetch(vals, 1, vr);
-            // the scales, before the keys report: two steps back everybody has read what lies here
+            }
+            cp_async_commit();
+        };
+        // lane g of the first eight has the page of a step's group g, and its scales
+        const auto page_of = [&](int i) {
+            const int t = from + i * kPromptTokens + 16 * (lane & 7);
+            if (i >= steps || t + 15 < view.lo || t >= to) return -1;
+            const int pg = table[t >> shift];
+            if ((unsigned)pg < (unsigned)c.pages) return pg;
+            report_invalid(g.a.status);
+            return -1;
+        };
+        const auto scale_of = [&](int pg, int w) { return pg >= 0 ? c.scale[w][pg * c.s_page[w] + head * c.s_head[w]] : 0.f; };
+        float most = 0.f;                                                 // the largest scale of values so far
+        int page = page_of(0), page1 = page_of(1);
+        float ks = scale_of(page, 0), vs = scale_of(page, 1);
+        fetch(0, page, keys, 0);
+        fetch(0, page, vals, 1);
+        for (int i = 0; i < steps; ++i) {
+            const int t = from + i * kPromptTokens, buf = i & 1;
+            const int page2 = page_of(i + 2);
+            const float ks1 = scale_of(page1, 0), vs1 = scale_of(page1, 1);
+            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u))) break;
             if (warp == 8) {
+                // the scales, before the keys report: what lay here four steps ago has been read
                 float m = vs;
 #pragma unroll
                 for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 most = fmaxf(most, m);
+                if (lane < 8) {
+                    StepScales& sc = scales[i & 3];
+                    // (a share of less than 2^-40 of the largest scale is taken as that)
+                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
+                    sc.key[lane] = ks;
+                    sc.shift[lane] = lg + 7.f;
+                    sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
+                    if (lane == 0) sc.ref = most;
+                }
             }
-            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u))) break;
-            if (warp == 8 && lane < 8) {
-                StepScales& sc = scales[i & 3];
-                // (a share of less than 2^-40 of the largest scale is taken as that)
-                const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
-                sc.key[lane] = ks;
-                sc.shift[lane] = lg + 7.f;
-                sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
-                if (lane == 0) sc.ref = most;
+            cp_async_wait<1>();
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                uint32_t w[kPiece / 4];
+                read_shared<kPiece>(raw + (uint32_t)p * kGroup, w);
+                put(k_s + (uint32_t)buf * S::kTile, p, w);
             }
-#pragma unroll
-            for (int p = 0; p < 8; ++p)
-#pragma unroll
-                for (int a = 0; a < S::kAtoms; ++a) put(k_s + (uint32_t)buf * S::kTile, p, a, kr[p][a]);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
+            fetch(i + 1, page1, keys, 0);
+            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u))) break;
+            cp_async_wait<1>();
             const bool low = t < view.whole_lo, high = g.a.causal && t + kPromptTokens > view.whole_hi;
             if (low || high) {
+#pragma unroll 1
+                for (int p = 0; p < 8; ++p) {
+                    uint32_t w[kPiece / 4];
+                    read_shared<kPiece>(raw + (uint32_t)(8 + p) * kGroup, w);
 #pragma unroll
-                for (int p = 0; p < 8; ++p)
-#pragma unroll
-                    for (int a = 0; a < S::kAtoms; ++a) {
-                        uint32_t w[2] = {vr[p][a].x, vr[p][a].y};
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            const uint32_t n = nan_bytes(w[q]);
-                            if (n == 0u) continue;
-                            for (int e = 0; e < 4; ++e)
-                                if ((n >> (8 * e)) & 0x80u) {
-                                    if (high) atomicMin(&nan_first[64 * a + 8 * piece + 4 * q + e], t + 16 * p + sub);
-                                    else atomicMax(&nan_last[64 * a + 8 * piece + 4 * q + e], t + 16 * p + sub);
-                                }
-                            w[q] &= ~((n >> 7) * 0xffu);
-                        }
-                        vr[p][a] = make_uint2(w[0], w[1]);
+                    for (int q = 0; q < kPiece / 4; ++q) {
+                        const uint32_t n = nan_bytes(w[q]);
+                        if (n == 0u) continue;
+                        for (int e = 0; e < 4; ++e)
+                            if ((n >> (8 * e)) & 0x80u) {
+                                if (high) atomicMin(&nan_first[kPiece * piece + 4 * q + e], t + 16 * p + sub);
+                                else atomicMax(&nan_last[kPiece * piece + 4 * q + e], t + 16 * p + sub);
+                            }
+                        w[q] &= ~((n >> 7) * 0xffu);
                     }
+                    put(v_s + (uint32_t)buf * S::kTile, p, w);
+                }
+            } else {
+#pragma unroll
+                for (int p = 0; p < 8; ++p) {
+                    uint32_t w[kPiece / 4];
+                    read_shared<kPiece>(raw + (uint32_t)(8 + p) * kGroup, w);
+                    put(v_s + (uint32_t)buf * S::kTile, p, w);
+                }
             }
-            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u))) break;
-#pragma unroll
-            for (int p = 0; p < 8; ++p)
-#pragma unroll
-                for (int a = 0; a < S::kAtoms; ++a) put(v_s + (uint32_t)buf * S::kTile, p, a, vr[p][a]);
             fence_proxy_async_shared();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&v_full[buf]));
+            fetch(i + 1, page1, vals, 1);
+            page1 = page2;
+            ks = ks1;
+            vs = vs1;
         }
+        cp_async_wait<0>();
         named_arrive(1, 384);
     } else {
         registers_down<40>();
@@ -465,12 +534,19 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             for (int i = 0; i < steps && ok; ++i) {
                 const int buf = i & 1, next = (i + 1) & 1;
                 for (int tl = 0; tl < tiles && ok; ++tl) {
-                    ok = wait(&p_ready[tl], (uint32_t)i & 1u, 37u) && (tl > 0 || wait(&v_full[buf], (uint32_t)(i >> 1) & 1u, 38u));
+                    // (the first half of P is multiplied while the second is being written)
+                    ok = (tl > 0 || wait(&v_full[buf], (uint32_t)(i >> 1) & 1u, 38u)) && wait(&p_ready[tl][0], (uint32_t)i & 1u, 37u);
                     if (!ok) break;
                     tc_fence_after();
                     const uint64_t b = dv + at(v_s + (uint32_t)buf * S::kTile);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
+                    for (int k = 0; k < 4; ++k)
+                        mma_f16_ta(tmem + S::kOut + (uint32_t)(tl * D), tmem + S::kScores + (uint32_t)(tl * 128 + 8 * k), b + (uint64_t)(128 * k), kIdescO, i > 0 || k > 0 ? 1u : 0u);
+                    ok = wait(&p_ready[tl][1], (uint32_t)i & 1u, 37u);
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 4; k < 8; ++k)
                         mma_f16_ta(tmem + S::kOut + (uint32_t)(tl * D), tmem + S::kScores + (uint32_t)(tl * 128 + 8 * k), b + (uint64_t)(128 * k), kIdescO, i > 0 || k > 0 ? 1u : 0u);
                     mma_commit(smem_u32(&o_done[tl]));
                     if (tl == tiles - 1) mma_commit(smem_u32(&v_empty[buf]));
