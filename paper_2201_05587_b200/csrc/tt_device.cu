@@ -198,6 +198,19 @@ private:
 
 }  // namespace
 
+// An output matrix [rows][cols] of 32 or 16 bits, rows `pitch` elements apart, in blocks of 32 rows x box_cols (64 or 128 bytes, swizzled).
+tt_status encode_output(void* out, void* base, int bytes, long long cols, long long rows, long long pitch, int box_cols) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return TT_ERR_CUDA;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)(pitch * bytes)};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, 32};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = fn(reinterpret_cast<CUtensorMap*>(out), bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, base, dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, box_cols * bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? TT_OK : TT_ERR_CUDA;
+}
 // A matrix of bytes [rows][cols], rows `pitch` bytes apart -> 2-D tensor map, box = [128, box_rows], 128-byte swizzle: K-major tiles of 8-bit
 // operands.
 tt_status encode_bytes(void* out, const void* base, long long cols, long long rows, long long pitch, int box_rows) {

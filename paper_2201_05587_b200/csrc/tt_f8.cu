@@ -122,6 +122,7 @@ struct DenseF8 {
     unsigned* status;
     int rows_a, rows_b, blocks, blocks_per_split, split, stages, tiles_a;
     int y_type, act, wide;
+    int tiles;                                              // pairs: of 256 x TN
     unsigned idesc;
     unsigned long long wait_ns;
 };
@@ -150,6 +151,13 @@ __device__ __forceinline__ float4 ld_cluster_v4f(uint32_t addr) {
     float4 v;
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
     return v;
+}
+
+// apply_act, but for NaN, which stays NaN (a NaN operand is to show).
+__device__ __forceinline__ float activate(float v, int act) {
+    if (act == TT_ACT_GELU_ERF) return gelu_erf(v);
+    if (act != TT_ACT_NONE) v = v < 0.f ? 0.f : v;
+    return act == TT_ACT_RELU6 && v > 6.f ? 6.f : v;
 }
 
 template <int TN, bool SWAP>
@@ -287,14 +295,14 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                     const float b = g.bias ? __ldg(g.bias + row) : 0.f;
 #pragma unroll
                     for (int j = 0; j < kCols; ++j)
-                        if (first_col + j < g.rows_b) store_one(g.y, (long long)(first_col + j) * g.y_row + row, g.y_type, apply_act(acc[j] + b, g.act));
+                        if (first_col + j < g.rows_b) store_one(g.y, (long long)(first_col + j) * g.y_row + row, g.y_type, activate(acc[j] + b, g.act));
                 }
             } else if (row < g.rows_a) {
                 const long long at = (long long)row * g.y_row + first_col;
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) {
                     const float b = g.bias && first_col + j < g.rows_b ? __ldg(g.bias + first_col + j) : 0.f;
-                    acc[j] = apply_act(acc[j] + b, g.act);
+                    acc[j] = activate(acc[j] + b, g.act);
                 }
                 if (g.wide && first_col + kCols <= g.rows_b) {
                     if (g.y_type == TT_TYPE_F32) store_wide<TT_TYPE_F32, kCols>(static_cast<float*>(g.y) + at, acc);
@@ -341,7 +349,7 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float b = g.bias && col + i < cols ? __ldg(g.bias + col + i) : 0.f;
-                    v[i] = apply_act(v[i] + b, g.act);
+                    v[i] = activate(v[i] + b, g.act);
                 }
                 if (g.wide && col + 4 <= cols) {
                     if (g.y_type == TT_TYPE_F32) *reinterpret_cast<float4*>(static_cast<float*>(g.y) + at) = make_float4(v[0], v[1], v[2], v[3]);
@@ -365,6 +373,255 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     }
 }
 
+// The same for many tokens: pairs of CTAs walk tiles of 256 x TN persistently.  Each CTA has 128 rows of A and half of B's in shared memory,
+// tcgen05.mma.cta_group::2 reads both CTAs', so an SM takes in (128 + TN / 2) * 128 bytes for 128 * TN * 128 products: 64 bytes a cycle at the tensor
+// core's rate, which is what an SM can get from the L2 (a 128 x 128 tile of one CTA needs twice that).  Two accumulators; the
+// sixteen read-out warps have a quarter of a block's sums each, 4 warps a scheduler, so that one waits for tensor memory while another adds.
+constexpr int kPairThreads = 128 + 512;                    // a warpgroup of TMA and MMA, four of read-out (96 registers each at launch; 32 and 112)
+constexpr unsigned kPairStaging = 16 * 4096;                // a block of 32 rows x 128 bytes for each read-out warp
+constexpr int kPairSmem = 230400;
+
+__device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* tmap, uint32_t bar_cluster, int c0, int c1) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+        ::"r"(dst), "l"(tmap), "r"(bar_cluster), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tmap), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]),
+                   "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr));
+}
+
+// mbar_arrive_remote where no ordinary memory access has to be seen: what is given back is tensor memory, whose loads have been waited for.  (With
+// release semantics the arrival took 1100 to 1800 cycles of the warp.)
+__device__ __forceinline__ void mbar_arrive_remote_relaxed(uint32_t bar, uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+        "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [ra];\n\t}"
+        ::"r"(bar), "r"(rank) : "memory");
+}
+
+template <int TN>
+__global__ void __launch_bounds__(kPairThreads, 1)
+tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_y, const DenseF8 g) {
+    constexpr int kCols = TN / 4;                          // columns of a read-out warp
+    constexpr uint32_t kStage = kF8TileA + TN / 2 * 128u;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[2], acc_empty[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    volatile int* abortp = &abort_flag;
+    pdl_allow_next();
+    const uint32_t rank = cluster_ctarank();
+    const int unit = (int)blockIdx.x / 2, n_units = (int)gridDim.x / 2;
+    const int my_tiles = g.tiles > unit ? (g.tiles - unit + n_units - 1) / n_units : 0;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 32u); }
+        abort_flag = 0;
+        fence_mbar_init();
+        fence_proxy_async_shared();
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                     // the peer's barriers exist before anything arrives on them
+    tc_fence_after();
+    const uint32_t tmem_base = *(volatile uint32_t*)&tmem_slot;
+    pdl_wait_prev();
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == 0 && elect_one()) {
+            int st = 0;
+            uint32_t ph = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (int i = 0; i < my_tiles && ok; ++i) {
+                const int t = unit + i * n_units, tm = t % g.tiles_a, tn = t / g.tiles_a;
+                const int a0 = (2 * tm + (int)rank) * 128, b0 = tn * TN + (int)rank * (TN / 2);
+                for (int kb = 0; kb < g.blocks; ++kb) {
+                    ok = bounded_wait(&empty_bar[st], ph ^ 1u, abortp, g.status, 1u, g.wait_ns);
+                    if (!ok) break;
+                    const uint32_t dst = base + (uint32_t)st * kStage;
+                    if (rank == 0) mbar_expect_tx(smem_u32(&full_bar[st]), 2u * kStage);
+                    const uint32_t bar = map_to_peer(smem_u32(&full_bar[st]), 0u);       // the pair's loads all report to rank 0
+                    tma_load_2d_pair(dst, &tmap_a, bar, kb * 128, a0);
+                    tma_load_2d_pair(dst + kF8TileA, &tmap_b, bar, kb * 128, b0);
+                    ++issued;
+                    if (++st == g.stages) { st = 0; ph ^= 1u; }
+                }
+            }
+            if (!ok || *abortp) {
+                // let copies in flight land before shared memory is given back (bounded); the other CTA's report to rank 0, it gives them time
+                const unsigned long long t0 = global_timer_ns();
+                if (rank == 0) {
+                    for (long long it = issued > g.stages ? issued - g.stages : 0; it < issued; ++it)
+                        while (!mbar_try_wait(smem_u32(&full_bar[it % g.stages]), (uint32_t)(it / g.stages) & 1u)) if (global_timer_ns() - t0 > 2000000ull) break;
+                } else {
+                    while (global_timer_ns() - t0 < 2000000ull) { }
+                }
+            }
+        }
+        if (warp == 1 && rank == 0 && elect_one()) {
+            const uint64_t d0 = make_desc(0u, 128);
+            int st = 0, buf = 0;
+            uint32_t ph = 0, aph = 0;
+            bool ok = true;
+            for (int i = 0; i < my_tiles && ok; ++i)
+                for (int kb = 0; kb < g.blocks; ++kb) {
+                    ok = bounded_wait<true>(&acc_empty[buf], aph ^ 1u, abortp, g.status, 2u, g.wait_ns) &&
+                         bounded_wait(&full_bar[st], ph, abortp, g.status, 3u, g.wait_ns);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t a = base + (uint32_t)st * kStage, b = a + kF8TileA;
+                    const uint64_t da = d0 + (uint64_t)((a & 0x3FFFFu) >> 4), db = d0 + (uint64_t)((b & 0x3FFFFu) >> 4);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem_base + (uint32_t)(buf * TN), da + 2u * k, db + 2u * k, g.idesc, k > 0 ? 1u : 0u);
+                    mma_commit_cg<2>(smem_u32(&empty_bar[st]));
+                    mma_commit_cg<2>(smem_u32(&acc_full[buf]));
+                    if (++st == g.stages) { st = 0; ph ^= 1u; }
+                    if (++buf == 2) { buf = 0; aph ^= 1u; }
+                }
+        }
+        __syncwarp();
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
+        const int quad = warp & 3, c0 = ((warp - 4) >> 2) * kCols;
+        const uint32_t staging = base + (uint32_t)g.stages * kStage + (uint32_t)(warp - 4) * 4096u;
+        const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)c0;
+        int buf = 0;
+        uint32_t aph = 0;
+        bool ok = true;
+        for (int i = 0; i < my_tiles; ++i) {
+            const int t = unit + i * n_units, tm = t % g.tiles_a, tn = t / g.tiles_a;
+            const int row0 = (2 * tm + (int)rank) * 128 + quad * 32, col0 = tn * TN + c0;
+            const float* as = g.a_scale + (long long)min(row0 + lane, g.rows_a - 1) * g.as_row;
+            const float* bs = g.b_scale + (long long)(min(col0, g.rows_b - 1) >> 7) * g.bs_row;
+            float acc[kCols];
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) acc[j] = 0.f;
+            float sa = __ldg(as), sb = __ldg(bs);
+            for (int kb = 0; kb < g.blocks; ++kb) {
+                const float s = sa * sb;
+                if (kb + 1 < g.blocks) { sa = __ldg(as + (kb + 1) * g.as_block); sb = __ldg(bs + (kb + 1) * g.bs_block); }
+                ok = ok && __all_sync(0xffffffffu, bounded_wait(&acc_full[buf], aph, abortp, g.status, 4u, g.wait_ns));
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t at = lanes + (uint32_t)(buf * TN);
+                uint32_t r[2][16];
+                tmem_ld16(at, r[0]);
+#pragma unroll
+                for (int j = 0; j < kCols / 16; ++j) {
+                    tmem_wait_ld();
+                    if (j + 1 < kCols / 16) tmem_ld16(at + 16u * (j + 1), r[(j + 1) & 1]);
+                    else {
+                        // (the accumulator is free again)
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&acc_empty[buf]), 0u);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; k += 2) {
+                        const float2 f = fma_pair(make_float2(__uint_as_float(r[j & 1][k]), __uint_as_float(r[j & 1][k + 1])), make_float2(s, s), make_float2(acc[16 * j + k], acc[16 * j + k + 1]));
+                        acc[16 * j + k] = f.x;
+                        acc[16 * j + k + 1] = f.y;
+                    }
+                }
+                if (++buf == 2) { buf = 0; aph ^= 1u; }
+            }
+            if (!ok) break;
+            if (g.bias) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[j] += __ldg(g.bias + min(col0 + j, g.rows_b - 1));
+            }
+            if (g.act == TT_ACT_GELU_ERF) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[j] = gelu_erf(acc[j]);
+            } else if (g.act != TT_ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) acc[j] = activate(acc[j], g.act);
+            }
+            // Blocks of 32 rows through shared memory, swizzled as the tensor map has it, and out by TMA; where rows are no multiples of 16 bytes, a
+            // row at a time (a lane's own row would be 32 places at once).
+            const int per = g.y_type == TT_TYPE_F32 ? 32 : kCols;           // columns of a block: 128 bytes of them, or 64 (kCols 32 in 16 bits)
+#pragma unroll
+            for (int part = 0; part < kCols / 32; ++part) {
+                if (part > 0 && g.y_type != TT_TYPE_F32) break;
+                const int col = col0 + part * per;
+                if (lane == 0) bulk_stores_pending<0>();
+                __syncwarp();
+                if (g.y_type == TT_TYPE_F32) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4)
+                        st_shared_v4(staging + (uint32_t)lane * 128u + ((uint32_t)((j >> 2) ^ (lane & 7)) << 4), acc[32 * part + j], acc[32 * part + j + 1], acc[32 * part + j + 2], acc[32 * part + j + 3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kCols; j += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = g.y_type == TT_TYPE_F16 ? down2<TT_TYPE_F16>(acc[j + 2 * e], acc[j + 2 * e + 1]) : down2<TT_TYPE_BF16>(acc[j + 2 * e], acc[j + 2 * e + 1]);
+                        const uint32_t x = kCols == 64 ? (uint32_t)(lane & 7) : (uint32_t)((lane >> 1) & 3);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(staging + (uint32_t)lane * (kCols * 2u) + (((uint32_t)(j >> 3) ^ x) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    }
+                }
+                if (g.wide) {
+                    fence_proxy_async_shared();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (row0 < g.rows_a && col < g.rows_b) tma_store_2d(&tmap_y, staging, col, row0);
+                        bulk_stores_commit();
+                    }
+                } else {
+                    __syncwarp();
+                    for (int r = 0; r < 32 && row0 + r < g.rows_a; ++r) {
+                        const long long at = (long long)(row0 + r) * g.y_row + col;
+                        if (g.y_type == TT_TYPE_F32) {
+                            if (col + lane < g.rows_b) static_cast<float*>(g.y)[at + lane] = ld_shared_f32(staging + (uint32_t)r * 128u + ((uint32_t)((lane >> 2) ^ (r & 7)) << 4) + 4u * (uint32_t)(lane & 3));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < kCols; j += 32) {
+                                const uint32_t e = (uint32_t)(lane + j), x = kCols == 64 ? (uint32_t)(r & 7) : (uint32_t)((r >> 1) & 3);
+                                uint16_t v;
+                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staging + (uint32_t)r * (kCols * 2u) + (((e >> 3) ^ x) << 4) + 2u * (e & 7u)) : "memory");
+                                if (col + (int)e < g.rows_b) static_cast<uint16_t*>(g.y)[at + e] = v;
+                            }
+                        }
+                    }
+                    __syncwarp();
+                }
+            }
+        }
+        if (lane == 0) bulk_stores_pending<0>();             // shared memory stays until the last store has read it
+        __syncwarp();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                                     // the pair stays together until neither CTA touches the other
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2u * TN) : "memory");
+    }
+}
+
 template <int TN, bool SWAP>
 static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb, DenseF8 g, void* stream) {
     constexpr int kStageBytes = (int)kF8TileA + TN * 128;
@@ -375,6 +632,39 @@ static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb,
     g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
     const int tiles_b = (g.rows_b + TN - 1) / TN;
     return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes, g.split, stream, ta, tb, g);
+}
+
+// Columns of a pair's tile, or 0 for CTAs on their own: what takes the fewest rounds of the SMs, by what a tile costs.
+static int pair_columns(long long m, long long n) {
+    const long long rows = (m + 255) / 256;
+    const auto rounds = [](long long tiles, long long at_once) { return (tiles + at_once - 1) / at_once; };
+    const long long wide = rounds(rows * ((n + 255) / 256), kSms / 2) * 56, narrow = rounds(rows * ((n + 127) / 128), kSms / 2) * 34;
+    const long long alone = rounds((m + 127) / 128 * ((n + 127) / 128), kSms) * 34;
+    return alone < wide && alone < narrow ? 0 : wide <= narrow ? 256 : 128;
+}
+
+template <int TN>
+static cudaError_t launch_dense_f8_pair(const CUtensorMap& ta, const CUtensorMap& tb, const CUtensorMap& ty, DenseF8 g, void* stream) {
+    constexpr int kStageBytes = (int)kF8TileA + TN / 2 * 128;
+    static OncePerDevice raised;
+    const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_dense_f8_pair_kernel<TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem); });
+    if (ready != cudaSuccess) return ready;
+    const int fits = (kPairSmem - 1024 - (int)kPairStaging) / kStageBytes;
+    g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
+    g.tiles_a = (g.rows_a + 255) / 256;
+    g.tiles = g.tiles_a * ((g.rows_b + TN - 1) / TN);
+    g.idesc = (1u << 4) | ((unsigned)(TN >> 3) << 17) | ((256u >> 4) << 24);
+    const int units = g.tiles < kSms / 2 ? g.tiles : kSms / 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(2u * (unsigned)units, 1, 1); cfg.blockDim = dim3(kPairThreads, 1, 1);
+    cfg.dynamicSmemBytes = kPairSmem; cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, tt_dense_f8_pair_kernel<TN>, ta, tb, ty, g);
 }
 
 }  // namespace tt
@@ -440,5 +730,14 @@ extern "C" tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* 
         return status_of(tn == 16 ? launch_dense_f8<16, true>(tw, tx, g, stream) : tn == 32 ? launch_dense_f8<32, true>(tw, tx, g, stream) : launch_dense_f8<64, true>(tw, tx, g, stream));
     }
     g.a_scale = a->x_scale; g.as_row = a->xs_row; g.as_block = a->xs_block; g.b_scale = a->w_scale; g.bs_row = a->ws_row; g.bs_block = a->ws_block;
+    const int pair_n = g.split > 1 ? 0 : pair_columns(a->m, a->nn);
+    if (pair_n > 0) {
+        CUtensorMap ty{};
+        g.wide = g.wide && a->nn * bytes % 16 == 0;        // (a TMA store clips in pieces of 16 bytes)
+        s = encode_bytes(&tw, a->w, a->kk, a->nn, a->w_row, pair_n / 2);
+        if (s == TT_OK && g.wide) s = encode_output(&ty, a->y, (int)bytes, a->nn, a->m, a->y_row, a->y_type == TT_TYPE_F32 ? 32 : pair_n / 4);
+        if (s != TT_OK) return s;
+        return status_of(pair_n == 256 ? launch_dense_f8_pair<256>(tx, tw, ty, g, stream) : launch_dense_f8_pair<128>(tx, tw, ty, g, stream));
+    }
     return status_of(launch_dense_f8<128, false>(tx, tw, g, stream));
 }

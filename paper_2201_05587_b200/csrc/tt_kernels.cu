@@ -1427,26 +1427,6 @@ __device__ __forceinline__ void mma_tf32_cg(uint32_t d_tmem, uint64_t adesc, uin
             ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
     }
 }
-// Arrive on the barrier at this shared-memory offset once every MMA issued so far has completed: in this CTA (CG 1),
-// or in both CTAs of the pair (CG 2; the arrival is multicast, no data moves).
-template <int CG>
-__device__ __forceinline__ void mma_commit_cg(uint32_t bar) {
-    if constexpr (CG == 1) {
-        mma_commit(bar);
-    } else {
-        const uint16_t mask = 3;
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                     ::"r"(bar), "h"(mask) : "memory");
-    }
-}
-// Arrive on the barrier at the same offset in the CTA of rank `rank` of this cluster.
-__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, uint32_t rank) {
-    asm volatile(
-        "{\n\t.reg .b32 ra;\n\t"
-        "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n\t}"
-        ::"r"(bar), "r"(rank) : "memory");
-}
 // TMA load whose completion is reported to a barrier given by its cluster-wide address, which may lie in the other
 // CTA of the pair (no multicast: the data goes to this CTA's shared memory only).
 __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const void* tmap, uint32_t bar_cluster, int c0, int c1, int c2) {
@@ -1459,10 +1439,6 @@ __device__ __forceinline__ void tma_store_3d(const void* tmap, uint32_t src, int
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(tmap), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
-__device__ __forceinline__ void bulk_stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-// Wait until at most N of the store groups this thread committed have still to read their shared memory.
-template <int N>
-__device__ __forceinline__ void bulk_stores_pending() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
 
 // Instantiated for what a plan uses, so that a launch carries only the code it runs (a single-wave launch meets it cold: 3-6 %
 // on every record of this form, dense 2268 x 2256 -> 3944 76 -> 71 us).  MN: an operand is MN-major (otherwise the descriptors

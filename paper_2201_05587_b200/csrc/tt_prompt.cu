@@ -73,24 +73,6 @@ __device__ __forceinline__ void copy_async_or_zero(uint32_t dst, const void* src
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// mbar_wait without the call of a function (whose registers would be those of the launch, not of the warpgroup).
-__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* status, unsigned where) {
-    const uint32_t b = smem_u32(bar);
-    if (mbar_try_wait(b, parity)) return true;
-    const unsigned long long t0 = global_timer_ns();
-#pragma unroll 1
-    for (unsigned spins = 1; !mbar_try_wait(b, parity); ++spins) {
-        if ((spins & 31u) != 0u) continue;
-        if (*abort_flag) return false;
-        if (global_timer_ns() - t0 > kPromptWait) {
-            *abort_flag = 1;
-            atomicCAS(status, 0u, (unsigned)TT_ERR_TIMEOUT | (where << 8));
-            return false;
-        }
-    }
-    return true;
-}
-
 // Named barriers: 1 the softmax and the warps of keys and values, 2 the softmax and the MMA warp (at the end), 3 the softmax alone.
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
@@ -201,7 +183,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
             const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
             for (int i = 0; i < steps; ++i) {
-                if (!__all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u))) { fine = false; break; }
+                if (!__all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u, kPromptWait))) { fine = false; break; }
                 tc_fence_after();
                 const int t = from + i * kPromptTokens;
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
@@ -250,7 +232,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     sum *= alpha;
                     ref = new_ref;
                     if (i > 0) {
-                        if (!__all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u))) { fine = false; break; }
+                        if (!__all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kPromptWait))) { fine = false; break; }
                         tc_fence_after();
 #pragma unroll 1
                         for (int h = 0; h < D; h += 16) {                 // (few at a time: the scores are in registers)
@@ -307,7 +289,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
         };
         if (tile < tiles) {
-            if (steps > 0 && fine) fine = __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u));
+            if (steps > 0 && fine) fine = __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
             tc_fence_after();
             if (fine) {
                 const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
@@ -440,7 +422,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const int t = from + i * kPromptTokens, buf = i & 1;
             const int page2 = page_of(i + 2);
             const float ks1 = scale_of(page1, 0), vs1 = scale_of(page1, 1);
-            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u))) break;
+            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u, kPromptWait))) break;
             if (warp == 8) {
                 // the scales, before the keys report: what lay here four steps ago has been read
                 float m = vs;
@@ -468,7 +450,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
             fetch(i + 1, page1, keys, 0);
-            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u))) break;
+            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u, kPromptWait))) break;
             cp_async_wait<1>();
             const bool low = t < view.whole_lo, high = g.a.causal && t + kPromptTokens > view.whole_hi;
             if (low || high) {
@@ -517,7 +499,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             // an MN-major tile: groups of eight tokens 1024 bytes apart, the next 64 columns an atom's 16 KB further on
             const uint64_t dv = (uint64_t)(kAtom >> 4) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
             const auto at = [](uint32_t a) { return (uint64_t)((a & 0x3FFFFu) >> 4); };
-            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return bounded_wait(bar, parity, abortp, g.a.status, where); };
+            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return bounded_wait(bar, parity, abortp, g.a.status, where, kPromptWait); };
             const auto scores = [&](int tl, int buf) {
                 const uint64_t a = dk + at(q_s + (uint32_t)tl * S::kTile), b = dk + at(k_s + (uint32_t)buf * S::kTile);
 #pragma unroll

@@ -406,4 +406,52 @@ __device__ __forceinline__ uint32_t cluster_ctarank() {
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
 }
+
+// Arrive on the barrier at this shared-memory offset once every MMA issued so far has completed: in this CTA (CG 1),
+// or in both CTAs of the pair (CG 2; the arrival is multicast, no data moves).
+template <int CG>
+__device__ __forceinline__ void mma_commit_cg(uint32_t bar) {
+    if constexpr (CG == 1) {
+        mma_commit(bar);
+    } else {
+        const uint16_t mask = 3;
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"(mask) : "memory");
+    }
+}
+// Arrive on the barrier at the same offset in the CTA of rank `rank` of this cluster.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n\t}"
+        ::"r"(bar), "r"(rank) : "memory");
+}
+__device__ __forceinline__ void bulk_stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+// Wait until at most N of the store groups this thread committed have still to read their shared memory.
+template <int N>
+__device__ __forceinline__ void bulk_stores_pending() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+
+
+// mbar_wait and mbar_wait_cluster without the call of a function, for kernels whose warpgroups have registers of their own (setmaxnreg): a
+// function's are those of the launch.
+template <bool CLUSTER = false>
+__device__ __forceinline__ bool bounded_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned* status, unsigned where,
+                                             unsigned long long limit_ns) {
+    const uint32_t b = smem_u32(bar);
+    const auto done = [&] { return CLUSTER ? mbar_try_wait_cluster(b, parity) : mbar_try_wait(b, parity); };
+    if (done()) return true;
+    const unsigned long long t0 = global_timer_ns();
+#pragma unroll 1
+    for (unsigned spins = 1; !done(); ++spins) {
+        if ((spins & 31u) != 0u) continue;
+        if (*abort_flag) return false;
+        if (global_timer_ns() - t0 > limit_ns) {
+            *abort_flag = 1;
+            atomicCAS(status, 0u, (unsigned)TT_ERR_TIMEOUT | (where << 8));
+            return false;
+        }
+    }
+    return true;
+}
 }  // namespace tt

@@ -383,6 +383,25 @@ def test_dense_scales_of_any_strides_and_extremes():
 
 
 @gpu
+@pytest.mark.parametrize("m,n,k", [(1000, 3000, 640), (2500, 700, 1000), (257, 20000, 256), (5000, 129, 384)])
+@pytest.mark.parametrize("kind,act,pad", [("f32", B.TT_ACT_NONE, 8), ("bf16", B.TT_ACT_GELU_ERF, 8), ("f16", B.TT_ACT_RELU6, 8), ("bf16", B.TT_ACT_RELU, 3)])
+def test_dense_by_pairs(m, n, k, kind, act, pad):
+    check_dense(m, n, k, kind=kind, act=act, pad=pad + (-n) % 8 if pad == 8 else pad)
+
+
+@gpu
+@pytest.mark.parametrize("m", [5, 100, 2000])
+@pytest.mark.parametrize("act", [B.TT_ACT_NONE, B.TT_ACT_RELU, B.TT_ACT_RELU6, B.TT_ACT_GELU_ERF])
+def test_dense_nan_stays_nan(m, act):
+    x, xs, w, ws = dense_case(m, 2000, 300, 9)
+    x.view(torch.uint8)[m - 1, 299] = 0x7f
+    y = torch.empty(m, 2000, device="cuda")
+    B.dense_quantized(x, xs, w, ws, y, act=act).run()
+    nan = torch.isnan(y)
+    assert nan[m - 1].all() and not nan[:m - 1].any()
+
+
+@gpu
 def test_dense_one_row_without_a_pitch():
     x, xs, w, ws = dense_case(1, 200, 100, 3)
     tight = torch.empty(112, dtype=torch.uint8, device="cuda")[:100].view(1, 100).view(E4M3)
