@@ -417,8 +417,10 @@ __global__ void __launch_bounds__(kPairThreads, 1)
 tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_y, const DenseF8 g) {
     constexpr int kCols = TN / 4;                          // columns of a read-out warp
     constexpr uint32_t kStage = kF8TileA + TN / 2 * 128u;
+    constexpr int kParts = TN / 128, kBufs = 4 / kParts;   // a block's sums come in parts of 128 columns, half of B's rows of each CTA's
+    constexpr int kReaders = 16 / kParts;                  // read-out warps of a part
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[2], acc_empty[2];
+    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[4], acc_empty[4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -431,13 +433,13 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 32u); }
+        for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 2u * kReaders); }
         abort_flag = 0;
         fence_mbar_init();
         fence_proxy_async_shared();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(2u * TN) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -487,26 +489,33 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
             bool ok = true;
             for (int i = 0; i < my_tiles && ok; ++i)
                 for (int kb = 0; kb < g.blocks; ++kb) {
-                    ok = bounded_wait<true>(&acc_empty[buf], aph ^ 1u, abortp, g.status, 2u, g.wait_ns) &&
-                         bounded_wait(&full_bar[st], ph, abortp, g.status, 3u, g.wait_ns);
-                    if (!ok) break;
-                    tc_fence_after();
+                    ok = bounded_wait(&full_bar[st], ph, abortp, g.status, 3u, g.wait_ns);
                     const uint32_t a = base + (uint32_t)st * kStage, b = a + kF8TileA;
                     const uint64_t da = d0 + (uint64_t)((a & 0x3FFFFu) >> 4), db = d0 + (uint64_t)((b & 0x3FFFFu) >> 4);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem_base + (uint32_t)(buf * TN), da + 2u * k, db + 2u * k, g.idesc, k > 0 ? 1u : 0u);
+                    for (int h = 0; h < kParts; ++h) {
+                        ok = ok && bounded_wait<true>(&acc_empty[buf * kParts + h], aph ^ 1u, abortp, g.status, 2u, g.wait_ns);
+                        if (!ok) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            mma_f8_pair(tmem_base + (uint32_t)((buf * kParts + h) * 128), da + 2u * k, db + (uint64_t)(h * (64 * 128 / 16)) + 2u * k, g.idesc, k > 0 ? 1u : 0u);
+                        mma_commit_cg<2>(smem_u32(&acc_full[buf * kParts + h]));
+                    }
+                    if (!ok) break;
                     mma_commit_cg<2>(smem_u32(&empty_bar[st]));
-                    mma_commit_cg<2>(smem_u32(&acc_full[buf]));
                     if (++st == g.stages) { st = 0; ph ^= 1u; }
-                    if (++buf == 2) { buf = 0; aph ^= 1u; }
+                    if (++buf == kBufs) { buf = 0; aph ^= 1u; }
                 }
         }
         __syncwarp();
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
-        const int quad = warp & 3, c0 = ((warp - 4) >> 2) * kCols;
+        // four warps have 128 lanes x kCols columns of the tile; of a part's columns the first half is of this pair's first CTA's rows of B
+        const int quad = warp & 3, group = (warp - 4) >> 2, part = kParts == 2 ? group >> 1 : 0, at0 = kParts == 2 ? (group & 1) * 64 : group * kCols;
+        const int c0 = kParts == 2 ? (group & 1) * 128 + part * 64 : at0;
         const uint32_t staging = base + (uint32_t)g.stages * kStage + (uint32_t)(warp - 4) * 4096u;
-        const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)c0;
+        const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(part * 128 + at0);
         int buf = 0;
         uint32_t aph = 0;
         bool ok = true;
@@ -521,31 +530,31 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
             float sa = __ldg(as), sb = __ldg(bs);
             for (int kb = 0; kb < g.blocks; ++kb) {
                 const float s = sa * sb;
-                if (kb + 1 < g.blocks) { sa = __ldg(as + (kb + 1) * g.as_block); sb = __ldg(bs + (kb + 1) * g.bs_block); }
-                ok = ok && __all_sync(0xffffffffu, bounded_wait(&acc_full[buf], aph, abortp, g.status, 4u, g.wait_ns));
+                if (kb + 1 < g.blocks) { sa = __ldg(as += g.as_block); sb = __ldg(bs += g.bs_block); }
+                ok = ok && __all_sync(0xffffffffu, bounded_wait(&acc_full[buf * kParts + part], aph, abortp, g.status, 4u, g.wait_ns));
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t at = lanes + (uint32_t)(buf * TN);
-                uint32_t r[2][16];
-                tmem_ld16(at, r[0]);
+                const uint32_t at = lanes + (uint32_t)(buf * kParts * 128);
+                // (sixteen at a time: there are four warps a scheduler to take turns, and no registers for more)
 #pragma unroll
-                for (int j = 0; j < kCols / 16; ++j) {
+                for (int j = 0; j < kCols; j += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(at + (uint32_t)j, r);
                     tmem_wait_ld();
-                    if (j + 1 < kCols / 16) tmem_ld16(at + 16u * (j + 1), r[(j + 1) & 1]);
-                    else {
+                    if (j + 16 >= kCols) {
                         // (the accumulator is free again)
                         tc_fence_before();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&acc_empty[buf]), 0u);
+                        if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&acc_empty[buf * kParts + part]), 0u);
                     }
 #pragma unroll
                     for (int k = 0; k < 16; k += 2) {
-                        const float2 f = fma_pair(make_float2(__uint_as_float(r[j & 1][k]), __uint_as_float(r[j & 1][k + 1])), make_float2(s, s), make_float2(acc[16 * j + k], acc[16 * j + k + 1]));
-                        acc[16 * j + k] = f.x;
-                        acc[16 * j + k + 1] = f.y;
+                        const float2 f = fma_pair(make_float2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), make_float2(s, s), make_float2(acc[j + k], acc[j + k + 1]));
+                        acc[j + k] = f.x;
+                        acc[j + k + 1] = f.y;
                     }
                 }
-                if (++buf == 2) { buf = 0; aph ^= 1u; }
+                if (++buf == kBufs) { buf = 0; aph ^= 1u; }
             }
             if (!ok) break;
             if (g.bias) {
@@ -563,15 +572,15 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
             // row at a time (a lane's own row would be 32 places at once).
             const int per = g.y_type == TT_TYPE_F32 ? 32 : kCols;           // columns of a block: 128 bytes of them, or 64 (kCols 32 in 16 bits)
 #pragma unroll
-            for (int part = 0; part < kCols / 32; ++part) {
-                if (part > 0 && g.y_type != TT_TYPE_F32) break;
-                const int col = col0 + part * per;
+            for (int piece = 0; piece < kCols / 32; ++piece) {
+                if (piece > 0 && g.y_type != TT_TYPE_F32) break;
+                const int col = col0 + piece * per;
                 if (lane == 0) bulk_stores_pending<0>();
                 __syncwarp();
                 if (g.y_type == TT_TYPE_F32) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 4)
-                        st_shared_v4(staging + (uint32_t)lane * 128u + ((uint32_t)((j >> 2) ^ (lane & 7)) << 4), acc[32 * part + j], acc[32 * part + j + 1], acc[32 * part + j + 2], acc[32 * part + j + 3]);
+                        st_shared_v4(staging + (uint32_t)lane * 128u + ((uint32_t)((j >> 2) ^ (lane & 7)) << 4), acc[32 * piece + j], acc[32 * piece + j + 1], acc[32 * piece + j + 2], acc[32 * piece + j + 3]);
                 } else {
 #pragma unroll
                     for (int j = 0; j < kCols; j += 8) {
@@ -618,7 +627,7 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
     if (warp == 1) {
         __syncwarp();
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2u * TN) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
     }
 }
 
@@ -653,7 +662,7 @@ static cudaError_t launch_dense_f8_pair(const CUtensorMap& ta, const CUtensorMap
     g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
     g.tiles_a = (g.rows_a + 255) / 256;
     g.tiles = g.tiles_a * ((g.rows_b + TN - 1) / TN);
-    g.idesc = (1u << 4) | ((unsigned)(TN >> 3) << 17) | ((256u >> 4) << 24);
+    g.idesc = (1u << 4) | ((128u >> 3) << 17) | ((256u >> 4) << 24);
     const int units = g.tiles < kSms / 2 ? g.tiles : kSms / 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(2u * (unsigned)units, 1, 1); cfg.blockDim = dim3(kPairThreads, 1, 1);
