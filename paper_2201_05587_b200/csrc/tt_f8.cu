@@ -130,6 +130,7 @@ struct DenseF8 {
 constexpr int kF8Threads = 320;                            // warp 0 TMA, warp 1 MMA + tensor memory, warps 2-9 read-out
 constexpr unsigned kF8TileA = 128 * 128;
 constexpr int kF8MaxStages = 8;
+constexpr int kHalfSm = 113 * 1024;
 
 __device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -161,7 +162,7 @@ __device__ __forceinline__ float activate(float v, int act) {
 }
 
 template <int TN, bool SWAP>
-__global__ void __launch_bounds__(kF8Threads, 1)
+__global__ void __launch_bounds__(kF8Threads, SWAP ? 2 : 1)
 tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b, const DenseF8 g) {
     constexpr int kBufs = 512 / TN < 4 ? 512 / TN : 4;     // accumulators
     constexpr int kCols = TN / 2;                          // columns of a read-out warp
@@ -173,10 +174,13 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int* abortp = &abort_flag;
-    pdl_allow_next();
     const int tile_a = (int)blockIdx.x % g.tiles_a, tile_b = (int)blockIdx.x / g.tiles_a;
     const int kb0 = (int)blockIdx.z * g.blocks_per_split, kb1 = min(g.blocks, kb0 + g.blocks_per_split);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 8u); }
@@ -185,6 +189,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         fence_mbar_init();
         fence_proxy_async_shared();
     }
+    // Tensor memory is taken behind the wait for the launch in front and before the next one may begin: a CTA that waits for a launch holds none that
+    // the launch could be waiting for.
+    pdl_wait_prev();
     constexpr uint32_t kTmemCols = kBufs * TN < 32 ? 32 : kBufs * TN;
     if (warp == 1) {
         tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
@@ -194,7 +201,7 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *(volatile uint32_t*)&tmem_slot;
-    pdl_wait_prev();
+    pdl_allow_next();
 
     float acc[kCols];
 #pragma unroll
@@ -380,6 +387,7 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 constexpr int kPairThreads = 128 + 512;                    // a warpgroup of TMA and MMA, four of read-out (96 registers each at launch; 32 and 112)
 constexpr unsigned kPairStaging = 16 * 4096;                // a block of 32 rows x 128 bytes for each read-out warp
 constexpr int kPairSmem = 230400;
+constexpr int kBand = 16;
 
 __device__ __forceinline__ void mma_f8_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -426,11 +434,14 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     volatile int* abortp = &abort_flag;
-    pdl_allow_next();
     const uint32_t rank = cluster_ctarank();
     const int unit = (int)blockIdx.x / 2, n_units = (int)gridDim.x / 2;
     const int my_tiles = g.tiles > unit ? (g.tiles - unit + n_units - 1) / n_units : 0;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
         for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 2u * kReaders); }
@@ -438,6 +449,7 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
         fence_mbar_init();
         fence_proxy_async_shared();
     }
+    pdl_wait_prev();                                        // (before tensor memory is taken, see above)
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -447,7 +459,14 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
     cluster_sync_all();                                     // the peer's barriers exist before anything arrives on them
     tc_fence_after();
     const uint32_t tmem_base = *(volatile uint32_t*)&tmem_slot;
-    pdl_wait_prev();
+    pdl_allow_next();
+    // Tiles in bands of kBand of 256 rows, so that the pairs at work share rows of A and of B alike.
+    const int tiles_b = g.tiles / g.tiles_a;
+    const auto place = [&](int t, int& tm, int& tn) {
+        const int band = t / (kBand * tiles_b), in = t - band * kBand * tiles_b, high = min(kBand, g.tiles_a - band * kBand);
+        tn = in / high;
+        tm = band * kBand + in - tn * high;
+    };
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
@@ -457,7 +476,8 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
             long long issued = 0;
             bool ok = true;
             for (int i = 0; i < my_tiles && ok; ++i) {
-                const int t = unit + i * n_units, tm = t % g.tiles_a, tn = t / g.tiles_a;
+                int tm, tn;
+                place(unit + i * n_units, tm, tn);
                 const int a0 = (2 * tm + (int)rank) * 128, b0 = tn * TN + (int)rank * (TN / 2);
                 for (int kb = 0; kb < g.blocks; ++kb) {
                     ok = bounded_wait(&empty_bar[st], ph ^ 1u, abortp, g.status, 1u, g.wait_ns);
@@ -520,7 +540,8 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
         uint32_t aph = 0;
         bool ok = true;
         for (int i = 0; i < my_tiles; ++i) {
-            const int t = unit + i * n_units, tm = t % g.tiles_a, tn = t / g.tiles_a;
+            int tm, tn;
+            place(unit + i * n_units, tm, tn);
             const int row0 = (2 * tm + (int)rank) * 128 + quad * 32, col0 = tn * TN + c0;
             const float* as = g.a_scale + (long long)min(row0 + lane, g.rows_a - 1) * g.as_row;
             const float* bs = g.b_scale + (long long)(min(col0, g.rows_b - 1) >> 7) * g.bs_row;
@@ -637,7 +658,10 @@ static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb,
     static OncePerDevice raised;
     const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_dense_f8_kernel<TN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynSmemLimit); });
     if (ready != cudaSuccess) return ready;
-    const int fits = (kDynSmemLimit - 1024) / kStageBytes;
+    // SWAP takes half of an SM's shared memory: two CTAs fit, of this launch or the next one's, whose set-up then runs while this one's sums are
+    // joined; their columns of tensor memory fit together.  The other form takes all columns and so most of the shared memory: beside a CTA that
+    // holds some it would wait for them, and CTAs of two clusters that wait so for each other would do it forever.
+    const int fits = ((SWAP ? kHalfSm : kDynSmemLimit) - 1024) / kStageBytes;
     g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
     const int tiles_b = (g.rows_b + TN - 1) / TN;
     return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes, g.split, stream, ta, tb, g);

@@ -101,7 +101,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     const tt_cache& c = g.a.cache;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, head = blockIdx.y;
     volatile int* abortp = &abort_flag;
-    pdl_allow_next();
     pdl_wait_prev();
     TileView view;
     const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most)
@@ -136,6 +135,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
+    pdl_allow_next();                                                     // (the next launch may take tensor memory: this CTA has its own)
 
     // a softmax thread's row
     const int tile = warp >> 2, r = (int)threadIdx.x & 255;
