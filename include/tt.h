@@ -558,7 +558,7 @@ tt_status tt_cache_append(const tt_cache_append_args* a, void* cuda_stream);
  * last of its lengths[b] tokens; a query sees the tokens up to its own (causal) or all of them, and of those the last `window`
  * if that is not 0 (counted from its own token; causal only).  A query that sees none gives zeros; rows of y behind the last query are left as they were.
  * max_count: the most queries of any sequence, max_length: the longest of the lengths, bounds that the work is dealt by (0: not known, then
- * tokens and max_pages * block); a longer sequence is an error of its status word, more queries only cost time.
+ * tokens and max_pages * block); a sequence beyond them is reported in the status word.
  * workspace: tt_cache_attention_workspace bytes of device memory on a 16-byte boundary, cleared once before its first call; calls leave it
  * ready for the next one.  Runs that share a workspace follow each other: the caller orders them when they go to different streams.
  * Deterministic. */

@@ -93,11 +93,12 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
 // One pass over the visible keys and values with a running maximum and sum of each row (a query of one head).  The heads that share a key
 // head are rows of one tile, so a key is read once for all of them.
 //
-// Tiles of 8 to 32 rows: the cache's bytes are the bound.  A warp takes runs of 64 tokens, 16 at a time, as the 16 rows of m16n8k16
-// products: scores^T = K Q^T and o^T = V^T P^T, so eight query rows cost half of what they would as rows.  Its lanes fetch just the bytes that they
-// multiply: the order of the reduction is free as long as both factors have it, so lane (g, c) takes 16 bytes in a row of the keys g and
-// g + 8, and of four values 16 bytes in a row of columns, and nothing is exchanged through shared memory.  It is only the buffer of the
-// copies under way, each lane's its own, so there is no barrier in the loop.
+// Tiles of 8 to 32 rows: the cache's bytes are the bound.  A warp takes runs of 64 tokens, 16 or 32 at a time, as the rows of m16n8k16
+// products: scores^T = K Q^T and o^T = V^T P^T, so eight query rows cost half of what they would as rows.  The order of a reduction is free as
+// long as both factors have it, so lane (g, c) takes 16 bytes in a row of the keys g and g + 8, and of four values 16 bytes in a row of
+// columns; which keys, and which columns, is chosen so that the swizzled lines of a box are read without bank conflicts.  Boxes arrive by TMA in
+// a ring of the warp's own, so the loop has no barrier but theirs.  (Copied by the lanes, 16 bytes each, they were bound by what the load
+// unit takes, 4 TB/s.)
 //   e4m3 -> 16-bit floating point is exact, and so is a row of queries: brought to a maximum of 2^14..2^15 by a power of two, which the
 // scores' factor takes back.  Probabilities are rounded to 11 bits, times 2^15 and the page's scale over the largest so far, so that what is
 // 2^-29 of the largest still has all of them; sums are in 32 bits.
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
 
 constexpr int kRun = 64;                    // tokens that a warp takes in a row
 constexpr int kAttendWarps = 4;
+constexpr unsigned long long kAttendWait = 1000000000ull;   // nanoseconds that a wait takes at most
 constexpr int kFewRows = 32;                // rows of a tile at most
 constexpr int kMostSplits = 256;            // of a sequence: the last CTA has the maxima and sums of all of them in shared memory
 
@@ -118,11 +120,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
     return t;
 }
-template <int N>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
-}
 constexpr int widest(int bytes) { return bytes % 16 == 0 ? 16 : bytes % 8 == 0 ? 8 : 4; }
 // Over the eight lanes that have the same pair of rows.
 __device__ __forceinline__ float octet_max(float v) {
@@ -135,31 +132,57 @@ __device__ __forceinline__ float octet_sum(float v) {
     for (int d = 4; d < 32; d <<= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
+// Groups of 16 tokens that a step takes: two, where the registers hold them, so that the latencies of one group's products, maxima and
+// exponentials are behind the other's.
+constexpr int attend_groups(int d, int nt) { return nt * d <= 128 ? 2 : 1; }
 // CTAs that their registers leave room for on an SM.
-constexpr int attend_ctas(int d, int nt) { return nt <= 2 && nt * d <= 128 ? 4 : nt * d <= 128 || (nt <= 2 && nt * d <= 256) ? 3 : 2; }
+constexpr int attend_ctas(int d, int nt) { return nt <= 2 && nt * d <= 256 ? 3 : 2; }
 
 template <int D, int NT>
 struct AttendShape {
     static constexpr int kKey = widest(D / 4), kKeyPieces = D / 4 / kKey;           // bytes of a key that a lane fetches at a time, and how often
     static constexpr int kVal = widest(D / 8), kValPieces = D / 8 / kVal;
     static constexpr int kRows = 8 * NT;
+    static constexpr int kGroups = attend_groups(D, NT), kTokens = kStep * kGroups; // ... and the tokens of a step
     static constexpr bool kQueryRegs = NT == 1 || NT * D <= 128;                     // the queries' fragments stay in registers
-    static constexpr uint32_t kKeyBytes = 2u * kKeyPieces * 32u * kKey, kStage = kKeyBytes + 4u * kValPieces * 32u * kVal + 256u;      // 16 tokens, and each lane's copy of two scales
-    static constexpr int kStages = D <= 64 ? 6 : D <= 128 ? 3 : 2;
+    // A step's keys, and its values: boxes of kTokens lines of kLine bytes, swizzled as the tensor map has it.
+    static constexpr int kLine = 8 * kVal, kBoxes = D / kLine;
+    static constexpr uint32_t kBox = kTokens * kLine, kStage = 2u * kTokens * D;
     static constexpr uint32_t kQuery = kQueryRegs ? 0u : NT * (D / 16) * 256u;
+    static constexpr int kCtas = attend_ctas(D, NT);
+    static constexpr int kFits = (int)((227u * 1024u / kCtas - 3072u - kQuery) / (kAttendWarps * kStage));
+    static constexpr int kStages = kFits > 6 ? 6 : kFits;                            // steps in shared memory: one is worked on, the others are under way
     static constexpr uint32_t kRing = kAttendWarps * kStages * kStage;
     static constexpr uint32_t kJoin = kAttendWarps * kRows * (D + 4) * 4u;           // the warps' results (over the ring)
     static constexpr uint32_t kLists = kMostSplits * kRows * 8u;                     // ... the splits' maxima and sums
     static constexpr uint32_t kMore = kRing > kJoin ? (kRing > kLists ? kRing : kLists) : (kJoin > kLists ? kJoin : kLists);
-    static constexpr uint32_t kBytes = kQuery + kMore;
-    static constexpr int kCtas = attend_ctas(D, NT);
+    static constexpr uint32_t kBytes = 1024u + kQuery + kMore;                       // (the ring on 1024 bytes)
+    // The key of a group that row g of the products is (and g + 8), and the place in a line of what lane g takes of a value.
+    static __device__ __forceinline__ int key_of(int g) { return kLine == 128 ? (g & 1) * 4 + (g >> 1) : kLine == 64 ? g ^ ((g >> 1) & 1) : g; }
+    static __device__ __forceinline__ int column_of(int g) { return (kLine == 128 ? (g & 1) * 4 + (g >> 1) : g) * kVal; }
+    static __device__ __forceinline__ uint32_t place(int row, int byte) {            // of a byte of a line in its box
+        const int swz = kLine == 128 ? row & 7 : kLine == 64 ? (row >> 1) & 3 : (row >> 2) & 1;
+        return (uint32_t)(row * kLine + (((byte >> 4) ^ swz) << 4) + (byte & 15));
+    }
+    static_assert(kStages >= 2, "copies run ahead");
 };
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)) tt_attend_few_kernel(const __grid_constant__ Attend g) {
+__global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)) tt_attend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Attend g) {
     typedef AttendShape<D, NT> S;
-    extern __shared__ __align__(16) uint8_t smem[];
-    __shared__ int last_one;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t full_bar[kAttendWarps][S::kStages];
+    __shared__ int last_one, abort_flag;
+    volatile int* abortp = &abort_flag;
+    if (threadIdx.x < kAttendWarps * S::kStages) mbar_init(smem_u32(&full_bar[0][0] + threadIdx.x), 1u);
+    if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_v) : "memory");
+        abort_flag = 0;
+    }
+    fence_mbar_init();
+    fence_proxy_async_shared();
+    __syncthreads();
     pdl_allow_next();
     pdl_wait_prev();
     const tt_cache& c = g.a.cache;
@@ -172,57 +195,70 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     if ((int)blockIdx.z >= active) return;
     const int from = base + (int)blockIdx.z * g.chunk, to = min(hi, from + g.chunk);
 
-    const uint32_t query = smem_u32(smem), ring = query + S::kQuery + (uint32_t)warp * S::kStages * S::kStage;
-    // ---- the copies of a step: 16 tokens of one page ----
-    const int steps = [&] {                                  // of this warp
+    const uint32_t base_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem = smem_raw + (base_s - smem_u32(smem_raw));
+    const uint32_t ring = base_s + (uint32_t)warp * S::kStages * S::kStage, query = base_s + S::kMore;
+    // ---- the copies of a step: groups of 16 tokens, each of one page ----
+    const int groups = [&] {                                 // of this warp
         const int runs = to > from ? (to - from + kRun - 1) / kRun : 0;
         if (warp >= runs) return 0;
         const int mine = (runs - warp + kAttendWarps - 1) / kAttendWarps;
         const int last = from + ((mine - 1) * kAttendWarps + warp) * kRun;
         return (mine - 1) * (kRun / kStep) + (min(kRun, to - last) + kStep - 1) / kStep;
     }();
-    const auto token_of = [&](int step) { return from + ((step >> 2) * kAttendWarps + warp) * kRun + (step & 3) * kStep; };
+    const int steps = (groups + S::kGroups - 1) / S::kGroups;
+    const auto token_of = [&](int group) { return from + ((group >> 2) * kAttendWarps + warp) * kRun + (group & 3) * kStep; };
+    // Lane l has the page and the scales of group 32 i + l, and of the set of 32 behind it.
     const int* table = c.table + b * c.table_row;
-    const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + gq * c.token[0] + cq * S::kKey;
-    const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + 2 * cq * c.token[1] + gq * S::kVal;
-    const float* kscale = c.scale[0] + head * c.s_head[0];
-    const float* vscale = c.scale[1] + head * c.s_head[1];
-    bool bad = false;
     const int shift = 31 - __clz(c.block);
-    const auto page_of = [&](int step) { return step < steps ? table[token_of(step) >> shift] : 0; };
-    const auto fetch = [&](int step, int page, uint32_t slot) {
-        if (step < steps) {
-            if ((unsigned)page >= (unsigned)c.pages) { bad = true; page = 0; }
-            slot += (uint32_t)lane * 16u;                    // (a piece of 16 bytes has a line of 512 for the warp, a smaller one its share)
-            const int t = token_of(step) & (c.block - 1);
-            const uint8_t* k = keys + (page * c.page[0] + t * c.token[0]);
-            const uint8_t* v = vals + (page * c.page[1] + t * c.token[1]);
-            const uint32_t ks = slot - (uint32_t)lane * (16u - S::kKey), vs = slot + S::kKeyBytes - (uint32_t)lane * (16u - S::kVal);
-#pragma unroll
-            for (int n = 0; n < 2; ++n) {
-#pragma unroll
-                for (int p = 0; p < S::kKeyPieces; ++p) copy_async<S::kKey>(ks + (uint32_t)((n * S::kKeyPieces + p) * 32 * S::kKey), k + p * 4 * S::kKey);
-                k += 8 * c.token[0];
+    struct Set { int page; float ks, vs; };
+    const auto look_up = [&](int set) {
+        const int group = 32 * set + lane;
+        Set x{-1, 0.f, 0.f};
+        if (group < groups) {
+            x.page = table[token_of(group) >> shift];
+            if ((unsigned)x.page >= (unsigned)c.pages) {
+                report_invalid(g.a.status);
+                x.page = -1;                                  // (a box outside of the tensor is zeros)
+            } else {
+                x.ks = c.scale[0][x.page * c.s_page[0] + head * c.s_head[0]];
+                x.vs = c.scale[1][x.page * c.s_page[1] + head * c.s_head[1]];
             }
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {                    // tokens 2c, 2c + 1, 2c + 8, 2c + 9
-#pragma unroll
-                for (int p = 0; p < S::kValPieces; ++p) copy_async<S::kVal>(vs + (uint32_t)((n * S::kValPieces + p) * 32 * S::kVal), v + p * 8 * S::kVal);
-                v += n == 1 ? 7 * c.token[1] : c.token[1];
-            }
-            const uint32_t at = slot - (uint32_t)lane * 8u + S::kStage - 256u;
-            copy_async<4>(at, kscale + page * c.s_page[0]);
-            copy_async<4>(at + 4u, vscale + page * c.s_page[1]);
         }
-        cp_async_commit();
+        return x;
     };
-    int next_page = page_of(0);
+    Set now = look_up(0), then = look_up(1);
+    int set = 0;                                             // of the step that is worked on
+    const bool whole_boxes = c.block >= S::kTokens;          // a step's tokens are of one page
+    const auto fetch = [&](int step, uint32_t slot, int stage) {
+        if (step >= steps) return;
+        int pages[S::kGroups];
 #pragma unroll
-    for (int i = 0; i < S::kStages - 1; ++i) {
-        const int page = next_page;
-        next_page = page_of(i + 1);
-        fetch(i, page, ring + (uint32_t)i * S::kStage);
-    }
+        for (int i = 0; i < S::kGroups; ++i) {
+            const int group = step * S::kGroups + i;
+            pages[i] = __shfl_sync(0xffffffffu, (group >> 5) == set ? now.page : then.page, group & 31);
+        }
+        if (lane == 0) {
+            const uint32_t bar = smem_u32(&full_bar[warp][stage]);
+            mbar_expect_tx(bar, S::kStage);
+            const int t = token_of(step * S::kGroups) & (c.block - 1);
+#pragma unroll
+            for (int w = 0; w < 2; ++w)
+#pragma unroll
+                for (int x = 0; x < S::kBoxes; ++x) {
+                    const uint32_t dst = slot + (uint32_t)(w * S::kBoxes + x) * S::kBox;
+                    const CUtensorMap* map = w ? &tmap_v : &tmap_k;
+                    if (S::kGroups == 1 || whole_boxes) tma_load_4d(dst, map, bar, x * S::kLine, t, head, pages[0]);
+                    else {
+#pragma unroll
+                        for (int i = 0; i < S::kGroups; ++i)
+                            tma_load_4d(dst + (uint32_t)(i * kStep * S::kLine), map, bar, x * S::kLine, token_of(step * S::kGroups + i) & (c.block - 1), head, pages[i]);
+                    }
+                }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < S::kStages - 1; ++i) fetch(i, ring + (uint32_t)i * S::kStage, i);
 
     // ---- queries: lane (g, c) has of rows g, g + 8, ... what it has of the keys ----
     const auto q_row = [&](int r) { const int t = (h0 + r) / g.group; return make_int2(start + t0 + t, head * g.group + (h0 + r - t * g.group)); };
@@ -296,84 +332,118 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         for (int e = 0; e < 2; ++e) { top[n][e] = -INFINITY; sum[n][e] = 0.f; }
     const auto sees = [&](int r, int tok) {
         const int pos = before + t0 + (h0 + r) / g.group;
-        return tok < hi && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
+        return tok < to && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
     };
 
-    uint32_t slot = ring, ahead = ring + (uint32_t)(S::kStages - 1) * S::kStage;      // of this step, of the one that is fetched
+    // what a lane reads of a step's boxes
+    const int row0 = S::key_of(gq), rows_v[2] = {S::key_of(2 * cq), S::key_of(2 * cq + 1)};
+    const uint32_t k_at = S::place(row0, cq * S::kKey), v_at[2] = {S::place(rows_v[0], S::column_of(gq)), S::place(rows_v[1], S::column_of(gq))};
+    const auto key_at = [&](int p) {                        // piece p, a line's second 64 bytes or the next box
+        return S::kLine == 128 ? (uint32_t)(p >> 1) * S::kBox + (k_at ^ ((uint32_t)(p & 1) << 6)) : (uint32_t)p * S::kBox + k_at;
+    };
+    int stage = 0, ahead = S::kStages - 1;                   // of this step, of the one that is fetched
+    uint32_t phase = 0u;
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
-        {
-            const int page = next_page;
-            next_page = page_of(step + S::kStages);
-            fetch(step + S::kStages - 1, page, ahead);
-            ahead = ahead + S::kStage == ring + S::kStages * S::kStage ? ring : ahead + S::kStage;
+        if ((step * S::kGroups) >> 5 != set) {
+            ++set;
+            now = then;
+            then = look_up(set + 1);
         }
-        cp_async_wait<S::kStages - 1>();
-        const uint32_t at = slot;
-        slot = slot + S::kStage == ring + S::kStages * S::kStage ? ring : slot + S::kStage;
-        uint32_t scales[2];
-        read_shared<8>(at + S::kStage - 256u + (uint32_t)lane * 8u, scales);
-        const float ks = __uint_as_float(scales[0]), vs = __uint_as_float(scales[1]);
-        const int t = token_of(step);
-        const bool whole = t >= view.whole_lo && t + kStep <= view.whole_hi;
-        // scores of 16 tokens x rows: tokens g, g + 8 and rows 2c, 2c + 1 of each eight
-        float s[NT][2][4];                                   // (two sums each: a chain of products half as long)
+        __syncwarp();                                        // (every lane has read what lay where the next copies go)
+        fetch(step + S::kStages - 1, ring + (uint32_t)ahead * S::kStage, ahead);
+        if (++ahead == S::kStages) ahead = 0;
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&full_bar[warp][stage]), phase, abortp, g.a.status, 40u, kAttendWait))) break;
+        const uint32_t at = ring + (uint32_t)stage * S::kStage;
+        if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
+        const int t = token_of(step * S::kGroups);
+        const bool whole = t >= view.whole_lo && t + S::kTokens <= view.whole_hi && step * S::kGroups + S::kGroups <= groups;
+        float ks[S::kGroups], vs[S::kGroups], new_ref = ref;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < S::kGroups; ++i) {
+            const int group = step * S::kGroups + i;         // (a last step may have fewer: zeros)
+            ks[i] = __shfl_sync(0xffffffffu, now.ks, group & 31);
+            vs[i] = __shfl_sync(0xffffffffu, now.vs, group & 31);
+            new_ref = fmaxf(new_ref, vs[i]);
+        }
+        // scores of 16 tokens x rows: tokens g, g + 8 and rows 2c, 2c + 1 of each eight (in two sums, a chain of products half as long)
+        float s[S::kGroups][NT][2][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[n][0][e] = s[n][1][e] = 0.f;
+        for (int i = 0; i < S::kGroups; ++i)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i][n][0][e] = s[i][n][1][e] = 0.f;
 #pragma unroll
         for (int p = 0; p < S::kKeyPieces; ++p) {
-            uint32_t k[2][S::kKey / 4];
+            uint32_t k[S::kGroups][2][S::kKey / 4];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) read_shared<S::kKey>(at + (uint32_t)((n * S::kKeyPieces + p) * 32 + lane) * S::kKey, k[n]);
+            for (int i = 0; i < S::kGroups; ++i)
+#pragma unroll
+                for (int n = 0; n < 2; ++n) read_shared<S::kKey>(at + key_at(p) + (uint32_t)((i * kStep + 8 * n) * S::kLine), k[i][n]);
 #pragma unroll
             for (int w = 0; w < S::kKey / 4; ++w) {
-                uint32_t a0, a1, a2, a3;
-                f16_pairs_of_e4m3(k[0][w], a0, a2);
-                f16_pairs_of_e4m3(k[1][w], a1, a3);
-                const int i = p * (S::kKey / 4) + w;
+                const int j = p * (S::kKey / 4) + w;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    if constexpr (S::kQueryRegs) mma_16x8x16(s[n][i & 1], a0, a1, a2, a3, q[n][i][0], q[n][i][1]);
-                    else {
-                        uint32_t qq[2];
-                        read_shared<8>(query + (uint32_t)(((n * (D / 16) + i) * 32 + lane) * 8), qq);
-                        mma_16x8x16(s[n][i & 1], a0, a1, a2, a3, qq[0], qq[1]);
+                for (int i = 0; i < S::kGroups; ++i) {
+                    uint32_t a0, a1, a2, a3;
+                    f16_pairs_of_e4m3(k[i][0][w], a0, a2);
+                    f16_pairs_of_e4m3(k[i][1][w], a1, a3);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        if constexpr (S::kQueryRegs) mma_16x8x16(s[i][n][j & 1], a0, a1, a2, a3, q[n][j][0], q[n][j][1]);
+                        else {
+                            uint32_t qq[2];
+                            read_shared<8>(query + (uint32_t)(((n * (D / 16) + j) * 32 + lane) * 8), qq);
+                            mma_16x8x16(s[i][n][j & 1], a0, a1, a2, a3, qq[0], qq[1]);
+                        }
                     }
                 }
             }
         }
         // the running maximum, in powers of two
-        const float new_ref = fmaxf(ref, vs);
-        const float unit = vs == new_ref ? 32768.f : __fdividef(vs, new_ref) * 32768.f;
         const float shrink = ref == new_ref ? 1.f : __fdividef(ref, new_ref);
         bool moved = shrink != 1.f;
         ref = new_ref;
-        float alpha[NT][2];
-        uint32_t pb[NT][2];
+        float unit[S::kGroups], alpha[NT][2];
+        uint32_t pb[S::kGroups][NT][2];
+#pragma unroll
+        for (int i = 0; i < S::kGroups; ++i) unit[i] = vs[i] == new_ref ? 32768.f : __fdividef(vs[i], new_ref) * 32768.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float v[4];
+            float v[S::kGroups][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = (s[n][0][e] + s[n][1][e]) * (factor[n][e & 1] * ks);
-                if (!whole) v[e] = sees(8 * n + 2 * cq + (e & 1), t + gq + 8 * (e >> 1)) ? v[e] : -INFINITY;
-            }
+            for (int i = 0; i < S::kGroups; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[i][e] = (s[i][n][0][e] + s[i][n][1][e]) * (factor[n][e & 1] * ks[i]);
+                    if (!whole) v[i][e] = sees(8 * n + 2 * cq + (e & 1), t + kStep * i + row0 + 8 * (e >> 1)) ? v[i][e] : -INFINITY;
+                }
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const float mx = fmaxf(top[n][e], octet_max(fmaxf(v[e], v[e + 2])));
+                float mx = fmaxf(v[0][e], v[0][e + 2]);
+#pragma unroll
+                for (int i = 1; i < S::kGroups; ++i) mx = fmaxf(mx, fmaxf(v[i][e], v[i][e + 2]));
+                mx = fmaxf(top[n][e], octet_max(mx));
                 const float ref_max = mx == -INFINITY ? 0.f : mx;
                 const float keep = exp2_fast(top[n][e] - ref_max);
                 moved = moved || mx != top[n][e];
                 top[n][e] = mx;
-                v[e] = exp2_fast(v[e] - ref_max);
-                v[e + 2] = exp2_fast(v[e + 2] - ref_max);
-                sum[n][e] = fmaf(sum[n][e], keep, v[e] + v[e + 2]);
+                float add = 0.f;
+#pragma unroll
+                for (int i = 0; i < S::kGroups; ++i) {
+                    v[i][e] = exp2_fast(v[i][e] - ref_max);
+                    v[i][e + 2] = exp2_fast(v[i][e + 2] - ref_max);
+                    add += v[i][e] + v[i][e + 2];
+                }
+                sum[n][e] = fmaf(sum[n][e], keep, add);
                 alpha[n][e] = keep * shrink;
             }
-            pb[n][0] = transpose_8x8(down2<TT_TYPE_F16>(v[0] * unit, v[1] * unit));
-            pb[n][1] = transpose_8x8(down2<TT_TYPE_F16>(v[2] * unit, v[3] * unit));
+#pragma unroll
+            for (int i = 0; i < S::kGroups; ++i) {
+                pb[i][n][0] = transpose_8x8(down2<TT_TYPE_F16>(v[i][0] * unit[i], v[i][1] * unit[i]));
+                pb[i][n][1] = transpose_8x8(down2<TT_TYPE_F16>(v[i][2] * unit[i], v[i][3] * unit[i]));
+            }
         }
         if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
@@ -385,68 +455,73 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         }
         // values
 #pragma unroll
-        for (int p = 0; p < S::kValPieces; ++p) {
-            uint32_t v[4][S::kVal / 4];
+        for (int i = 0; i < S::kGroups; ++i)
 #pragma unroll
-            for (int n = 0; n < 4; ++n) read_shared<S::kVal>(at + S::kKeyBytes + (uint32_t)((n * S::kValPieces + p) * 32 + lane) * S::kVal, v[n]);
-            if (!whole) {
-                // What no row of the tile sees is not multiplied (it may be anything), and a NaN that only some rows see reaches just those: it is
-                // replaced by 0 in the product, and another product counts for each row how many of a column's it sees.
-                uint32_t nans = 0u;
+            for (int p = 0; p < S::kValPieces; ++p) {
+                uint32_t v[4][S::kVal / 4];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const int tok = t + 2 * cq + (n & 1) + 8 * (n >> 1);
-                    const bool any = tok >= lo && tok < hi;
+                for (int n = 0; n < 4; ++n) read_shared<S::kVal>(at + (uint32_t)(S::kBoxes + p) * S::kBox + v_at[n & 1] + (uint32_t)((i * kStep + 8 * (n >> 1)) * S::kLine), v[n]);
+                if (!whole) {
+                    // What no row of the tile sees is not multiplied (it may be anything), and a NaN that only some rows see reaches just those: it is
+                    // replaced by 0 in the product, and another product counts for each row how many of a column's it sees.
+                    uint32_t nans = 0u;
 #pragma unroll
-                    for (int w = 0; w < S::kVal / 4; ++w) {
-                        v[n][w] = any ? v[n][w] : 0u;
-                        nans |= nan_bytes(v[n][w]);
-                    }
-                }
-                if (__any_sync(0xffffffffu, nans != 0u)) {
+                    for (int n = 0; n < 4; ++n) {
+                        const int tok = t + kStep * i + rows_v[n & 1] + 8 * (n >> 1);
+                        const bool any = tok >= lo && tok < min(hi, to);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint32_t see[2];
-#pragma unroll
-                        for (int r = 0; r < 2; ++r)
-                            see[r] = (sees(8 * n + gq, t + 8 * r + 2 * cq) ? 0x3c00u : 0u) | (sees(8 * n + gq, t + 8 * r + 2 * cq + 1) ? 0x3c000000u : 0u);
-#pragma unroll
-                        for (int j = 0; j < S::kVal; j += 2) {
-                            const auto is_nan = [&](int m, int i) { return ((v[m][i >> 2] >> (8 * (i & 3))) & 0x7fu) == 0x7fu; };
-                            uint32_t a[4];
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) a[r] = (is_nan(r & 2, j + (r & 1)) ? 0x3c00u : 0u) | (is_nan((r & 2) + 1, j + (r & 1)) ? 0x3c000000u : 0u);
-                            float hit[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_16x8x16(hit, a[0], a[1], a[2], a[3], see[0], see[1]);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) if (hit[e] > 0.f) o[n][(p * S::kVal + j) / 2][e] = __int_as_float(0x7fffffff);
+                        for (int w = 0; w < S::kVal / 4; ++w) {
+                            v[n][w] = any ? v[n][w] : 0u;
+                            nans |= nan_bytes(v[n][w]);
                         }
                     }
+                    if (__any_sync(0xffffffffu, nans != 0u)) {
 #pragma unroll
-                    for (int n = 0; n < 4; ++n)
+                        for (int n = 0; n < NT; ++n) {
+                            uint32_t see[2];
 #pragma unroll
-                        for (int w = 0; w < S::kVal / 4; ++w) v[n][w] &= ~((nan_bytes(v[n][w]) >> 7) * 0xffu);
+                            for (int r = 0; r < 2; ++r)
+                                see[r] = (sees(8 * n + gq, t + kStep * i + 8 * r + rows_v[0]) ? 0x3c00u : 0u) | (sees(8 * n + gq, t + kStep * i + 8 * r + rows_v[1]) ? 0x3c000000u : 0u);
+#pragma unroll
+                            for (int j = 0; j < S::kVal; j += 2) {
+                                const auto is_nan = [&](int m, int x) { return ((v[m][x >> 2] >> (8 * (x & 3))) & 0x7fu) == 0x7fu; };
+                                uint32_t a[4];
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) a[r] = (is_nan(r & 2, j + (r & 1)) ? 0x3c00u : 0u) | (is_nan((r & 2) + 1, j + (r & 1)) ? 0x3c000000u : 0u);
+                                float hit[4] = {0.f, 0.f, 0.f, 0.f};
+                                mma_16x8x16(hit, a[0], a[1], a[2], a[3], see[0], see[1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) if (hit[e] > 0.f) o[n][(p * S::kVal + j) / 2][e] = __int_as_float(0x7fffffff);
+                            }
+                        }
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+#pragma unroll
+                            for (int w = 0; w < S::kVal / 4; ++w) v[n][w] &= ~((nan_bytes(v[n][w]) >> 7) * 0xffu);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < S::kVal; j += 2) {
+                    // bytes j, j + 1 of two tokens side by side: the pairs of the reduction, two columns of them
+                    const uint32_t sel = (j & 2) ? 0x7362u : 0x5140u;
+                    uint32_t a0, a1, a2, a3;
+                    f16_pairs_of_e4m3(__byte_perm(v[0][j >> 2], v[1][j >> 2], sel), a0, a1);
+                    f16_pairs_of_e4m3(__byte_perm(v[2][j >> 2], v[3][j >> 2], sel), a2, a3);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma_16x8x16(o[n][(p * S::kVal + j) / 2], a0, a1, a2, a3, pb[i][n][0], pb[i][n][1]);
                 }
             }
-#pragma unroll
-            for (int j = 0; j < S::kVal; j += 2) {
-                // bytes j, j + 1 of two tokens side by side: the pairs of the reduction, two columns of them
-                const uint32_t sel = (j & 2) ? 0x7362u : 0x5140u;
-                uint32_t a0, a1, a2, a3;
-                f16_pairs_of_e4m3(__byte_perm(v[0][j >> 2], v[1][j >> 2], sel), a0, a1);
-                f16_pairs_of_e4m3(__byte_perm(v[2][j >> 2], v[3][j >> 2], sel), a2, a3);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) mma_16x8x16(o[n][(p * S::kVal + j) / 2], a0, a1, a2, a3, pb[n][0], pb[n][1]);
-            }
-        }
     }
-    if (bad) report_invalid(g.a.status);
+    // a wait that gave up: the copies under way land before the shared memory is used again (bounded)
+    if (*abortp && lane == 0) {
+        const unsigned long long t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 2000000ull) { }
+    }
 
     // ---- the warps' results together: maximum, sum and o of every row, through shared memory ----
-    cp_async_wait<0>();
     __syncthreads();                                         // (the ring is idle)
     constexpr int kLine = D + 4;                             // floats of a row: o, then maximum, sum
-    float* join = reinterpret_cast<float*>(smem + S::kQuery);
+    float* join = reinterpret_cast<float*>(smem);
     const float to_real = ref * 3.0517578125e-5f;            // 2^-15
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -458,7 +533,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             for (int p = 0; p < S::kValPieces; ++p)
 #pragma unroll
                 for (int j = 0; j < S::kVal; j += 2)
-                    *reinterpret_cast<float2*>(line + (p * 8 + gq) * S::kVal + j) = make_float2(o[n][(p * S::kVal + j) / 2][e] * to_real, o[n][(p * S::kVal + j) / 2][e + 2] * to_real);
+                    *reinterpret_cast<float2*>(line + p * S::kLine + S::column_of(gq) + j) = make_float2(o[n][(p * S::kVal + j) / 2][e] * to_real, o[n][(p * S::kVal + j) / 2][e + 2] * to_real);
             if (gq == 0) *reinterpret_cast<float2*>(line + D) = make_float2(top[n][e], total);
         }
     __syncthreads();
@@ -610,7 +685,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         f = g;
         // As many rows as a sequence has, up to what the registers hold: a key that is fetched and converted serves all of them.
         f.rows = most_rows <= 8 ? 8 : most_rows <= 16 || c.d > 128 ? 16 : 32;
-        f.by_sequence = prompts;
+        f.by_sequence = prompts || ((a.max_count > 0 || c.batch == 1) && most_rows <= f.rows);      // (no more than a tile each)
         if (prompts) f.most = kFewRows;
         plan.few_units = f.by_sequence ? c.batch : (long long)a.tokens * g.group / f.rows + c.batch;
         const long long tiles = plan.few_units * c.heads, span = span_of(f.rows) + kRun;      // (splits begin at multiples of kRun)
@@ -621,7 +696,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         constexpr int kGrain = kAttendWarps * kRun;
         long long chunk = ((span - kRun) * tiles + slots - 1) / slots;
         chunk = (chunk + kGrain - 1) / kGrain * kGrain;
-        if (chunk < 2 * kGrain) chunk = 2 * kGrain;
+        if (chunk < kGrain) chunk = kGrain;
         if (c.batch > 1 && chunk > 8 * kGrain) chunk = 8 * kGrain;
         while ((span + chunk - 1) / chunk > kMostSplits || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
         f.chunk = (int)(chunk < span ? chunk : span);
@@ -664,7 +739,16 @@ static cudaError_t launch_attend(const Attend& g, long long units, void* stream)
     static OncePerDevice raised;
     const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
     if (ready != cudaSuccess) return ready;
-    return launch(tt_attend_few_kernel<D, NT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, g);
+    CUtensorMap maps[2];
+    for (int w = 0; w < 2; ++w) {
+        const tt_cache& c = g.a.cache;
+        const int box = c.block >= S::kTokens ? S::kTokens : kStep;
+        // (without pages nothing is read: the map is of any memory)
+        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], S::kLine, box)
+                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, S::kLine, box);
+        if (st != TT_OK) return cudaErrorInvalidValue;
+    }
+    return launch(tt_attend_few_kernel<D, NT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, maps[0], maps[1], g);
 }
 template <int D>
 static cudaError_t launch_attend_rows(const Attend& g, long long units, void* stream) {

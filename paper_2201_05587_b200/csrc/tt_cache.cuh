@@ -7,15 +7,20 @@ namespace tt {
 
 __device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(status, 0u, (unsigned)TT_ERR_INVALID_ARG); }
 
-// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] / per + extra * b and up (as many as it can need
-// at most), so a unit finds its sequence by bisection.
+// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] * mul / per + extra * b and up (as many as it can need
+// at most).  The whole warp looks for a unit's, 32 places at a time (a lane on its own would take the logarithm of the batch in loads, one after the other).
 __device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
-    int lo = 0, hi = batch - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (starts[mid] * mul / per + (long long)extra * mid <= unit) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x & 31;
+    const auto begin = [&](int b) { return starts[b] * mul / per + (long long)extra * b; };
+    int lo = 0, n = batch;                                   // it is one of lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 31) / 32, b = lo + lane * step;
+        const unsigned in = __ballot_sync(0xffffffffu, lane * step < n && begin(b) <= unit);
+        const int last = in ? 31 - __clz((int)in) : 0;       // (places rise; whatever they hold, the result is one of the batch)
+        n = min(step, n - last * step);
+        lo += last * step;
     }
-    first = starts[lo] * mul / per + (long long)extra * lo;
+    first = begin(lo);
     return lo;
 }
 
@@ -53,7 +58,7 @@ __device__ __forceinline__ bool view_tile(const Attend& g, int tile_rows, long l
     v.start = g.a.starts[v.b];
     const int count = g.a.starts[v.b + 1] - v.start, length = g.a.lengths[v.b];
     if (count == 0) return false;
-    if (count < 0 || v.start < 0 || v.start + (long long)count > g.a.tokens || length < 0 || length > g.max_length) {
+    if (count < 0 || v.start < 0 || v.start + (long long)count > g.a.tokens || length < 0 || length > g.max_length || (g.a.max_count > 0 && count > g.a.max_count)) {
         if (threadIdx.x == 0) report_invalid(g.a.status);
         return false;
     }

@@ -708,10 +708,34 @@ def test_attention_splits_a_long_sequence(length, window):
 
 
 @gpu
+@pytest.mark.parametrize("batch", [33, 70, 1100])
+@pytest.mark.parametrize("count,max_count", [(1, 1), (1, 0), (3, 3), (3, 0)])
+def test_attention_of_large_batches(batch, count, max_count):
+    lengths = [(17 * b) % 60 for b in range(batch)]
+    counts = [min(n, 1 + b % count) if b % 7 else 0 for b, n in enumerate(lengths)]
+    p = Pages(lengths, 1, 32, 16, seed=batch)
+    check_attention(p, counts, 4, max_count=max_count)
+    x = torch.randn(sum(counts), 1, 32, generator=gen(1), device="cuda")
+    check_append(p, counts, [x, -x])
+
+
+@gpu
 def test_attention_rows_that_see_nothing_are_zeros():
     p = Pages([0, 3, 0], 1, 64, 16, seed=1)
     y = check_attention(p, [2, 5, 0], 2)                          # the first two queries of the second sequence stand in front of its tokens
     assert (y[:4] == 0).all() and (y[4:7] != 0).any()
+
+
+@gpu
+def test_attention_over_no_pages_at_all():
+    for pages, columns in ((0, 3), (4, 0)):
+        k = torch.zeros(pages, 2, 16, 64, dtype=torch.uint8, device="cuda").view(E4M3)
+        s = torch.zeros(pages, 2, device="cuda")
+        q = torch.randn(3, 4, 64, generator=gen(1), device="cuda").to(torch.bfloat16)
+        y = torch.full_like(q, 5.0)
+        call = B.cache_attention(B.Cache(k, k, s, s, torch.zeros(2, columns, dtype=torch.int32, device="cuda")), q, y, int32([0, 1, 3]), int32([0, 0]), 0.1)
+        call.run()
+        assert call.status() == B.TT_OK and (y == 0).all()
 
 
 @gpu
@@ -811,9 +835,10 @@ def test_attention_reports_what_only_the_device_sees():
         call = B.cache_attention(p.cache(), q, torch.empty_like(q), int32(starts), int32(lengths), 0.1)
         call.run()
         assert call.status() == B.TT_ERR_INVALID_ARG, (table, lengths, starts)
-    call = B.cache_attention(p.cache(), q, torch.empty_like(q), int32([0, 2]), int32([20]), 0.1, max_length=16)
-    call.run()
-    assert call.status() == B.TT_ERR_INVALID_ARG
+    for bound in (dict(max_length=16), dict(max_count=1)):
+        call = B.cache_attention(p.cache(), q, torch.empty_like(q), int32([0, 2]), int32([20]), 0.1, **bound)
+        call.run()
+        assert call.status() == B.TT_ERR_INVALID_ARG, bound
 
 
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
