@@ -167,6 +167,25 @@ struct AttendShape {
     static_assert(kStages >= 2, "copies run ahead");
 };
 
+// The tokens of a split.  Only the device knows the lengths: the split that deals all sequences' tokens to the CTAs that the SMs hold at once, less a
+// fifth, as every sequence has a last split that is not full.  (8 sequences of up to 16384 tokens: 34 us so; by the longest that there may be 42.)  No
+// less than what the grid has room for.
+template <int ROWS>
+__device__ __forceinline__ int split_tokens(const Attend& g) {
+    constexpr int kGrain = kAttendWarps * kRun;
+    const tt_cache& c = g.a.cache;
+    if (g.splits == 1 || c.batch > 1024) return g.chunk;
+    unsigned runs = 0u;                                      // of all sequences' tiles
+    for (int b = threadIdx.x & 31; b < c.batch; b += 32) {
+        const long long rows = (long long)(g.a.starts[b + 1] - g.a.starts[b]) * g.group;
+        const int length = min(max(g.a.lengths[b], 0), g.span);
+        if (rows >= g.least && rows <= g.most) runs += (unsigned)min((long long)(length + kRun - 1) / kRun * ((rows + ROWS - 1) / ROWS), 1ll << 20);
+    }
+    const long long all = __reduce_add_sync(0xffffffffu, min(runs, 1u << 26));
+    const long long share = (all * c.heads * kRun + g.share - 1) / g.share;
+    return max(g.chunk, (int)min((share + kGrain - 1) / kGrain * kGrain, (long long)g.span + kRun));
+}
+
 template <int D, int NT>
 __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)) tt_attend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Attend g) {
     typedef AttendShape<D, NT> S;
@@ -190,10 +209,10 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     TileView view;
     if (!view_tile(g, S::kRows, blockIdx.x, view)) return;
     const int b = view.b, start = view.start, rows = view.rows, t0 = view.t0, h0 = view.h0, before = view.before, lo = view.lo, hi = view.hi;
-    const int base = lo / kRun * kRun;
-    const int active = hi > lo ? (hi - base + g.chunk - 1) / g.chunk : 1;
+    const int base = lo / kRun * kRun, chunk = split_tokens<S::kRows>(g);
+    const int active = hi > lo ? (hi - base + chunk - 1) / chunk : 1;
     if ((int)blockIdx.z >= active) return;
-    const int from = base + (int)blockIdx.z * g.chunk, to = min(hi, from + g.chunk);
+    const int from = base + (int)blockIdx.z * chunk, to = min(hi, from + chunk);
 
     const uint32_t base_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base_s - smem_u32(smem_raw));
@@ -612,7 +631,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     for (int e = threadIdx.x; e < rows * (D / 4); e += kAttendWarps * 32) {
         const int r = e / (D / 4), i = 4 * (e - r * (D / 4));
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
+#pragma unroll 16
         for (int z = 0; z < active; ++z) {
             const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + r * D + i));
             const float w = lists[z * S::kRows + r].x;
@@ -690,17 +709,21 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         plan.few_units = f.by_sequence ? c.batch : (long long)a.tokens * g.group / f.rows + c.batch;
         const long long tiles = plan.few_units * c.heads, span = span_of(f.rows) + kRun;      // (splits begin at multiples of kRun)
         if (tiles > 0x7fffffffll) return TT_ERR_INVALID_ARG;
-        // One sequence: a share for each CTA that the SMs hold at once.  Several, of lengths that only the device knows: a quarter of that, so
-        // that long and short ones even out.  No split is shorter than what makes joining it cheap.
-        const long long slots = (long long)kSms * attend_ctas(c.d, f.rows / 8) * (c.batch > 1 ? 4 : 1);
+        // The CTAs that the SMs hold at once share all tokens (split_tokens); the grid has room for as many splits of a sequence as four rounds of
+        // them allow, most of which find nothing to do where there are many sequences.
+        const long long slots = (long long)kSms * attend_ctas(c.d, f.rows / 8);
         constexpr int kGrain = kAttendWarps * kRun;
-        long long chunk = ((span - kRun) * tiles + slots - 1) / slots;
+        f.span = (int)(span - kRun);
+        f.share = (int)(c.batch > 1 ? slots * 4 / 5 : slots);
+        long long splits = c.batch > 1 ? 4 * slots / tiles : slots / tiles;
+        if (splits > kMostSplits) splits = kMostSplits;
+        if (splits < 1) splits = 1;
+        long long chunk = (span + splits - 1) / splits;
         chunk = (chunk + kGrain - 1) / kGrain * kGrain;
         if (chunk < kGrain) chunk = kGrain;
-        if (c.batch > 1 && chunk > 8 * kGrain) chunk = 8 * kGrain;
-        while ((span + chunk - 1) / chunk > kMostSplits || (span + chunk - 1) / chunk * tiles > 0x7fffffffll) chunk *= 2;
-        f.chunk = (int)(chunk < span ? chunk : span);
+        f.chunk = (int)chunk;
         f.splits = (int)((span + chunk - 1) / chunk);
+        if (f.splits < 1) f.splits = 1;
         plan.bytes = workspace_part(f, plan.few_units);
     }
     if (prompts) {

@@ -31,6 +31,7 @@ struct Attend {
     tt_cache_attention_args a;
     int group, rows;                        // query heads of a key head; rows of a tile
     int chunk, splits, max_length;          // tokens of a split, most splits
+    int span, share;                        // tokens that a tile can see; CTAs that all tokens are dealt to
     int least, most;                        // rows of the sequences that the kernel takes
     int by_sequence;                        // no more than one tile each: tile b is sequence b's
     int q_wide, y_wide;                     // four values of q, of y at a time
