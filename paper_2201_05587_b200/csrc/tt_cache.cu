@@ -1,72 +1,101 @@
 // A paged cache of keys and values in e4m3, a scale for each page and head: new tokens into it, and attention over it.
 #include <cuda_runtime.h>
 #include <cstring>
+#include <type_traits>
 #include "tt_cache.cuh"
 
 namespace tt {
 
 // ---- append ---------------------------------------------------------------------------------------------------------------
 //
-// A CTA has the new tokens of one page and head, of the keys or of the values: their maximum first, then (the second reading comes from the
-// caches) their conversion; where the page holds tokens already and the scale has to rise, those are brought to it.
-template <int TYPE, bool WIDE>
+// The new tokens of one page and head, of the keys or of the values, are a CTA's, or a warp's where there are few of them: read once into registers
+// (what is more than kHeld pieces a thread is read again, from the caches), their maximum, their conversion; where the page holds
+// tokens already and the scale has to rise, those are brought to it.
+template <int TYPE, bool WIDE, bool WARP>
 __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_append_args a) {
     __shared__ float warp_most[8];
     typedef typename Element<TYPE>::type T;
     pdl_allow_next();
     pdl_wait_prev();
     const tt_cache& c = a.cache;
-    const int head = (int)blockIdx.y >> 1, w = (int)blockIdx.y & 1;
+    const int which = WARP ? (int)blockIdx.y * 8 + ((int)threadIdx.x >> 5) : (int)blockIdx.y, head = which >> 1, w = which & 1;
+    const int me = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x;
+    constexpr int kThreads = WARP ? 32 : 256;
+    if (WARP && head >= c.heads) return;
     long long first_unit;
     const int b = sequence_of(a.starts, c.batch, 1, c.block, 2, blockIdx.x, first_unit);
     const int start = a.starts[b], count = a.starts[b + 1] - start, length = a.lengths[b];
     if (count == 0) return;
     if (count < 0 || start < 0 || start + (long long)count > a.tokens || length < count || length > (long long)c.max_pages * c.block) {
-        if (threadIdx.x == 0) report_invalid(a.status);
+        if (me == 0) report_invalid(a.status);
         return;
     }
     const int first = length - count;                       // position of the first new token
     const long long index = first / c.block + ((long long)blockIdx.x - first_unit);
     if (index * c.block >= length) return;
-    const int page = c.table[b * c.table_row + index];
-    if (page < 0 || page >= c.pages) {
-        if (threadIdx.x == 0) report_invalid(a.status);
-        return;
-    }
     const int lo = max(first, (int)index * c.block), hi = min(length, (int)index * c.block + c.block);
     const int held = lo - (int)index * c.block;             // tokens that the page holds already
-    constexpr int kPiece = WIDE ? 8 : 1;                    // values a thread takes at a time
+    constexpr int kPiece = WIDE ? 8 : 1, kHeld = WIDE ? 4 : 16;      // values a thread takes at a time, and how often it keeps them
     const int pieces = c.d / kPiece, total = (hi - lo) * pieces;
-    const T* x = static_cast<const T*>(a.x[w]) + (long long)(start + (lo - first)) * a.x_token[w] + (long long)head * a.x_head[w];
-    float most = 0.f;
-    for (int e = threadIdx.x; e < total; e += blockDim.x) {
-        const int t = e / pieces, i = (e - t * pieces) * kPiece;
-        float v[kPiece];
-        if constexpr (WIDE) load_wide<TYPE, kPiece>(x + t * a.x_token[w] + i, v);
-        else v[0] = Element<TYPE>::up(x[t * a.x_token[w] + i]);
+    const T* x = static_cast<const T*>(a.x[w]) + ((long long)(start + (lo - first)) * a.x_token[w] + (long long)head * a.x_head[w]);
+    const auto place = [&](int e, int& t, int& i) { t = e / pieces; i = (e - t * pieces) * kPiece; };
+    struct One { float v; };
+    typedef typename std::conditional<WIDE, Eights<TYPE, 1>, One>::type Piece;
+    const auto load = [&](int e, Piece& u) {
+        int t, i;
+        place(e, t, i);
+        if constexpr (WIDE) u.load(x + t * a.x_token[w], i, 0, c.d, true);
+        else u.v = Element<TYPE>::up(x[t * a.x_token[w] + i]);
+    };
+    // the largest finite magnitude of u and m; nan: whether there is one that is not
+    const auto more = [&](const Piece& u, float m, bool& odd) {
+        if constexpr (WIDE) {
+            const float n = u.most();
+            if (n < INFINITY) return fmaxf(m, n);
+            odd = true;
+            return fmaxf(m, u.finite_most());
+        } else {
+            odd = odd || !(fabsf(u.v) < INFINITY);
+            return finite_max(m, u.v);
+        }
+    };
+    Piece v[kHeld];
 #pragma unroll
-        for (int j = 0; j < kPiece; ++j) most = finite_max(most, v[j]);
+    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) load(me + k * kThreads, v[k]);      // (on their way while the page is looked up)
+    const int page = c.table[b * c.table_row + index];
+    if (page < 0 || page >= c.pages) {
+        if (me == 0) report_invalid(a.status);
+        return;
+    }
+    float* scale = c.scale[w] + page * c.s_page[w] + head * c.s_head[w];
+    const float old = held > 0 ? *scale : 0.f;
+    float most = 0.f;
+    bool odd = false;
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) most = more(v[k], most, odd);
+    for (int e = me + kHeld * kThreads; e < total; e += kThreads) {
+        Piece u;
+        load(e, u);
+        most = more(u, most, odd);
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-    float* scale = c.scale[w] + page * c.s_page[w] + head * c.s_head[w];
-    const float old = held > 0 ? *scale : 0.f;
-    if (blockDim.x > 32) {
-        if ((threadIdx.x & 31) == 0) warp_most[threadIdx.x >> 5] = most;
-        __syncthreads();                                    // (and every thread has read the old scale)
-        for (int i = 0; i < (int)blockDim.x >> 5; ++i) most = fmaxf(most, warp_most[i]);
-    } else {
-        __syncwarp();
+    if constexpr (WARP) __syncwarp();                       // (every thread has read the old scale)
+    else {
+        if ((me & 31) == 0) warp_most[me >> 5] = most;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, warp_most[i]);
     }
     float s = power_scale(most);
     if (held > 0 && old >= s) s = old;
-    if (threadIdx.x == 0 && (held == 0 || s != old)) *scale = s;
+    if (me == 0 && (held == 0 || s != old)) *scale = s;
     uint8_t* data = static_cast<uint8_t*>(c.data[w]) + page * c.page[w] + head * c.head[w];
     if (held > 0 && s != old) {
         // (a ratio of powers of two as the calls here leave them; a scale of another origin is taken as it is)
         const float ratio = __fdiv_rn(old, s);
         const int words = c.d / 4;
-        for (int e = threadIdx.x; e < held * words; e += blockDim.x) {
+        for (int e = me; e < held * words; e += kThreads) {
             const int t = e / words;
             uint32_t* p = reinterpret_cast<uint32_t*>(data + t * c.token[w]) + (e - t * words);
             const uint32_t q = *p;
@@ -75,16 +104,27 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
     }
     const bool power = (__float_as_int(s) & 0x7fffff) == 0 && s >= 1.17549435e-38f && s <= 1.329227996e36f;      // 2^-126 .. 2^120
     const float inv = power ? power_inverse(s) : 0.f;
-    for (int e = threadIdx.x; e < total; e += blockDim.x) {
-        const int t = e / pieces, i = (e - t * pieces) * kPiece;
-        float v[kPiece];
-        if constexpr (WIDE) load_wide<TYPE, kPiece>(x + t * a.x_token[w] + i, v);
-        else v[0] = Element<TYPE>::up(x[t * a.x_token[w] + i]);
-#pragma unroll
-        for (int j = 0; j < kPiece; ++j) v[j] = power ? v[j] * inv : __fdiv_rn(v[j], s);
+    const auto put = [&](int e, const Piece& u) {
+        int t, i;
+        place(e, t, i);
         uint8_t* q = data + (long long)(held + t) * c.token[w] + i;
-        if constexpr (WIDE) *reinterpret_cast<uint2*>(q) = make_uint2(to_e4m3x4(v[0], v[1], v[2], v[3]), to_e4m3x4(v[4], v[5], v[6], v[7]));
-        else *q = (uint8_t)to_e4m3x4(v[0], 0.f, 0.f, 0.f);
+        if constexpr (WIDE) {
+            uint2 out;
+            if (power) out = odd ? u.template bytes<false>(0, inv) : u.template bytes<true>(0, inv);
+            else {
+                const float2 p0 = u.pair(0), p1 = u.pair(1), p2 = u.pair(2), p3 = u.pair(3);
+                out.x = to_e4m3x4(__fdiv_rn(p0.x, s), __fdiv_rn(p0.y, s), __fdiv_rn(p1.x, s), __fdiv_rn(p1.y, s));
+                out.y = to_e4m3x4(__fdiv_rn(p2.x, s), __fdiv_rn(p2.y, s), __fdiv_rn(p3.x, s), __fdiv_rn(p3.y, s));
+            }
+            *reinterpret_cast<uint2*>(q) = out;
+        } else *q = (uint8_t)to_e4m3x4(power ? u.v * inv : __fdiv_rn(u.v, s), 0.f, 0.f, 0.f);
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) put(me + k * kThreads, v[k]);
+    for (int e = me + kHeld * kThreads; e < total; e += kThreads) {
+        Piece u;
+        load(e, u);
+        put(e, u);
     }
 }
 
@@ -802,14 +842,13 @@ extern "C" tt_status tt_cache_append(const tt_cache_append_args* a, void* stream
     }
     const long long units = a->tokens / c.block + 2ll * c.batch;
     if (units > 0x7fffffff) return TT_ERR_INVALID_ARG;
-    // A warp has a page's tokens where there is hardly more than one of them, eight warps where there are many.
-    const long long values = (long long)(a->tokens / c.batch < c.block ? a->tokens / c.batch : c.block) * c.d;
-    const int threads = values <= 512 ? 32 : values <= 2048 ? 128 : 256;
-    const dim3 grid((unsigned)units, 2u * (unsigned)c.heads, 1);
-    const auto go = [&](auto kern) { return status_of(launch(kern, grid, threads, 0, 1, stream, *a)); };
-    if (a->type == TT_TYPE_F32) return wide ? go(tt_cache_append_kernel<TT_TYPE_F32, true>) : go(tt_cache_append_kernel<TT_TYPE_F32, false>);
-    if (a->type == TT_TYPE_F16) return wide ? go(tt_cache_append_kernel<TT_TYPE_F16, true>) : go(tt_cache_append_kernel<TT_TYPE_F16, false>);
-    return wide ? go(tt_cache_append_kernel<TT_TYPE_BF16, true>) : go(tt_cache_append_kernel<TT_TYPE_BF16, false>);
+    // A warp has a page's tokens where there is hardly more than one of them, a CTA where there are many.
+    const bool warp = (long long)(a->tokens / c.batch < c.block ? a->tokens / c.batch : c.block) * c.d <= 1024;
+    const dim3 grid((unsigned)units, warp ? (2u * (unsigned)c.heads + 7u) / 8u : 2u * (unsigned)c.heads, 1);
+    const auto go = [&](auto by_warp, auto by_cta) { return status_of(launch(warp ? by_warp : by_cta, grid, 256, 0, 1, stream, *a)); };
+#define TT_APPEND(TYPE) (wide ? go(tt_cache_append_kernel<TYPE, true, true>, tt_cache_append_kernel<TYPE, true, false>) : go(tt_cache_append_kernel<TYPE, false, true>, tt_cache_append_kernel<TYPE, false, false>))
+    return a->type == TT_TYPE_F32 ? TT_APPEND(TT_TYPE_F32) : a->type == TT_TYPE_F16 ? TT_APPEND(TT_TYPE_F16) : TT_APPEND(TT_TYPE_BF16);
+#undef TT_APPEND
 }
 
 extern "C" tt_status tt_cache_attention_workspace(const tt_cache_attention_args* a, int64_t* bytes) {

@@ -12,6 +12,13 @@ __device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(sta
 __device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
     const int lane = threadIdx.x & 31;
     const auto begin = [&](int b) { return starts[b] * mul / per + (long long)extra * b; };
+    if (batch <= 128) {                                      // all places at once
+        int in = 0;
+#pragma unroll
+        for (int i = 0; i < 128; i += 32) in += __popc(__ballot_sync(0xffffffffu, i + lane < batch && begin(i + lane) <= unit));
+        first = begin(max(0, in - 1));
+        return max(0, in - 1);
+    }
     int lo = 0, n = batch;                                   // it is one of lo .. lo + n - 1
     while (n > 1) {
         const int step = (n + 31) / 32, b = lo + lane * step;

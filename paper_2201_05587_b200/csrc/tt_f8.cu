@@ -12,47 +12,51 @@ namespace tt {
 // s = 2^ceil(log2(max |x| / 448)) comes from the bits of the maximum, x / s is a product with the power 1 / s, so the only rounding is the
 // one to e4m3.  Bound by memory: every value is read once and kept in registers between the maximum and the conversion.
 
-// Rows of activations: 16 lanes have a block of 128 columns, 8 values each; a warp has UNROLL * 256 columns of one row in flight.
-template <int TYPE, int UNROLL>
-__global__ void __launch_bounds__(256) tt_quantize_rows_kernel(const tt_quantize_args a, int pieces, long long tasks, int wide) {
+// Rows of activations: a warp has one block of columns of eight rows, of four at a time, so that the scales of a block come out side by side.  Eight
+// lanes have a row's block, 8 values of either half each (a warp's loads are whole lines).
+template <int TYPE>
+__global__ void __launch_bounds__(256) tt_quantize_rows_kernel(const tt_quantize_args a, int blocks, long long tasks, int wide) {
     pdl_allow_next();
     pdl_wait_prev();
     const int lane = threadIdx.x & 31;
     const long long task = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     if (task >= tasks) return;
     typedef typename Element<TYPE>::type T;
-    const long long row = task / pieces;
-    const int first = (int)(task - row * pieces) * (256 * UNROLL) + 8 * lane;
-    const T* x = static_cast<const T*>(a.x) + row * a.x_row;
-    uint8_t* q = static_cast<uint8_t*>(a.q) + row * a.q_row;
-    float v[UNROLL][8];
+    const long long row8 = task / blocks;
+    const int block = (int)(task - row8 * blocks), c = block * 128 + 8 * (lane & 7);
+    const long long row0 = row8 * 8 + (lane >> 3);
+    Eights<TYPE, 2> v[2];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int c = first + 256 * u;
-        if (wide && c + 8 <= a.kk) load_wide<TYPE, 8>(x + c, v[u]);
-        else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[u][i] = c + i < a.kk ? Element<TYPE>::up(x[c + i]) : 0.f;
-        }
+    for (int u = 0; u < 2; ++u) {
+        if (row0 + 4 * u < a.m) v[u].load(static_cast<const T*>(a.x) + (row0 + 4 * u) * a.x_row, c, 64, a.kk, wide);
+        else v[u].zero();
     }
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int c = first + 256 * u;
-        float most = 0.f;
+    for (int u = 0; u < 2; ++u) {
+        const long long row = row0 + 4 * u;
+        float most = v[u].most();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = finite_max(most, v[u][i]);
+        for (int d = 4; d > 0; d >>= 1) most = __uint_as_float(max(__float_as_uint(most), __float_as_uint(__shfl_xor_sync(0xffffffffu, most, d))));      // (NaN is the largest)
+        const bool finite = most < INFINITY;
+        if (__any_sync(0xffffffffu, !finite)) {
+            most = v[u].finite_most();
 #pragma unroll
-        for (int d = 8; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-        const float s = power_scale(most), inv = power_inverse(s);
-        if (c >= a.kk) continue;
-        const uint32_t lo = to_e4m3x4(v[u][0] * inv, v[u][1] * inv, v[u][2] * inv, v[u][3] * inv);
-        const uint32_t hi = to_e4m3x4(v[u][4] * inv, v[u][5] * inv, v[u][6] * inv, v[u][7] * inv);
-        if (wide && c + 8 <= a.kk) *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
-        else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) if (c + i < a.kk) q[c + i] = (uint8_t)((i < 4 ? lo : hi) >> (8 * (i & 3)));
+            for (int d = 4; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
         }
-        if ((lane & 15) == 0) a.scales[(long long)(c >> 7) * a.s_block + row * a.s_row] = s;
+        const float s = power_scale(most), inv = power_inverse(s);
+        if (row >= a.m) continue;
+        uint8_t* q = static_cast<uint8_t*>(a.q) + row * a.q_row;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint2 w = finite ? v[u].template bytes<true>(h, inv) : v[u].template bytes<false>(h, inv);
+            const int at = c + 64 * h;
+            if (wide && at + 8 <= a.kk) *reinterpret_cast<uint2*>(q + at) = w;
+            else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) if (at + i < a.kk) q[at + i] = (uint8_t)((i < 4 ? w.x : w.y) >> (8 * (i & 3)));
+            }
+        }
+        if ((lane & 7) == 0) a.scales[block * a.s_block + row * a.s_row] = s;
     }
 }
 
@@ -718,14 +722,11 @@ extern "C" tt_status tt_quantize(const tt_quantize_args* a, void* stream) {
         const auto kern = a->x_type == TT_TYPE_F32 ? tt_quantize_blocks_kernel<TT_TYPE_F32> : a->x_type == TT_TYPE_F16 ? tt_quantize_blocks_kernel<TT_TYPE_F16> : tt_quantize_blocks_kernel<TT_TYPE_BF16>;
         return status_of(launch(kern, dim3((unsigned)grid, 1, 1), 256, 0, 1, stream, *a, blocks, wide));
     }
-    // Four loads in flight per lane, where that leaves every SM some warps; few rows are spread over as many warps as they have.
-    const bool deep = (long long)a->m * a->kk >= (1 << 21);
-    const int step = deep ? 1024 : 256, pieces = (a->kk + step - 1) / step, threads = deep ? 256 : 64;
-    const long long tasks = (long long)a->m * pieces, grid = (tasks + threads / 32 - 1) / (threads / 32);
+    // (few tasks: a warp to a CTA, so that they are spread over the SMs)
+    const long long tasks = (a->m + 7ll) / 8 * blocks, grid_threads = tasks < 8ll * kSms ? 32 : 256, grid = (tasks * 32 + grid_threads - 1) / grid_threads;
     if (grid > 0x7fffffff) return TT_ERR_INVALID_ARG;
-    const auto kern = deep ? (a->x_type == TT_TYPE_F32 ? tt_quantize_rows_kernel<TT_TYPE_F32, 4> : a->x_type == TT_TYPE_F16 ? tt_quantize_rows_kernel<TT_TYPE_F16, 4> : tt_quantize_rows_kernel<TT_TYPE_BF16, 4>)
-                           : (a->x_type == TT_TYPE_F32 ? tt_quantize_rows_kernel<TT_TYPE_F32, 1> : a->x_type == TT_TYPE_F16 ? tt_quantize_rows_kernel<TT_TYPE_F16, 1> : tt_quantize_rows_kernel<TT_TYPE_BF16, 1>);
-    return status_of(launch(kern, dim3((unsigned)grid, 1, 1), threads, 0, 1, stream, *a, pieces, tasks, wide));
+    const auto kern = a->x_type == TT_TYPE_F32 ? tt_quantize_rows_kernel<TT_TYPE_F32> : a->x_type == TT_TYPE_F16 ? tt_quantize_rows_kernel<TT_TYPE_F16> : tt_quantize_rows_kernel<TT_TYPE_BF16>;
+    return status_of(launch(kern, dim3((unsigned)grid, 1, 1), (int)grid_threads, 0, 1, stream, *a, blocks, tasks, wide));
 }
 
 extern "C" tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* stream) {

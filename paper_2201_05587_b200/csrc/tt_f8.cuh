@@ -107,17 +107,96 @@ __device__ __forceinline__ float power_scale(float most) {
 // 1 / s of such a power, which is exact (s is at most 2^120).
 __device__ __forceinline__ float power_inverse(float s) { return __int_as_float((254 << 23) - __float_as_int(s)); }
 
-// Four values -> four e4m3 bytes, the first in the low byte.  Infinities, which the conversion would bring to 448, become NaN.
-__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {
-    const auto fine = [](float v) { return fabsf(v) < INFINITY ? v : __int_as_float(0x7fffffff); };
+// Four finite values -> four e4m3 bytes, the first in the low byte.
+__device__ __forceinline__ uint32_t finite_to_e4m3x4(float a, float b, float c, float d) {
     uint32_t w;
     asm("{\n\t.reg .b16 lo, hi;\n\t"
         "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\t"
         "cvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
         "mov.b32 %0, {lo, hi};\n\t}"
-        : "=r"(w) : "f"(fine(a)), "f"(fine(b)), "f"(fine(c)), "f"(fine(d)));
+        : "=r"(w) : "f"(a), "f"(b), "f"(c), "f"(d));
     return w;
 }
+// The same of any values: infinities, which the conversion would bring to 448, become NaN.
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {
+    const auto fine = [](float v) { return fabsf(v) < INFINITY ? v : __int_as_float(0x7fffffff); };
+    return finite_to_e4m3x4(fine(a), fine(b), fine(c), fine(d));
+}
+// N times eight values as they lie in memory.  Magnitudes of 16-bit types are compared as integers, in pairs; values that are all finite, as they
+// nearly always are, need no look at each.
+template <int TYPE, int N>
+struct Eights {
+    uint4 raw[N * (TYPE == TT_TYPE_F32 ? 2 : 1)];
+
+    // Values c .. c + 7, c + step .. c + step + 7, ... of a row of n (zeros behind it).
+    __device__ __forceinline__ void load(const typename Element<TYPE>::type* x, int c, int step, int n, bool wide) {
+        constexpr int kPer = 16 / type_bytes(TYPE);
+#pragma unroll
+        for (int h = 0; h < N; ++h)
+#pragma unroll
+            for (int q = 0; q < 8 / kPer; ++q) {
+                const int at = c + step * h + q * kPer;
+                uint4& w = raw[h * (8 / kPer) + q];
+                if (wide && at + kPer <= n) w = *reinterpret_cast<const uint4*>(x + at);
+                else {
+                    uint32_t u[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        if (at + i >= n) continue;
+                        if constexpr (TYPE == TT_TYPE_F32) u[i] = __float_as_uint(x[at + i]);
+                        else u[i >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(x)[at + i] << (16 * (i & 1));
+                    }
+                    w = make_uint4(u[0], u[1], u[2], u[3]);
+                }
+            }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (uint4& w : raw) w = make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ float2 pair(int i) const {                  // values 2 i, 2 i + 1
+        if constexpr (TYPE == TT_TYPE_F32) {
+            const uint4& w = raw[i >> 1];
+            return i & 1 ? make_float2(__uint_as_float(w.z), __uint_as_float(w.w)) : make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+        } else {
+            const uint4& w = raw[i >> 2];
+            return up2<TYPE>((i & 3) == 0 ? w.x : (i & 3) == 1 ? w.y : (i & 3) == 2 ? w.z : w.w);
+        }
+    }
+    // The largest magnitude, infinities and NaN included.
+    __device__ __forceinline__ float most() const {
+        if constexpr (TYPE == TT_TYPE_F32) {
+            uint32_t m = 0u;
+#pragma unroll
+            for (const uint4& w : raw) m = max(max(m, max(w.x & 0x7fffffffu, w.y & 0x7fffffffu)), max(w.z & 0x7fffffffu, w.w & 0x7fffffffu));
+            return __uint_as_float(m);
+        } else {
+            uint32_t m = 0u;
+#pragma unroll
+            for (const uint4& w : raw) m = __vmaxu2(__vmaxu2(__vmaxu2(m, w.x & 0x7fff7fffu), w.y & 0x7fff7fffu), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
+            const uint32_t one = max(m & 0xffffu, m >> 16);
+            return up2<TYPE>(one).x;
+        }
+    }
+    __device__ __forceinline__ float finite_most() const {
+        float m = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) { const float2 v = pair(i); m = finite_max(finite_max(m, v.x), v.y); }
+        return m;
+    }
+    // The bytes of eight h, times inv.
+    template <bool FINITE>
+    __device__ __forceinline__ uint2 bytes(int h, float inv) const {
+        uint32_t w[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const float2 a = pair(4 * h + 2 * q), b = pair(4 * h + 2 * q + 1);
+            w[q] = FINITE ? finite_to_e4m3x4(a.x * inv, a.y * inv, b.x * inv, b.y * inv) : to_e4m3x4(a.x * inv, a.y * inv, b.x * inv, b.y * inv);
+        }
+        return make_uint2(w[0], w[1]);
+    }
+};
+
 // Two e4m3 bytes (of the low half word) -> two values in one word of 16-bit floating point, which holds every e4m3 value.
 __device__ __forceinline__ uint32_t f16x2_of_e4m3(uint32_t two) {
     uint32_t h;

@@ -29,6 +29,42 @@ __device__ __forceinline__ void rotary_turn(long long p, unsigned long long turn
     s *= inverse ? -factor : factor;
 }
 
+__device__ __forceinline__ long long position(const tt_rotary_args& a, int token) {
+    return a.position_bits == 64 ? static_cast<const long long*>(a.positions)[token] : (long long)static_cast<const int*>(a.positions)[token];
+}
+
+// 16 bytes of pairs side by side, or of their first and of their second values.
+template <int TYPE, bool INTERLEAVED, int PAIRS>
+__device__ __forceinline__ void turn_piece(uint4* w, const float (&c)[PAIRS], const float (&s)[PAIRS]) {
+    const auto word = [&](int part, int i) -> uint32_t& { return i == 0 ? w[part].x : i == 1 ? w[part].y : i == 2 ? w[part].z : w[part].w; };
+    if constexpr (INTERLEAVED) {
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) {
+            if constexpr (TYPE == TT_TYPE_F32) {
+                const float a = __uint_as_float(word(0, 2 * i)), b = __uint_as_float(word(0, 2 * i + 1));
+                word(0, 2 * i) = __float_as_uint(a * c[i] - b * s[i]);
+                word(0, 2 * i + 1) = __float_as_uint(b * c[i] + a * s[i]);
+            } else {
+                const float2 v = up2<TYPE>(word(0, i));
+                word(0, i) = down2<TYPE>(v.x * c[i] - v.y * s[i], v.y * c[i] + v.x * s[i]);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (TYPE == TT_TYPE_F32) {
+                const float a = __uint_as_float(word(0, i)), b = __uint_as_float(word(1, i));
+                word(0, i) = __float_as_uint(a * c[i] - b * s[i]);
+                word(1, i) = __float_as_uint(b * c[i] + a * s[i]);
+            } else {
+                const float2 a = up2<TYPE>(word(0, i)), b = up2<TYPE>(word(1, i));
+                word(0, i) = down2<TYPE>(a.x * c[2 * i] - b.x * s[2 * i], a.y * c[2 * i + 1] - b.y * s[2 * i + 1]);
+                word(1, i) = down2<TYPE>(b.x * c[2 * i] + a.x * s[2 * i], b.y * c[2 * i + 1] + a.y * s[2 * i + 1]);
+            }
+        }
+    }
+}
+
 // V values a piece: 16 bytes, or one (one pair, where values lie at no better than their own size).
 template <int TYPE, int V, bool INTERLEAVED>
 __global__ void __launch_bounds__(128) tt_rotary_kernel(const Rotary g) {
@@ -36,65 +72,77 @@ __global__ void __launch_bounds__(128) tt_rotary_kernel(const Rotary g) {
     pdl_wait_prev();
     typedef typename Element<TYPE>::type T;
     constexpr int kPairs = V == 1 ? 1 : INTERLEAVED ? V / 2 : V;       // pairs of a piece
-    constexpr int kLoad = V == 1 ? 2 : INTERLEAVED ? V : 2 * V;        // ... and its values
     const long long t = (long long)blockIdx.x * blockDim.x + threadIdx.x;
     if (t >= g.threads) return;
     const int unit = (int)(t % g.units);
     const long long rest = t / g.units;
     const int h0 = (int)(rest % g.head_step), token = (int)(rest / g.head_step), half = g.a.rot >> 1;
     const bool turned = unit < g.rot_units;
-    float c[kPairs], s[kPairs];
-    if (turned) {
-        const long long p = g.a.position_bits == 64 ? static_cast<const long long*>(g.a.positions)[token] : (long long)static_cast<const int*>(g.a.positions)[token];
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) rotary_turn(p, g.a.turns[unit * kPairs + i], g.a.factor, g.a.inverse != 0, c[i], s[i]);
-    }
     const int all = g.a.heads[0] + g.a.heads[1];
-    if (turned) {
-        const int at = INTERLEAVED ? unit * 2 * kPairs : unit * kPairs;            // the piece's first value; of halves, the second part's at + half
-#pragma unroll 2
+    // of head h, the piece's first value; in halves, the second part's are `half` further on
+    const int at = !turned ? g.a.rot + (unit - g.rot_units) * V : INTERLEAVED ? unit * 2 * kPairs : unit * kPairs;
+    const auto from = [&](int h) {
+        const int w = h >= g.a.heads[0] ? 1 : 0;
+        return static_cast<const T*>(g.a.x[w]) + ((long long)token * g.a.x_token[w] + (long long)(h - (w ? g.a.heads[0] : 0)) * g.a.x_head[w] + at);
+    };
+    const auto to = [&](int h) {
+        const int w = h >= g.a.heads[0] ? 1 : 0;
+        return static_cast<T*>(g.a.y[w]) + ((long long)token * g.a.y_token[w] + (long long)(h - (w ? g.a.heads[0] : 0)) * g.a.y_head[w] + at);
+    };
+    if constexpr (V == 1) {
+        float c[1], s[1];
+        if (turned) rotary_turn(position(g.a, token), g.a.turns[unit], g.a.factor, g.a.inverse != 0, c[0], s[0]);
         for (int h = h0; h < all; h += g.head_step) {
-            const int w = h >= g.a.heads[0] ? 1 : 0, hh = h - (w ? g.a.heads[0] : 0);
-            const T* x = static_cast<const T*>(g.a.x[w]) + (long long)token * g.a.x_token[w] + (long long)hh * g.a.x_head[w] + at;
-            T* y = static_cast<T*>(g.a.y[w]) + (long long)token * g.a.y_token[w] + (long long)hh * g.a.y_head[w] + at;
-            float v[kLoad];
-            if constexpr (V == 1) {
-                v[0] = Element<TYPE>::up(x[0]);
-                v[1] = Element<TYPE>::up(x[INTERLEAVED ? 1 : half]);
-                y[0] = Element<TYPE>::down(v[0] * c[0] - v[1] * s[0]);
-                y[INTERLEAVED ? 1 : half] = Element<TYPE>::down(v[1] * c[0] + v[0] * s[0]);
-            } else if constexpr (INTERLEAVED) {
-                load_wide<TYPE, V>(x, v);
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const float a = v[2 * i], b = v[2 * i + 1];
-                    v[2 * i] = a * c[i] - b * s[i];
-                    v[2 * i + 1] = b * c[i] + a * s[i];
-                }
-                store_wide<TYPE, V>(y, v);
-            } else {
-                float a[V], b[V];
-                load_wide<TYPE, V>(x, a);
-                load_wide<TYPE, V>(x + half, b);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float u = a[i] * c[i] - b[i] * s[i];
-                    b[i] = b[i] * c[i] + a[i] * s[i];
-                    a[i] = u;
-                }
-                store_wide<TYPE, V>(y, a);
-                store_wide<TYPE, V>(y + half, b);
-            }
+            const T* x = from(h);
+            T* y = to(h);
+            if (turned) {
+                const int other = INTERLEAVED ? 1 : half;
+                const float a = Element<TYPE>::up(x[0]), b = Element<TYPE>::up(x[other]);
+                y[0] = Element<TYPE>::down(a * c[0] - b * s[0]);
+                y[other] = Element<TYPE>::down(b * c[0] + a * s[0]);
+            } else *y = *x;
         }
     } else {
-        const int at = g.a.rot + (unit - g.rot_units) * V;
-#pragma unroll 4
-        for (int h = h0; h < all; h += g.head_step) {
-            const int w = h >= g.a.heads[0] ? 1 : 0, hh = h - (w ? g.a.heads[0] : 0);
-            const T* x = static_cast<const T*>(g.a.x[w]) + (long long)token * g.a.x_token[w] + (long long)hh * g.a.x_head[w] + at;
-            T* y = static_cast<T*>(g.a.y[w]) + (long long)token * g.a.y_token[w] + (long long)hh * g.a.y_head[w] + at;
-            if constexpr (V == 1) *y = *x;
-            else *reinterpret_cast<uint4*>(y) = *reinterpret_cast<const uint4*>(x);
+        // kBatch heads are under way at a time, the first ones while the sines are taken
+        constexpr int kParts = INTERLEAVED ? 1 : 2, kBatch = INTERLEAVED ? 4 : 2;
+        uint4 v[kBatch][kParts];
+        const auto load = [&](int h) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i, h += g.head_step) {
+                if (h >= all) break;
+                const T* x = from(h);
+                v[i][0] = *reinterpret_cast<const uint4*>(x);
+                if (kParts == 2 && turned) v[i][kParts - 1] = *reinterpret_cast<const uint4*>(x + half);
+            }
+        };
+        load(h0);
+        float c[kPairs], s[kPairs];
+        if (turned) {
+            const long long p = position(g.a, token);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) rotary_turn(p, g.a.turns[unit * kPairs + i], g.a.factor, g.a.inverse != 0, c[i], s[i]);
+        }
+        for (int h = h0; h < all;) {
+            const int first = h;
+            uint4 w[kBatch][kParts];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+#pragma unroll
+                for (int j = 0; j < kParts; ++j) w[i][j] = v[i][j];
+            h += kBatch * g.head_step;
+            load(h);
+            if (turned) {
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) turn_piece<TYPE, INTERLEAVED, kPairs>(w[i], c, s);
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int hh = first + i * g.head_step;
+                if (hh >= all) break;
+                T* y = to(hh);
+                *reinterpret_cast<uint4*>(y) = w[i][0];
+                if (kParts == 2 && turned) *reinterpret_cast<uint4*>(y + half) = w[i][kParts - 1];
+            }
         }
     }
 }
