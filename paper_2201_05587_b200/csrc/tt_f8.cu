@@ -152,12 +152,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* v) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr));
 }
-__device__ __forceinline__ float4 ld_cluster_v4f(uint32_t addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 // apply_act, but for NaN, which stays NaN (a NaN operand is to show).
 __device__ __forceinline__ float activate(float v, int act) {
     if (act == TT_ACT_GELU_ERF) return gelu_erf(v);
@@ -172,7 +166,7 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     constexpr int kCols = TN / 2;                          // columns of a read-out warp
     constexpr uint32_t kStage = kF8TileA + TN * 128u;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[kBufs], acc_empty[kBufs], drained;
+    __shared__ uint64_t full_bar[kF8MaxStages], empty_bar[kF8MaxStages], acc_full[kBufs], acc_empty[kBufs], drained, red_bar;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -181,6 +175,11 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     const int tile_a = (int)blockIdx.x % g.tiles_a, tile_b = (int)blockIdx.x / g.tiles_a;
     const int kb0 = (int)blockIdx.z * g.blocks_per_split, kb1 = min(g.blocks, kb0 + g.blocks_per_split);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // what a CTA of a cluster of `split` adds up in the end: a band of lines of the tile, SWAP: a column of 128 rows each, else a row of TN columns (+ 4)
+    constexpr uint32_t kLine = SWAP ? 512u : (TN + 4) * 4u;
+    constexpr int kLines = SWAP ? TN : 128;
+    const int per = kLines / g.split;
+    const uint32_t band_bytes = (uint32_t)per * kLine, landing = base + (uint32_t)g.stages * kStage;
     if (threadIdx.x == 32) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmap_b) : "memory");
@@ -189,23 +188,30 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
         for (int i = 0; i < g.stages; ++i) { mbar_init(smem_u32(&full_bar[i]), 1u); mbar_init(smem_u32(&empty_bar[i]), 1u); }
         for (int i = 0; i < kBufs; ++i) { mbar_init(smem_u32(&acc_full[i]), 1u); mbar_init(smem_u32(&acc_empty[i]), 8u); }
         mbar_init(smem_u32(&drained), 1u);
+        mbar_init(smem_u32(&red_bar), 1u);
         abort_flag = 0;
         fence_mbar_init();
+        if (g.split > 1) mbar_expect_tx(smem_u32(&red_bar), (uint32_t)(g.split - 1) * band_bytes);
         fence_proxy_async_shared();
     }
+    __syncthreads();
+    if (g.split > 1) cluster_arrive();                      // (this CTA's barriers and landing place exist)
     // Tensor memory is taken behind the wait for the launch in front and before the next one may begin: a CTA that waits for a launch holds none that
-    // the launch could be waiting for.
+    // the launch could be waiting for.  The copies do not wait for it.
     pdl_wait_prev();
     constexpr uint32_t kTmemCols = kBufs * TN < 32 ? 32 : kBufs * TN;
-    if (warp == 1) {
-        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
-        tmem_relinquish();
+    uint32_t tmem_base = 0u;
+    if (warp > 0) {
+        if (warp == 1) {
+            tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
+            tmem_relinquish();
+        }
+        tc_fence_before();
+        asm volatile("bar.sync 1, %0;" ::"n"(kF8Threads - 32) : "memory");
+        tc_fence_after();
+        tmem_base = *(volatile uint32_t*)&tmem_slot;
+        pdl_allow_next();
     }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem_base = *(volatile uint32_t*)&tmem_slot;
-    pdl_allow_next();
 
     float acc[kCols];
 #pragma unroll
@@ -326,10 +332,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             }
         }
     } else {
-        // partial sums to shared memory (the pipeline is idle: the last block's products are done with it), SWAP: [column][128 rows], else
-        // [row][TN + 4]
-        constexpr uint32_t kLine = SWAP ? 512u : (TN + 4) * 4u;
-        __syncthreads();
+        // Partial sums to shared memory (the pipeline is idle: the last block's products are done with it), every peer's band to it in one copy
+        // (loads from a peer's shared memory run at some 10 bytes a cycle), and this CTA's band added up as the others' arrive.
+        const uint32_t me = (uint32_t)blockIdx.z;
         if (warp >= 2) {
             const uint32_t r = (uint32_t)(quad * 32 + lane);
             if constexpr (SWAP) {
@@ -339,21 +344,26 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 #pragma unroll
                 for (int j = 0; j < kCols; j += 4) st_shared_v4(base + r * kLine + (uint32_t)(half * kCols + j) * 4u, acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
             }
+            fence_proxy_async_shared();
+            asm volatile("bar.sync 2, 256;" ::: "memory");
         }
-        cluster_arrive();
-        cluster_wait();
-        if (warp >= 2 && !*abortp) {
-            // a band of lines for each CTA of the cluster, four values at a time
-            constexpr int kLines = SWAP ? TN : 128, kQuads = SWAP ? 32 : TN / 4;
-            const int per = (kLines + g.split - 1) / g.split, l0 = (int)blockIdx.z * per, l1 = min(kLines, l0 + per);
-            for (int e = (int)threadIdx.x - 64 + l0 * kQuads; e < l1 * kQuads; e += 256) {
-                const int line = e / kQuads, c = 4 * (e - line * kQuads);
+        __syncwarp();
+        cluster_wait();                                     // the peers are there
+        if (warp == 2 && lane < g.split && lane != (int)me && !*abortp) {
+            const uint32_t slot = me < (uint32_t)lane ? me : me - 1u;
+            bulk_copy_to_peer(map_to_peer(landing + slot * band_bytes, (uint32_t)lane), base + (uint32_t)lane * band_bytes, band_bytes, map_to_peer(smem_u32(&red_bar), (uint32_t)lane));
+        }
+        __syncwarp();
+        if (warp >= 2 && __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&red_bar), 0u, abortp, g.status, 5u, g.wait_ns))) {
+            constexpr int kQuads = SWAP ? 32 : TN / 4;       // four values at a time
+            for (int e = (int)threadIdx.x - 64; e < per * kQuads; e += 256) {
+                const int in = e / kQuads, c = 4 * (e - in * kQuads), line = (int)me * per + in;
                 const int token = (SWAP ? tile_b * TN : tile_a * 128) + line, col = (SWAP ? tile_a * 128 : tile_b * TN) + c;
                 const int tokens = SWAP ? g.rows_b : g.rows_a, cols = SWAP ? g.rows_a : g.rows_b;
                 if (token >= tokens || col >= cols) continue;
                 float v[4] = {0.f, 0.f, 0.f, 0.f};
-                for (int p = 0; p < g.split; ++p) {
-                    const float4 f = ld_cluster_v4f(map_to_peer(base + (uint32_t)line * kLine + (uint32_t)c * 4u, (uint32_t)p));
+                for (uint32_t p = 0; p < (uint32_t)g.split; ++p) {          // (in the order of the splits)
+                    const float4 f = ld_shared_v4f((p == me ? base + me * band_bytes : landing + (p < me ? p : p - 1u) * band_bytes) + (uint32_t)in * kLine + (uint32_t)c * 4u);
                     v[0] += f.x; v[1] += f.y; v[2] += f.z; v[3] += f.w;
                 }
                 const long long at = (long long)token * g.y_row + col;
@@ -372,7 +382,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 }
             }
         }
-        cluster_arrive();                                   // nobody leaves while its sums may still be read
+        if (warp == 2) bulk_copies_done();
+        __syncwarp();
+        cluster_arrive();                                   // nobody leaves while a copy may be on its way to it
         cluster_wait();
     }
     tc_fence_before();
@@ -665,10 +677,11 @@ static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb,
     // SWAP takes half of an SM's shared memory: two CTAs fit, of this launch or the next one's, whose set-up then runs while this one's sums are
     // joined; their columns of tensor memory fit together.  The other form takes all columns and so most of the shared memory: beside a CTA that
     // holds some it would wait for them, and CTAs of two clusters that wait so for each other would do it forever.
-    const int fits = ((SWAP ? kHalfSm : kDynSmemLimit) - 1024) / kStageBytes;
+    const int landing = g.split > 1 ? (SWAP ? TN * 512 : 128 * (TN + 4) * 4) / g.split * (g.split - 1) : 0;      // the peers' bands
+    const int fits = ((SWAP ? kHalfSm : kDynSmemLimit) - 1024 - landing) / kStageBytes;
     g.stages = fits < kF8MaxStages ? fits : kF8MaxStages;
     const int tiles_b = (g.rows_b + TN - 1) / TN;
-    return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes, g.split, stream, ta, tb, g);
+    return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes + landing, g.split, stream, ta, tb, g);
 }
 
 // Columns of a pair's tile, or 0 for CTAs on their own: what takes the fewest rounds of the SMs, by what a tile costs.
