@@ -304,7 +304,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 
     // ---- out: y[token][column of the weights] ----
     const int first_col = tile_b * TN + half * kCols;
-    if (g.split == 1) {
+    // (32 columns of a row, 64 bytes or more, leave as well from their lane as by way of shared memory, and sooner; 64 take 2 us longer that way)
+    constexpr bool kAlone = !SWAP && TN <= 32;
+    if ((SWAP || kAlone) && g.split == 1) {
         if (warp >= 2 && !*abortp) {
             const int row = tile_a * 128 + quad * 32 + lane;
             if constexpr (SWAP) {
@@ -332,8 +334,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             }
         }
     } else {
-        // Partial sums to shared memory (the pipeline is idle: the last block's products are done with it), every peer's band to it in one copy
-        // (loads from a peer's shared memory run at some 10 bytes a cycle), and this CTA's band added up as the others' arrive.
+        // Sums to shared memory (the pipeline is idle: the last block's products are done with it), every peer's band of them to it in one copy
+        // (loads from a peer's shared memory run at some 10 bytes a cycle), and this CTA's band added up as the others' arrive.  A tile that is
+        // not split goes this way too, so that rows leave as rows.
         const uint32_t me = (uint32_t)blockIdx.z;
         if (warp >= 2) {
             const uint32_t r = (uint32_t)(quad * 32 + lane);
@@ -348,13 +351,13 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             asm volatile("bar.sync 2, 256;" ::: "memory");
         }
         __syncwarp();
-        cluster_wait();                                     // the peers are there
+        if (g.split > 1) cluster_wait();                    // the peers are there
         if (warp == 2 && lane < g.split && lane != (int)me && !*abortp) {
             const uint32_t slot = me < (uint32_t)lane ? me : me - 1u;
             bulk_copy_to_peer(map_to_peer(landing + slot * band_bytes, (uint32_t)lane), base + (uint32_t)lane * band_bytes, band_bytes, map_to_peer(smem_u32(&red_bar), (uint32_t)lane));
         }
         __syncwarp();
-        if (warp >= 2 && __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&red_bar), 0u, abortp, g.status, 5u, g.wait_ns))) {
+        if (warp >= 2 && (g.split == 1 ? !*abortp : __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&red_bar), 0u, abortp, g.status, 5u, g.wait_ns)))) {
             constexpr int kQuads = SWAP ? 32 : TN / 4;       // four values at a time
             for (int e = (int)threadIdx.x - 64; e < per * kQuads; e += 256) {
                 const int in = e / kQuads, c = 4 * (e - in * kQuads), line = (int)me * per + in;
@@ -382,10 +385,11 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 }
             }
         }
-        if (warp == 2) bulk_copies_done();
-        __syncwarp();
-        cluster_arrive();                                   // nobody leaves while a copy may be on its way to it
-        cluster_wait();
+        if (g.split > 1) {
+            __syncwarp();
+            cluster_arrive();                               // nobody leaves while a copy may be on its way to it
+            cluster_wait();
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -596,7 +600,11 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
             if (!ok) break;
             if (g.bias) {
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) acc[j] += __ldg(g.bias + min(col0 + j, g.rows_b - 1));
+                for (int part32 = 0; part32 < kCols; part32 += 32) {
+                    const float b = __ldg(g.bias + min(col0 + part32 + lane, g.rows_b - 1));
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) acc[part32 + j] += __shfl_sync(0xffffffffu, b, j);
+                }
             }
             if (g.act == TT_ACT_GELU_ERF) {
 #pragma unroll
@@ -684,13 +692,31 @@ static cudaError_t launch_dense_f8(const CUtensorMap& ta, const CUtensorMap& tb,
     return launch(tt_dense_f8_kernel<TN, SWAP>, dim3((unsigned)(g.tiles_a * tiles_b), 1, (unsigned)g.split), kF8Threads, 1024 + (size_t)g.stages * kStageBytes + landing, g.split, stream, ta, tb, g);
 }
 
-// Columns of a pair's tile, or 0 for CTAs on their own: what takes the fewest rounds of the SMs, by what a tile costs.
-static int pair_columns(long long m, long long n) {
-    const long long rows = (m + 255) / 256;
-    const auto rounds = [](long long tiles, long long at_once) { return (tiles + at_once - 1) / at_once; };
-    const long long wide = rounds(rows * ((n + 255) / 256), kSms / 2) * 56, narrow = rounds(rows * ((n + 127) / 128), kSms / 2) * 34;
-    const long long alone = rounds((m + 127) / 128 * ((n + 127) / 128), kSms) * 34;
-    return alone < wide && alone < narrow ? 0 : wide <= narrow ? 256 : 128;
+// The forms that the layer is built in, and what they cost, in microseconds on a B200: fitted to 30 layers of 8 to 8192 tokens, 128 to 14336 columns
+// and 1000 to 8192 products under every form and split.  A launch takes kLaunch; a block of 128 products of a tile takes `block` (what the L2 gives an SM
+// is the bound); the exchange of splits and the way out are a tile's; what does not fit the SMs at once comes later, and with the next CTA's set-up.
+struct F8Form { bool swap; int tn, pair; float block, exchange, out; };
+constexpr F8Form kF8Forms[] = {
+    {true, 16, 0, 0.215f, 0.3f, 0.1f}, {true, 32, 0, 0.22f, 0.5f, 0.2f}, {true, 64, 0, 0.29f, 1.5f, 0.4f},
+    {false, 32, 0, 0.215f, 0.5f, 0.3f}, {false, 64, 0, 0.30f, 1.3f, 0.6f}, {false, 128, 0, 0.36f, 3.2f, 2.0f},
+    {false, 128, 1, 0.345f, 0.f, 0.8f}, {false, 256, 1, 0.47f, 0.f, 1.5f}};
+struct F8Choice { F8Form form; int split; };
+static F8Choice choose_f8(long long m, long long n, int blocks) {
+    constexpr float kLaunch = 4.6f, kNextCta = 3.0f;
+    F8Choice best{kF8Forms[7], 1};
+    float least = 3.4e38f;
+    for (const F8Form& f : kF8Forms) {
+        const long long rows = f.swap ? n : m, cols = f.swap ? m : n, high = f.pair ? 256 : 128;
+        const long long tiles = (rows + high - 1) / high * ((cols + f.tn - 1) / f.tn);
+        for (int split = 1; split <= (f.pair ? 1 : 8); split *= 2) {
+            if (split > 1 && (split * 2 > blocks || tiles * split > kSms)) break;
+            const long long at_once = f.pair ? kSms / 2 : kSms, rounds = (tiles * split + at_once - 1) / at_once;
+            const float tile = (float)((blocks + split - 1) / split) * f.block + (split > 1 ? f.exchange : f.out);
+            const float us = kLaunch + (float)rounds * tile + (f.pair ? 0.f : (float)(rounds - 1) * kNextCta);
+            if (us < least) { least = us; best = F8Choice{f, split}; }
+        }
+    }
+    return best;
 }
 
 template <int TN>
@@ -757,34 +783,30 @@ extern "C" tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* 
     g.wide = on16(a->y) && a->y_row * bytes % 16 == 0;
     g.blocks = (a->kk + kF8Block - 1) / kF8Block;
     g.wait_ns = 1000000000ull;
-    // Up to 64 tokens: the weights' rows take the 128 lanes, and the tokens a tile of 16, 32 or 64 columns.
-    const bool swap = a->m <= 64;
-    const int tn = swap ? (a->m <= 16 ? 16 : a->m <= 32 ? 32 : 64) : 128;
+    const F8Choice choice = choose_f8(a->m, a->nn, g.blocks);
+    const bool swap = choice.form.swap;
+    const int tn = choice.form.tn;
     g.rows_a = swap ? a->nn : a->m; g.rows_b = swap ? a->m : a->nn;
     g.tiles_a = (g.rows_a + 127) / 128;
-    const long long tiles = (long long)g.tiles_a * ((g.rows_b + tn - 1) / tn);
-    if (tiles > 0x7fffffff) return TT_ERR_INVALID_ARG;
-    g.split = 1;
-    while (g.split < 8 && tiles * g.split * 2 <= kSms && g.split * 4 <= g.blocks) g.split *= 2;
+    if ((long long)g.tiles_a * ((g.rows_b + tn - 1) / tn) > 0x7fffffff) return TT_ERR_INVALID_ARG;
+    g.split = choice.split;
     g.blocks_per_split = (g.blocks + g.split - 1) / g.split;
     g.idesc = (1u << 4) | ((unsigned)(tn >> 3) << 17) | ((unsigned)(kHwTileM >> 4) << 24);
-    CUtensorMap tx, tw;
-    tt_status s = encode_bytes(&tx, a->x, a->kk, a->m, a->x_row, swap ? tn : 128);
-    if (s == TT_OK) s = encode_bytes(&tw, a->w, a->kk, a->nn, a->w_row, swap ? 128 : tn);
-    if (s != TT_OK) return s;
     if (swap) {
         g.a_scale = a->w_scale; g.as_row = a->ws_row; g.as_block = a->ws_block; g.b_scale = a->x_scale; g.bs_row = a->xs_row; g.bs_block = a->xs_block;
-        return status_of(tn == 16 ? launch_dense_f8<16, true>(tw, tx, g, stream) : tn == 32 ? launch_dense_f8<32, true>(tw, tx, g, stream) : launch_dense_f8<64, true>(tw, tx, g, stream));
+    } else {
+        g.a_scale = a->x_scale; g.as_row = a->xs_row; g.as_block = a->xs_block; g.b_scale = a->w_scale; g.bs_row = a->ws_row; g.bs_block = a->ws_block;
     }
-    g.a_scale = a->x_scale; g.as_row = a->xs_row; g.as_block = a->xs_block; g.b_scale = a->w_scale; g.bs_row = a->ws_row; g.bs_block = a->ws_block;
-    const int pair_n = g.split > 1 ? 0 : pair_columns(a->m, a->nn);
-    if (pair_n > 0) {
-        CUtensorMap ty{};
+    CUtensorMap ta, tb, ty{};
+    tt_status s = swap ? encode_bytes(&ta, a->w, a->kk, a->nn, a->w_row, 128) : encode_bytes(&ta, a->x, a->kk, a->m, a->x_row, 128);
+    if (s == TT_OK) s = swap ? encode_bytes(&tb, a->x, a->kk, a->m, a->x_row, tn) : encode_bytes(&tb, a->w, a->kk, a->nn, a->w_row, choice.form.pair ? tn / 2 : tn);
+    if (s != TT_OK) return s;
+    if (choice.form.pair) {
         g.wide = g.wide && a->nn * bytes % 16 == 0;        // (a TMA store clips in pieces of 16 bytes)
-        s = encode_bytes(&tw, a->w, a->kk, a->nn, a->w_row, pair_n / 2);
-        if (s == TT_OK && g.wide) s = encode_output(&ty, a->y, (int)bytes, a->nn, a->m, a->y_row, a->y_type == TT_TYPE_F32 ? 32 : pair_n / 4);
+        if (g.wide) s = encode_output(&ty, a->y, (int)bytes, a->nn, a->m, a->y_row, a->y_type == TT_TYPE_F32 ? 32 : tn / 4);
         if (s != TT_OK) return s;
-        return status_of(pair_n == 256 ? launch_dense_f8_pair<256>(tx, tw, ty, g, stream) : launch_dense_f8_pair<128>(tx, tw, ty, g, stream));
+        return status_of(tn == 256 ? launch_dense_f8_pair<256>(ta, tb, ty, g, stream) : launch_dense_f8_pair<128>(ta, tb, ty, g, stream));
     }
-    return status_of(launch_dense_f8<128, false>(tx, tw, g, stream));
+    if (swap) return status_of(tn == 16 ? launch_dense_f8<16, true>(ta, tb, g, stream) : tn == 32 ? launch_dense_f8<32, true>(ta, tb, g, stream) : launch_dense_f8<64, true>(ta, tb, g, stream));
+    return status_of(tn == 32 ? launch_dense_f8<32, false>(ta, tb, g, stream) : tn == 64 ? launch_dense_f8<64, false>(ta, tb, g, stream) : launch_dense_f8<128, false>(ta, tb, g, stream));
 }

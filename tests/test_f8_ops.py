@@ -360,7 +360,7 @@ def test_dense_types_and_activations(kind, act, m, pad):
 
 
 @gpu
-@pytest.mark.parametrize("m,n,k", [(8, 4096, 4096), (1, 128, 8192), (128, 128, 8192), (600, 2304, 768), (1500, 1300, 500)])
+@pytest.mark.parametrize("m,n,k", [(8, 4096, 4096), (1, 128, 8192), (128, 128, 8192), (600, 2304, 768), (1500, 1300, 500), (200, 2000, 1000), (4000, 128, 1000), (2000, 300, 2000), (130, 4096, 1024), (64, 900, 3000), (30, 300, 8000)])
 def test_dense_larger(m, n, k):
     check_dense(m, n, k)
 
