@@ -2,8 +2,8 @@
 // exponentials are the bound, not the cache's bytes.
 //
 // A CTA has two tiles of 128 rows and walks the keys 128 at a time.  Four warps bring keys and values from the pages, turn them into 16-bit floating
-// point (exactly) and leave them as operand tiles, which serve both tiles of rows.  S = Q K^T goes to tensor memory; a thread of the softmax warps
-// has one row of it, takes its maximum, and leaves P = 2^(s - m) in S's place as the first operand of O += P V, whose sums stay
+// point (exactly) and leave them as operand tiles, which serve both tiles of rows.  S = Q K^T goes to tensor memory; two threads of the
+// softmax warps have a row of it, take its maximum, and leave P = 2^(s - m) in S's place as the first operand of O += P V, whose sums stay
 // in tensor memory.  While one tile's softmax runs, the tensor core is at the other tile's products.
 //   O is multiplied only when a maximum has grown by more than 2^8 since it was last: P may be up to 2^8 times what it
 // would be, which 16 bits have room for (it is brought to 2^15 at most), and the row's sum has the same factor.  A page's scale of values is in
@@ -16,7 +16,8 @@
 
 namespace tt {
 
-constexpr int kPromptThreads = 512;         // warps 0-3 and 4-7 softmax of a tile each, 8-11 keys and values, 12 MMA and tensor memory
+constexpr int kPromptThreads = 768;         // warps 0-7 and 8-15 softmax of a tile each, 16-19 keys and values, 20 MMA and tensor memory, 21 pages, scales and copies
+constexpr int kSoftmax = 512;               // threads of the softmax, two to a row
 constexpr unsigned long long kPromptWait = 1000000000ull;                    // nanoseconds that a wait takes at most
 constexpr uint32_t kAtom = 128u * 128u;     // 128 rows of 64 values
 
@@ -38,13 +39,13 @@ __device__ __forceinline__ void tmem_st8u(uint32_t taddr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]));
 }
-// 32 columns from here on.
-__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t* v) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-                 "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-                   "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
-                   "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]));
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float tmem_ld1(uint32_t taddr) {
+    float v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n\ttcgen05.wait::ld.sync.aligned;" : "=f"(v) : "r"(taddr) : "memory");
+    return v;
 }
 __device__ __forceinline__ float max_of(float a, float b, float c) {
     float m;
@@ -61,15 +62,7 @@ __device__ __forceinline__ void tmem_ld8u(uint32_t taddr, uint32_t* v) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
 }
-// N bytes to shared memory, or N zeros.
-template <int N>
-__device__ __forceinline__ void copy_async_or_zero(uint32_t dst, const void* src, bool copy) {
-    const int bytes = copy ? N : 0;
-    if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(bytes), "n"(N) : "memory");
-}
-// Registers of a warpgroup from here on.  512 threads begin with 128 each (65536): 184 for the softmax's
-// two, 96 and 40 for the others make 64512.
+// Registers of a warpgroup from here on.  768 threads begin with 80 each (61440): 96 for the softmax's four, 56 and 40 for the others make 61440.
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
@@ -89,10 +82,10 @@ struct PromptShape {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(const __grid_constant__ Attend g) {
+__global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v, const __grid_constant__ Attend g) {
     typedef PromptShape<D> S;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2], drained;
+    __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2], raw_full[2], raw_empty[2], drained;
     __shared__ StepScales scales[4];
     __shared__ int nan_first[D], nan_last[D];
     __shared__ uint32_t tmem_slot;
@@ -115,19 +108,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t q_s = base, k_s = base + 2u * S::kTile, v_s = base + 4u * S::kTile;
     if (threadIdx.x == 0) {
-        mbar_init(smem_u32(&q_full), 8u);
+        mbar_init(smem_u32(&q_full), 16u);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&k_full[i]), 4u); mbar_init(smem_u32(&v_full[i]), 4u);
+            mbar_init(smem_u32(&k_full[i]), 5u); mbar_init(smem_u32(&v_full[i]), 4u);
             mbar_init(smem_u32(&k_empty[i]), 1u); mbar_init(smem_u32(&v_empty[i]), 1u);
             mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i][0]), 4u); mbar_init(smem_u32(&p_ready[i][1]), 4u); mbar_init(smem_u32(&o_done[i]), 1u);
         }
+        mbar_init(smem_u32(&raw_full[0]), 1u); mbar_init(smem_u32(&raw_full[1]), 1u);
+        mbar_init(smem_u32(&raw_empty[0]), 4u); mbar_init(smem_u32(&raw_empty[1]), 4u);
         mbar_init(smem_u32(&drained), 1u);
         abort_flag = 0;
         fence_mbar_init();
         fence_proxy_async_shared();
     }
     if ((int)threadIdx.x < D) { nan_first[threadIdx.x] = INT_MAX; nan_last[threadIdx.x] = INT_MIN; }
-    if (warp == 12) {
+    if (warp == 20) {
         tmem_alloc(smem_u32(&tmem_slot), 512u);
         tmem_relinquish();
     }
@@ -138,14 +133,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     pdl_allow_next();                                                     // (the next launch may take tensor memory: this CTA has its own)
 
     // a softmax thread's row
-    const int tile = warp >> 2, r = (int)threadIdx.x & 255;
-    const bool mine = warp < 8 && r < view.rows;
+    const int tile = warp >> 3, half = (warp >> 2) & 1, r = tile * 128 + (int)(threadIdx.x & 127);      // (a half of its columns)
+    const bool mine = warp < 16 && r < view.rows;
     const int row_t = view.t0 + (view.h0 + r) / g.group, row_h = head * g.group + (view.h0 + r) % g.group;
     float top = -INFINITY, used = 0.f, sum = 0.f, ref = 0.f;              // maximum; the one that O and the sum are relative to; the unit of O
     bool fine = true;
 
-    if (warp < 8) {
-        registers_up<184>();
+    if (warp < 16) {
+        registers_up<96>();
         // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
         const int lr = r & 127;
         const long long at = (view.start + (long long)row_t) * g.a.q_token + (long long)row_h * g.a.q_head;
@@ -165,7 +160,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         const float factor = fabsf(g.scale_log2) / size;
         const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)lr * 128u;
 #pragma unroll 8
-        for (int i = 0; i < D; i += 4) {
+        for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 4) {
             float v[4] = {0.f, 0.f, 0.f, 0.f};
             if (mine) load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
             const uint32_t to_ = line + (uint32_t)(i / 8 % S::kAtoms) * kAtom + (((uint32_t)(i / (8 * S::kAtoms)) ^ (uint32_t)(lr & 7)) << 4) + (uint32_t)(i & 4) * 2u;
@@ -179,49 +174,47 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         // ---------------- softmax ----------------
         const int row_pos = view.before + row_t;                          // the row sees tokens row_lo .. row_hi - 1
         const int row_hi = g.a.causal ? min(view.hi, row_pos + 1) : view.hi, row_lo = g.a.window > 0 ? row_pos + 1 - g.a.window : 0;
+        const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
+        const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
         if (tile < tiles) {
-            const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
-            const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
             for (int i = 0; i < steps; ++i) {
-                if (!__all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u, kPromptWait))) { fine = false; break; }
+                // (a warp that gives up goes on, without waiting: the others of its tile meet it below)
+                fine = fine && __all_sync(0xffffffffu, bounded_wait(&s_full[tile], (uint32_t)i & 1u, abortp, g.a.status, 31u, kPromptWait));
                 tc_fence_after();
                 const int t = from + i * kPromptTokens;
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
-                const int j_lo = row_lo - t, j_hi = row_hi - t;           // the row sees columns j_lo .. j_hi - 1
-                uint32_t v[128];
+                const int j_lo = row_lo - t - 64 * half, j_hi = row_hi - t - 64 * half;      // the row sees columns j_lo .. j_hi - 1 of this half
+                uint32_t v[64];
 #pragma unroll
-                for (int h = 0; h < 4; ++h) tmem_ld32(s_t + 32u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
+                for (int h = 0; h < 2; ++h) tmem_ld32(s_t + 64u * (uint32_t)half + 32u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
                 tmem_wait_ld();
                 if (!whole) {
 #pragma unroll
-                    for (int k = 0; k < 128; ++k) v[k] = k >= j_lo && k < j_hi ? v[k] : 0xff800000u;      // (-inf)
+                    for (int k = 0; k < 64; ++k) v[k] = k >= j_lo && k < j_hi ? v[k] : 0xff800000u;      // (-inf)
                 }
-                float key[8], shift[8], back[8];
-                const uint32_t info = smem_u32(&scales[i & 3]);
+                const uint32_t info = smem_u32(&scales[i & 3]) + 16u * (uint32_t)half;
+                float4 keys = ld_shared_v4f(info);
+                float m[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float4 a = ld_shared_v4f(info + 16u * h), b = ld_shared_v4f(info + 32u + 16u * h), d = ld_shared_v4f(info + 64u + 16u * h);
-                    key[4 * h] = a.x; key[4 * h + 1] = a.y; key[4 * h + 2] = a.z; key[4 * h + 3] = a.w;
-                    shift[4 * h] = b.x; shift[4 * h + 1] = b.y; shift[4 * h + 2] = b.z; shift[4 * h + 3] = b.w;
-                    back[4 * h] = d.x; back[4 * h + 1] = d.y; back[4 * h + 2] = d.z; back[4 * h + 3] = d.w;
-                }
-                float mx = top, m[8];
-#pragma unroll
-                for (int gr = 0; gr < 8; ++gr) m[gr] = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
+                for (int gr = 0; gr < 4; ++gr) m[gr] = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
 #pragma unroll
                 for (int k = 2; k < 16; k += 2)
 #pragma unroll
-                    for (int gr = 0; gr < 8; ++gr) m[gr] = max_of(m[gr], __uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1]));
-#pragma unroll
-                for (int gr = 0; gr < 8; ++gr) {
-                    // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
-                    key[gr] = fmaxf(factor * key[gr], 1.17549435e-38f);
-                    mx = fmaxf(mx, m[gr] * key[gr]);
-                }
+                    for (int gr = 0; gr < 4; ++gr) m[gr] = max_of(m[gr], __uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1]));
+                // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
+                const auto factor_of = [&](float key) { return fmaxf(factor * key, 1.17549435e-38f); };
+                keys = make_float4(factor_of(keys.x), factor_of(keys.y), factor_of(keys.z), factor_of(keys.w));
+                float mx = max_of(fmaxf(m[0] * keys.x, m[1] * keys.y), m[2] * keys.z, m[3] * keys.w);
+                // The halves tell each other their maxima in tensor memory, in a column that its writer has read and that nobody but the reader writes next.
+                tmem_st1(s_t + (half ? 64u : 32u), mx);
+                tmem_wait_st();
+                tc_fence_before();
+                named_sync(4 + tile, 256);
+                tc_fence_after();
                 const float seen = top;
-                top = mx;
+                top = max_of(top, mx, tmem_ld1(s_t + (half ? 32u : 64u)));
                 // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
-                const float new_ref = ld_shared_f32(info + 96u);
+                const float new_ref = ld_shared_f32(smem_u32(&scales[i & 3].ref));
                 const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
                 const bool move = top > used + 8.f || first || ref != new_ref;
                 if (__any_sync(0xffffffffu, move)) {
@@ -231,57 +224,47 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     used = now;
                     sum *= alpha;
                     ref = new_ref;
-                    if (i > 0) {
-                        if (!__all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kPromptWait))) { fine = false; break; }
+                    if (i > 0 && half == 0) {                             // (in front of the first half of P, which lets the product begin)
+                        fine = fine && __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
                         tc_fence_after();
 #pragma unroll 1
-                        for (int h = 0; h < D; h += 16) {                 // (few at a time: the scores are in registers)
-                            uint32_t o[16];
+                        for (int h = 0; h < D; h += 8) {                  // (few at a time: the scores are in registers)
+                            uint32_t o[8];
                             tmem_ld8u(o_t + (uint32_t)h, o);
-                            tmem_ld8u(o_t + (uint32_t)h + 8u, o + 8);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
+                            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
                             tmem_st8u(o_t + (uint32_t)h, o);
-                            tmem_st8u(o_t + (uint32_t)h + 8u, o + 8);
                         }
                     }
                 }
-                // exponentials of a group while the sums and the conversion of the one before are under way
-                float2 e[2][8];
-                uint32_t p[32];
+                const float4 shift = ld_shared_v4f(info + 32u), back = ld_shared_v4f(info + 64u);
 #pragma unroll
-                for (int gr = 0; gr < 9; ++gr) {
-                    if (gr < 8) {
-                        const float f = key[gr], add = shift[gr] - used;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k)
-                            e[gr & 1][k] = fma_pair(make_float2(__uint_as_float(v[16 * gr + 2 * k]), __uint_as_float(v[16 * gr + 2 * k + 1])), make_float2(f, f), make_float2(add, add));
-                    }
+                for (int gr = 0; gr < 4; ++gr) {
+                    const float f = gr == 0 ? keys.x : gr == 1 ? keys.y : gr == 2 ? keys.z : keys.w;
+                    const float add = (gr == 0 ? shift.x : gr == 1 ? shift.y : gr == 2 ? shift.z : shift.w) - used;
+                    float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    uint32_t p[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        if (gr < 8) { e[gr & 1][k].x = exp2_fast(e[gr & 1][k].x); e[gr & 1][k].y = exp2_fast(e[gr & 1][k].y); }
-                        if (gr > 0) p[8 * ((gr - 1) & 3) + k] = down2<TT_TYPE_F16>(e[(gr - 1) & 1][k].x, e[(gr - 1) & 1][k].y);
+                        float2 e = fma_pair(make_float2(__uint_as_float(v[16 * gr + 2 * k]), __uint_as_float(v[16 * gr + 2 * k + 1])), make_float2(f, f), make_float2(add, add));
+                        e.x = exp2_fast(e.x);
+                        e.y = exp2_fast(e.y);
+                        part[k & 1] = add_pair(part[k & 1], e);
+                        p[k] = down2<TT_TYPE_F16>(e.x, e.y);
                     }
-                    if (gr > 0) {
-                        float2 (&d)[8] = e[(gr - 1) & 1];
-                        const float2 a = add_pair(add_pair(add_pair(d[0], d[1]), add_pair(d[2], d[3])), add_pair(add_pair(d[4], d[5]), add_pair(d[6], d[7])));
-                        sum = fmaf(a.x + a.y, back[gr - 1], sum);
-                    }
-                    if (gr == 4 || gr == 8) {
-                        constexpr int kHalf[9] = {0, 0, 0, 0, 0, 0, 0, 0, 1};
-                        const int h = kHalf[gr];
-                        tmem_st32u(s_t + 32u * h, p);
-                        tmem_wait_st();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile][h]));
-                    }
+                    part[0] = add_pair(part[0], part[1]);
+                    sum = fmaf(part[0].x + part[0].y, gr == 0 ? back.x : gr == 1 ? back.y : gr == 2 ? back.z : back.w, sum);
+                    tmem_st8u(s_t + 32u * (uint32_t)half + 8u * gr, p);
                 }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile][half]));
             }
         }
         // ---------------- out ----------------
-        named_sync(1, 384);                                               // (every NaN of the steps at the edges has been noted)
+        named_sync(1, kSoftmax + 128);                                               // (every NaN of the steps at the edges has been noted)
         const long long place = unit * c.heads + head;
         constexpr int kPart = kPromptRows * (D + 2);
         const auto store = [&](int rr, int i, const float (&v)[4]) {
@@ -291,15 +274,23 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         if (tile < tiles) {
             if (steps > 0 && fine) fine = __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
             tc_fence_after();
+            if (steps > 0) {
+                // the row's sum: both halves', by way of the scores' columns (every product that read them is done)
+                tmem_st1(s_t + (half ? 64u : 32u), sum);
+                tmem_wait_st();
+                tc_fence_before();
+                named_sync(4 + tile, 256);
+                tc_fence_after();
+                sum += tmem_ld1(s_t + (half ? 32u : 64u));
+            }
             if (fine) {
-                const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
                 const int pos = row_pos;
                 const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
                 // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
                 const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
                 float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
 #pragma unroll 1
-                for (int h = 0; h < D; h += 32) {
+                for (int h = half * (D / 2); h < (half + 1) * (D / 2); h += 32) {
                     uint32_t v[32];
                     if (steps > 0) {
                         tmem_ld32(o_t + (uint32_t)h, v);
@@ -321,24 +312,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     }
                     __syncwarp();
                 }
-                if (active > 1 && mine) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, none ? 0.f : sum);
+                if (active > 1 && mine && half == 0) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, none ? 0.f : sum);
             }
         }
         tc_fence_before();
         __syncwarp();
-        named_arrive(2, 288);                                             // (the tensor memory has been read)
+        named_arrive(2, kSoftmax + 32);                                             // (the tensor memory has been read)
         if (active == 1) return;
 
         // ---------------- the splits together, by the last CTA of the tile ----------------
         __threadfence();
-        named_sync(3, 256);
+        named_sync(3, kSoftmax);
         if (threadIdx.x == 0) last_one = atomicAdd(g.counters + place, 1u) == (unsigned)active - 1u;
-        named_sync(3, 256);
+        named_sync(3, kSoftmax);
         if (!last_one) return;
         __threadfence();
         const float* parts = g.partial + place * g.splits * kPart;
         float* share = reinterpret_cast<float*>(smem_raw);               // [split][row]
-        if (mine) {
+        if (mine && half == 0) {
             float mx = -INFINITY, l = 0.f;
             for (int z = 0; z < active; ++z) {
                 const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * r));
@@ -353,8 +344,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const float inv = l != 0.f ? 1.f / l : 0.f;
             for (int z = 0; z < active; ++z) share[z * kPromptRows + r] *= inv;
         }
-        named_sync(3, 256);
-        for (int e = threadIdx.x; e < view.rows * (D / 4); e += 256) {
+        named_sync(3, kSoftmax);
+        for (int e = threadIdx.x; e < view.rows * (D / 4); e += kSoftmax) {
             const int rr = e / (D / 4), i = 4 * (e - rr * (D / 4));
             float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -366,20 +357,16 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             store(rr, i, v);
         }
         if (threadIdx.x == 0) g.counters[place] = 0u;                    // ready for the next call
-    } else if (warp < 12) {
-        registers_down<96>();
+    } else if (warp < 20) {
+        registers_down<56>();
         // ---------------- keys and values: pages -> operand tiles ----------------
-        // Eight lanes have a token; the four warps take the 16 tokens of a group at a time.  A lane copies kPiece values a step ahead into a place of
-        // its own, and turns them into one 16-byte chunk of each atom's line (all banks at once): value kPiece * lane + 8 a + e of a head is
-        // value e of chunk `lane` of atom a, and the queries and the outputs are ordered alike.
+        // A step's bytes arrive by TMA, a step ahead.  Eight lanes have a token; the four warps take the 16 tokens of a group at a time, and a lane turns
+        // kPiece values into one 16-byte chunk of each atom's line (all banks at once): value kPiece * lane + 8 a + e of a head is value e of chunk
+        // `lane` of atom a, and the queries and the outputs are ordered alike.
         constexpr int kPiece = 8 * S::kAtoms;
-        const int dt = (int)threadIdx.x - 256, piece = dt & 7, sub = dt >> 3;
-        const uint8_t* keys = static_cast<const uint8_t*>(c.data[0]) + head * c.head[0] + sub * c.token[0] + kPiece * piece;
-        const uint8_t* vals = static_cast<const uint8_t*>(c.data[1]) + head * c.head[1] + sub * c.token[1] + kPiece * piece;
-        const int* table = c.table + view.b * c.table_row;
-        const int shift = 31 - __clz(c.block);
-        const uint32_t raw = base + 6u * S::kTile + (uint32_t)(dt * kPiece);                     // (keys; the values' behind them)
-        constexpr uint32_t kGroup = 128u * kPiece;                                               // bytes of a group of 16 tokens there
+        const int dt = (int)threadIdx.x - kSoftmax, piece = dt & 7, sub = dt >> 3;
+        constexpr uint32_t kGroup = 128u * kPiece;                                               // bytes of a group of 16 tokens
+        const uint32_t raw = base + 6u * S::kTile + (uint32_t)(dt * kPiece);                    // (keys; the values' behind them)
         const uint32_t chunk = (uint32_t)sub * 128u + ((((uint32_t)piece) ^ ((uint32_t)sub & 7u)) << 4);
         const auto put = [&](uint32_t tile_s, int group, const uint32_t (&w)[kPiece / 4]) {
 #pragma unroll
@@ -390,74 +377,40 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(tile_s + chunk + (uint32_t)a * kAtom + (uint32_t)group * 2048u), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
             }
         };
-        const auto fetch = [&](int i, int pages, const uint8_t* data, int w) {
-            const int t = from + i * kPromptTokens;
-            if (i < steps) {
+        // the last step's tokens behind `to`, and those in front of what any row sees, may be anything: zeros
+        const auto bytes_of = [&](int w, int p, int t, bool edge, uint32_t (&x)[kPiece / 4]) {
+            read_shared<kPiece>(raw + (uint32_t)(8 * w + p) * kGroup, x);
+            if (edge) {
+                const int tok = t + 16 * p + sub;
+                if (tok < view.lo || tok >= to) {
 #pragma unroll
-                for (int p = 0; p < 8; ++p) {
-                    const int pg = __shfl_sync(0xffffffffu, pages, p), first = t + 16 * p, tok = first + sub;
-                    const bool any = pg >= 0 && tok >= view.lo && tok < to;                      // (else zeros)
-                    const uint8_t* at = any ? data + (pg * c.page[w] + (first & (c.block - 1)) * c.token[w]) : data;
-                    copy_async_or_zero<kPiece>(raw + (uint32_t)w * 8u * kGroup + (uint32_t)p * kGroup, at, any);
+                    for (int q = 0; q < kPiece / 4; ++q) x[q] = 0u;
                 }
             }
-            cp_async_commit();
         };
-        // lane g of the first eight has the page of a step's group g, and its scales
-        const auto page_of = [&](int i) {
-            const int t = from + i * kPromptTokens + 16 * (lane & 7);
-            if (i >= steps || t + 15 < view.lo || t >= to) return -1;
-            const int pg = table[t >> shift];
-            if ((unsigned)pg < (unsigned)c.pages) return pg;
-            report_invalid(g.a.status);
-            return -1;
-        };
-        const auto scale_of = [&](int pg, int w) { return pg >= 0 ? c.scale[w][pg * c.s_page[w] + head * c.s_head[w]] : 0.f; };
-        float most = 0.f;                                                 // the largest scale of values so far
-        int page = page_of(0), page1 = page_of(1);
-        float ks = scale_of(page, 0), vs = scale_of(page, 1);
-        fetch(0, page, keys, 0);
-        fetch(0, page, vals, 1);
-        for (int i = 0; i < steps; ++i) {
+        for (int i = 0; i < steps && fine; ++i) {
             const int t = from + i * kPromptTokens, buf = i & 1;
-            const int page2 = page_of(i + 2);
-            const float ks1 = scale_of(page1, 0), vs1 = scale_of(page1, 1);
-            if (!__all_sync(0xffffffffu, bounded_wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 33u, kPromptWait))) break;
-            if (warp == 8) {
-                // the scales, before the keys report: what lay here four steps ago has been read
-                float m = vs;
-#pragma unroll
-                for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-                most = fmaxf(most, m);
-                if (lane < 8) {
-                    StepScales& sc = scales[i & 3];
-                    // (a share of less than 2^-40 of the largest scale is taken as that)
-                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
-                    sc.key[lane] = ks;
-                    sc.shift[lane] = lg + 7.f;
-                    sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
-                    if (lane == 0) sc.ref = most;
-                }
-            }
-            cp_async_wait<1>();
+            const bool edge = t < view.lo || t + kPromptTokens > to;
+            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return bounded_wait(bar, parity, abortp, g.a.status, where, kPromptWait); };
+            fine = __all_sync(0xffffffffu, wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, 33u) && wait(&raw_full[0], (uint32_t)i & 1u, 40u));
+            if (!fine) break;
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
                 uint32_t w[kPiece / 4];
-                read_shared<kPiece>(raw + (uint32_t)p * kGroup, w);
+                bytes_of(0, p, t, edge, w);
                 put(k_s + (uint32_t)buf * S::kTile, p, w);
             }
             fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
-            fetch(i + 1, page1, keys, 0);
-            if (!__all_sync(0xffffffffu, bounded_wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, abortp, g.a.status, 34u, kPromptWait))) break;
-            cp_async_wait<1>();
+            if (lane == 0) { mbar_arrive(smem_u32(&raw_empty[0])); mbar_arrive(smem_u32(&k_full[buf])); }
+            fine = __all_sync(0xffffffffu, wait(&v_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, 34u) && wait(&raw_full[1], (uint32_t)i & 1u, 41u));
+            if (!fine) break;
             const bool low = t < view.whole_lo, high = g.a.causal && t + kPromptTokens > view.whole_hi;
             if (low || high) {
 #pragma unroll 1
                 for (int p = 0; p < 8; ++p) {
                     uint32_t w[kPiece / 4];
-                    read_shared<kPiece>(raw + (uint32_t)(8 + p) * kGroup, w);
+                    bytes_of(1, p, t, edge, w);
 #pragma unroll
                     for (int q = 0; q < kPiece / 4; ++q) {
                         const uint32_t n = nan_bytes(w[q]);
@@ -475,24 +428,79 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 #pragma unroll
                 for (int p = 0; p < 8; ++p) {
                     uint32_t w[kPiece / 4];
-                    read_shared<kPiece>(raw + (uint32_t)(8 + p) * kGroup, w);
+                    bytes_of(1, p, t, edge, w);
                     put(v_s + (uint32_t)buf * S::kTile, p, w);
                 }
             }
             fence_proxy_async_shared();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&v_full[buf]));
-            fetch(i + 1, page1, vals, 1);
-            page1 = page2;
-            ks = ks1;
-            vs = vs1;
+            if (lane == 0) { mbar_arrive(smem_u32(&raw_empty[1])); mbar_arrive(smem_u32(&v_full[buf])); }
         }
-        cp_async_wait<0>();
-        named_arrive(1, 384);
+        named_arrive(1, kSoftmax + 128);
     } else {
         registers_down<40>();
+        if (warp == 21 && steps > 0) {
+            // ---------------- pages, scales, copies ----------------
+            // lane g of the first eight has the page of a step's group g, and its scales; what is looked up is used a step later
+            const int* table = c.table + view.b * c.table_row;
+            const int shift = 31 - __clz(c.block), box = min(c.block, kPromptTokens);                // tokens of a box
+            const uint32_t raw0 = base + 6u * S::kTile;
+            const auto held = [&](int i) { const int t = from + i * kPromptTokens + 16 * (lane & 7); return i < steps && t + 15 >= view.lo && t < to; };
+            const auto page_of = [&](int i) { return held(i) ? table[(from + i * kPromptTokens + 16 * (lane & 7)) >> shift] : -1; };
+            const auto good = [&](int i, int pg) {
+                if ((unsigned)pg < (unsigned)c.pages) return pg;
+                if (held(i)) report_invalid(g.a.status);
+                return -1;                                                // (a box outside of the tensor is zeros)
+            };
+            const auto scale_of = [&](int pg, int w) { return pg >= 0 ? c.scale[w][pg * c.s_page[w] + head * c.s_head[w]] : 0.f; };
+            const auto wait = [&](uint64_t* bar, uint32_t parity, unsigned where) { return __all_sync(0xffffffffu, bounded_wait(bar, parity, abortp, g.a.status, where, kPromptWait)); };
+            const auto fetch = [&](int i, int pages, int w) {
+                if (lane == 0) mbar_expect_tx(smem_u32(&raw_full[w]), 128u * (uint32_t)D);
+                for (int p = 0; p < kPromptTokens; p += box) {
+                    const int pg = __shfl_sync(0xffffffffu, pages, p >> 4);
+                    if (lane == 0) tma_load_4d(raw0 + (uint32_t)(w * 128 + p) * (uint32_t)D, w ? &tmap_v : &tmap_k, smem_u32(&raw_full[w]), 0, (from + i * kPromptTokens + p) & (c.block - 1), head, pg);
+                }
+            };
+            int page = good(0, page_of(0)), page1 = page_of(1);
+            float ks = scale_of(page, 0), vs = scale_of(page, 1), most = 0.f;      // most: the largest scale of values so far
+            fetch(0, page, 0);
+            fetch(0, page, 1);
+            for (int i = 0; i < steps; ++i) {
+                const int buf = i & 1, page2 = page_of(i + 2), next = good(i + 1, page1);
+                const float ks1 = scale_of(next, 0), vs1 = scale_of(next, 1);
+                // the scales, before the keys report: what lay here four steps ago has been read
+                if (!wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, 42u)) break;
+                float m = vs;
+#pragma unroll
+                for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                most = fmaxf(most, m);
+                if (lane < 8) {
+                    StepScales& sc = scales[i & 3];
+                    // (a share of less than 2^-40 of the largest scale is taken as that)
+                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
+                    sc.key[lane] = ks;
+                    sc.shift[lane] = lg + 7.f;
+                    sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
+                    if (lane == 0) sc.ref = most;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));
+                if (i + 1 < steps) {
+                    if (!wait(&raw_empty[0], (uint32_t)i & 1u, 43u)) break;
+                    fetch(i + 1, next, 0);
+                    if (!wait(&raw_empty[1], (uint32_t)i & 1u, 44u)) break;
+                    fetch(i + 1, next, 1);
+                }
+                page1 = page2;
+                ks = ks1;
+                vs = vs1;
+            }
+            // shared memory stays until the copies have landed, also when somebody gave up (bounded)
+            const unsigned long long t0 = global_timer_ns();
+            while (*abortp && global_timer_ns() - t0 < 2000000ull) { }
+        }
         // ---------------- MMA issuer ----------------
-        if (warp == 12 && steps > 0 && elect_one()) {
+        if (warp == 20 && steps > 0 && elect_one()) {
             constexpr uint32_t kIdescS = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
             constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);     // values: the columns are the contiguous axis
             const uint64_t dk = make_desc(0u, 128);
@@ -547,9 +555,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const unsigned long long t0 = global_timer_ns();
             while (!mbar_try_wait(smem_u32(&drained), 0u)) if (global_timer_ns() - t0 > kPromptWait) break;
         }
-        if (warp == 12) {
+        if (warp == 20) {
             __syncwarp();
-            named_sync(2, 288);
+            named_sync(2, kSoftmax + 32);
             tc_fence_after();
             tmem_dealloc(tmem, 512u);
         }
@@ -564,7 +572,15 @@ static cudaError_t launch_prompt(const Attend& g, long long units, void* stream)
     static OncePerDevice raised;
     const cudaError_t ready = raised([] { return cudaFuncSetAttribute(tt_attend_prompt_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kBytes); });
     if (ready != cudaSuccess) return ready;
-    return launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, g);
+    CUtensorMap maps[2];
+    const tt_cache& c = g.a.cache;
+    for (int w = 0; w < 2; ++w) {
+        // (without pages nothing is read: the map is of any memory)
+        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], 0, c.block)
+                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, 0, c.block);
+        if (st != TT_OK) return cudaErrorInvalidValue;
+    }
+    return launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, maps[0], maps[1], g);
 }
 cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream) {
     return g.a.cache.d == 64 ? launch_prompt<64>(g, units, stream) : launch_prompt<128>(g, units, stream);
