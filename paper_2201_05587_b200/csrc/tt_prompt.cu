@@ -5,8 +5,9 @@
 // point (exactly) and leave them as operand tiles, which serve both tiles of rows.  S = Q K^T goes to tensor memory; two threads of the
 // softmax warps have a row of it, take its maximum, and leave P = 2^(s - m) in S's place as the first operand of O += P V, whose sums stay
 // in tensor memory.  While one tile's softmax runs, the tensor core is at the other tile's products.
-//   O is multiplied only when a maximum has grown by more than 2^8 since it was last: P may be up to 2^8 times what it
-// would be, which 16 bits have room for (it is brought to 2^15 at most), and the row's sum has the same factor.  A page's scale of values is in
+//   O is multiplied only when a maximum has grown by more than 2^11 since it was last: P may be up to 2^11 times what it
+// would be, which 16 bits have room for (it is brought to 2^15 at most, and what is 2^-18 of the largest has all of its bits), and the row's sum has
+// the same factor.  A page's scale of values is in
 // P too, as the part of the exponent, over the largest scale so far.
 //   NaN in values that only some rows of the tile see (the steps at the edge of what is visible) are taken out of the product and put into
 // the outputs of the rows that do: a column's first such token (at the upper edge; its last one at the lower) decides.
@@ -213,10 +214,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 tc_fence_after();
                 const float seen = top;
                 top = max_of(top, mx, tmem_ld1(s_t + (half ? 32u : 64u)));
-                // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
+                // O and the sum follow the maximum when it is 2^11 ahead, and the largest scale at once
                 const float new_ref = ld_shared_f32(smem_u32(&scales[i & 3].ref));
                 const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
-                const bool move = top > used + 8.f || first || ref != new_ref;
+                const bool move = top > used + 11.f || first || ref != new_ref;
                 if (__any_sync(0xffffffffu, move)) {
                     const float now = top == -INFINITY ? 0.f : top;
                     const float alpha = seen != -INFINITY ? exp2_fast(used - now) : 0.f;
@@ -228,13 +229,15 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                         fine = fine && __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
                         tc_fence_after();
 #pragma unroll 1
-                        for (int h = 0; h < D; h += 8) {                  // (few at a time: the scores are in registers)
-                            uint32_t o[8];
+                        for (int h = 0; h < D; h += 16) {                 // (few at a time: the scores are in registers)
+                            uint32_t o[16];
                             tmem_ld8u(o_t + (uint32_t)h, o);
+                            tmem_ld8u(o_t + (uint32_t)h + 8u, o + 8);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
                             tmem_st8u(o_t + (uint32_t)h, o);
+                            tmem_st8u(o_t + (uint32_t)h + 8u, o + 8);
                         }
                     }
                 }
@@ -286,8 +289,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             if (fine) {
                 const int pos = row_pos;
                 const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
-                // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
-                const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
+                // O is in units of 2^4 and the largest scale; a split's part stays relative to its sum
+                const float unit_o = ref * 0.0625f * (active == 1 ? 1.f / sum : 1.f);
                 float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
 #pragma unroll 1
                 for (int h = half * (D / 2); h < (half + 1) * (D / 2); h += 32) {
@@ -479,8 +482,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     // (a share of less than 2^-40 of the largest scale is taken as that)
                     const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
                     sc.key[lane] = ks;
-                    sc.shift[lane] = lg + 7.f;
-                    sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
+                    sc.shift[lane] = lg + 4.f;
+                    sc.back[lane] = exp2_fast(-lg) * 0.0625f;
                     if (lane == 0) sc.ref = most;
                 }
                 __syncwarp();
