@@ -63,6 +63,11 @@ __device__ __forceinline__ void tmem_ld8u(uint32_t taddr, uint32_t* v) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ float2 ld_shared_v2f(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
 // Registers of a warpgroup from here on.  768 threads begin with 80 each (61440): 96 for the softmax's four, 56 and 40 for the others make 61440.
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&k_full[i]), 5u); mbar_init(smem_u32(&v_full[i]), 4u);
             mbar_init(smem_u32(&k_empty[i]), 1u); mbar_init(smem_u32(&v_empty[i]), 1u);
-            mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i][0]), 4u); mbar_init(smem_u32(&p_ready[i][1]), 4u); mbar_init(smem_u32(&o_done[i]), 1u);
+            mbar_init(smem_u32(&s_full[i]), 1u); mbar_init(smem_u32(&p_ready[i][0]), 8u); mbar_init(smem_u32(&p_ready[i][1]), 8u); mbar_init(smem_u32(&o_done[i]), 1u);
         }
         mbar_init(smem_u32(&raw_full[0]), 1u); mbar_init(smem_u32(&raw_full[1]), 1u);
         mbar_init(smem_u32(&raw_empty[0]), 4u); mbar_init(smem_u32(&raw_empty[1]), 4u);
@@ -184,17 +189,21 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 tc_fence_after();
                 const int t = from + i * kPromptTokens;
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
-                const int j_lo = row_lo - t - 64 * half, j_hi = row_hi - t - 64 * half;      // the row sees columns j_lo .. j_hi - 1 of this half
+                // This half has columns 32 * half .. + 31 and the 32 that are 64 further on (so both halves' first 32 let a product begin); of a
+                // place k, `column` is relative to 32 * half, and the row sees columns j_lo .. j_hi - 1.
+                const int j_lo = row_lo - t - 32 * half, j_hi = row_hi - t - 32 * half;
+                const auto column = [](int k) { return k < 32 ? k : k + 32; };
                 uint32_t v[64];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) tmem_ld32(s_t + 64u * (uint32_t)half + 32u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
+                for (int h = 0; h < 2; ++h) tmem_ld32(s_t + 32u * (uint32_t)half + 64u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
                 tmem_wait_ld();
                 if (!whole) {
 #pragma unroll
-                    for (int k = 0; k < 64; ++k) v[k] = k >= j_lo && k < j_hi ? v[k] : 0xff800000u;      // (-inf)
+                    for (int k = 0; k < 64; ++k) v[k] = column(k) >= j_lo && column(k) < j_hi ? v[k] : 0xff800000u;      // (-inf)
                 }
-                const uint32_t info = smem_u32(&scales[i & 3]) + 16u * (uint32_t)half;
-                float4 keys = ld_shared_v4f(info);
+                const uint32_t info = smem_u32(&scales[i & 3]) + 8u * (uint32_t)half;
+                const auto four_of = [&](uint32_t at) { const float2 a = ld_shared_v2f(at), b = ld_shared_v2f(at + 16u); return make_float4(a.x, a.y, b.x, b.y); };
+                float4 keys = four_of(info);
                 float m[4];
 #pragma unroll
                 for (int gr = 0; gr < 4; ++gr) m[gr] = fmaxf(__uint_as_float(v[16 * gr]), __uint_as_float(v[16 * gr + 1]));
@@ -207,13 +216,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 keys = make_float4(factor_of(keys.x), factor_of(keys.y), factor_of(keys.z), factor_of(keys.w));
                 float mx = max_of(fmaxf(m[0] * keys.x, m[1] * keys.y), m[2] * keys.z, m[3] * keys.w);
                 // The halves tell each other their maxima in tensor memory, in a column that its writer has read and that nobody but the reader writes next.
-                tmem_st1(s_t + (half ? 64u : 32u), mx);
+                tmem_st1(s_t + (half ? 32u : 16u), mx);
                 tmem_wait_st();
                 tc_fence_before();
                 named_sync(4 + tile, 256);
                 tc_fence_after();
                 const float seen = top;
-                top = max_of(top, mx, tmem_ld1(s_t + (half ? 32u : 64u)));
+                top = max_of(top, mx, tmem_ld1(s_t + (half ? 16u : 32u)));
                 // O and the sum follow the maximum when it is 2^11 ahead, and the largest scale at once
                 const float new_ref = ld_shared_f32(smem_u32(&scales[i & 3].ref));
                 const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
@@ -241,7 +250,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                         }
                     }
                 }
-                const float4 shift = ld_shared_v4f(info + 32u), back = ld_shared_v4f(info + 64u);
+                const float4 shift = four_of(info + 32u), back = four_of(info + 64u);
 #pragma unroll
                 for (int gr = 0; gr < 4; ++gr) {
                     const float f = gr == 0 ? keys.x : gr == 1 ? keys.y : gr == 2 ? keys.z : keys.w;
@@ -258,12 +267,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     }
                     part[0] = add_pair(part[0], part[1]);
                     sum = fmaf(part[0].x + part[0].y, gr == 0 ? back.x : gr == 1 ? back.y : gr == 2 ? back.z : back.w, sum);
-                    tmem_st8u(s_t + 32u * (uint32_t)half + 8u * gr, p);
+                    tmem_st8u(s_t + 16u * (uint32_t)half + (gr < 2 ? 8u * gr : 16u + 8u * gr), p);
+                    if (gr & 1) {
+                        tmem_wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile][gr >> 1]));
+                    }
                 }
-                tmem_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&p_ready[tile][half]));
             }
         }
         // ---------------- out ----------------
