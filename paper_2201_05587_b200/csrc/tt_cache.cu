@@ -11,41 +11,54 @@ namespace tt {
 // The new tokens of one page and head, of the keys or of the values, are a CTA's, or a warp's where there are few of them: read once into registers
 // (what is more than kHeld pieces a thread is read again, from the caches), their maximum, their conversion; where the page holds
 // tokens already and the scale has to rise, those are brought to it.
+//   Bytes are the bound, but a page is only some thousands of values, so what each thread does once counts as much: addresses are stepped, not
+// divided for.
+constexpr int kAppendThreads = 128;         // of a CTA that has a page
 template <int TYPE, bool WIDE, bool WARP>
-__global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_append_args a) {
-    __shared__ float warp_most[8];
+__global__ void __launch_bounds__(WARP ? 256 : kAppendThreads, WARP ? 3 : 7) tt_cache_append_kernel(const tt_cache_append_args a) {
+    __shared__ float warp_most[kAppendThreads / 32];
     typedef typename Element<TYPE>::type T;
     pdl_allow_next();
     pdl_wait_prev();
     const tt_cache& c = a.cache;
     const int which = WARP ? (int)blockIdx.y * 8 + ((int)threadIdx.x >> 5) : (int)blockIdx.y, head = which >> 1, w = which & 1;
     const int me = WARP ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    constexpr int kThreads = WARP ? 32 : 256;
+    constexpr int kThreads = WARP ? 32 : kAppendThreads;
     if (WARP && head >= c.heads) return;
+    const int shift = 31 - __clz(c.block);                  // (a power of two)
     long long first_unit;
-    const int b = sequence_of(a.starts, c.batch, 1, c.block, 2, blockIdx.x, first_unit);
+    int b;
+    const bool found = sequence_of(a.starts, c.batch, [&](int start, int i) { return (start >> shift) + 2 * i; }, blockIdx.x, b, first_unit);
     const int start = a.starts[b], count = a.starts[b + 1] - start, length = a.lengths[b];
-    if (count == 0) return;
-    if (count < 0 || start < 0 || start + (long long)count > a.tokens || length < count || length > (long long)c.max_pages * c.block) {
+    if (found && count == 0) return;
+    if (!found || count < 0 || start < 0 || start + (long long)count > a.tokens || length < count || length > (long long)c.max_pages * c.block) {
         if (me == 0) report_invalid(a.status);
         return;
     }
     const int first = length - count;                       // position of the first new token
-    const long long index = first / c.block + ((long long)blockIdx.x - first_unit);
-    if (index * c.block >= length) return;
-    const int lo = max(first, (int)index * c.block), hi = min(length, (int)index * c.block + c.block);
-    const int held = lo - (int)index * c.block;             // tokens that the page holds already
-    constexpr int kPiece = WIDE ? 8 : 1, kHeld = WIDE ? 4 : 16;      // values a thread takes at a time, and how often it keeps them
-    const int pieces = c.d / kPiece, total = (hi - lo) * pieces;
-    const T* x = static_cast<const T*>(a.x[w]) + ((long long)(start + (lo - first)) * a.x_token[w] + (long long)head * a.x_head[w]);
-    const auto place = [&](int e, int& t, int& i) { t = e / pieces; i = (e - t * pieces) * kPiece; };
+    const long long index = (first >> shift) + ((long long)blockIdx.x - first_unit);
+    if (index << shift >= length) return;
+    const int lo = max(first, (int)index << shift), hi = (int)min((long long)length, (index + 1) << shift);
+    const int held = lo - ((int)index << shift);            // tokens that the page holds already
+    constexpr int kPiece = WIDE ? 8 : 1, kHeld = WIDE ? (WARP || TYPE == TT_TYPE_F32 ? 4 : 8) : 16;      // values a thread takes at a time, and how often it keeps them
+    const int pieces = c.d / kPiece;
+    // A thread's pieces are kThreads apart: value i of token t, then di values and dt tokens further on.
+    const int t0 = me / pieces, i0 = (me - t0 * pieces) * kPiece, dt = kThreads / pieces, di = (kThreads - dt * pieces) * kPiece;
+    const int n = ((hi - lo) * pieces - me + kThreads - 1) / kThreads;      // of them
+    const T* const x = static_cast<const T*>(a.x[w]) + ((long long)(start + (lo - first)) * a.x_token[w] + (long long)head * a.x_head[w]);
+    struct Walk {
+        int i; long long at;                                // the value of its token, and its place
+        __device__ __forceinline__ void next(int d, int di, long long step, long long wrap) {
+            i += di; at += step;
+            if (i >= d) { i -= d; at += wrap; }
+        }
+    };
+    const long long x_token = a.x_token[w], x_step = dt * x_token + di, x_wrap = x_token - c.d;
     struct One { float v; };
     typedef typename std::conditional<WIDE, Eights<TYPE, 1>, One>::type Piece;
-    const auto load = [&](int e, Piece& u) {
-        int t, i;
-        place(e, t, i);
-        if constexpr (WIDE) u.load(x + t * a.x_token[w], i, 0, c.d, true);
-        else u.v = Element<TYPE>::up(x[t * a.x_token[w] + i]);
+    const auto load = [&](const Walk& p, Piece& u) {
+        if constexpr (WIDE) u.load(x + p.at, 0, 0, 8, true);
+        else u.v = Element<TYPE>::up(x[p.at]);
     };
     // the largest finite magnitude of u and m; nan: whether there is one that is not
     const auto more = [&](const Piece& u, float m, bool& odd) {
@@ -60,8 +73,9 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
         }
     };
     Piece v[kHeld];
+    Walk p{i0, t0 * x_token + i0};
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) load(me + k * kThreads, v[k]);      // (on their way while the page is looked up)
+    for (int k = 0; k < kHeld; ++k, p.next(c.d, di, x_step, x_wrap)) if (k < n) load(p, v[k]);      // (on their way while the page is looked up)
     const int page = c.table[b * c.table_row + index];
     if (page < 0 || page >= c.pages) {
         if (me == 0) report_invalid(a.status);
@@ -72,11 +86,14 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
     float most = 0.f;
     bool odd = false;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) most = more(v[k], most, odd);
-    for (int e = me + kHeld * kThreads; e < total; e += kThreads) {
-        Piece u;
-        load(e, u);
-        most = more(u, most, odd);
+    for (int k = 0; k < kHeld; ++k) if (k < n) most = more(v[k], most, odd);
+    if (n > kHeld) {
+        Walk more_of = p;
+        for (int k = kHeld; k < n; ++k, more_of.next(c.d, di, x_step, x_wrap)) {
+            Piece u;
+            load(more_of, u);
+            most = more(u, most, odd);
+        }
     }
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
@@ -85,29 +102,27 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
         if ((me & 31) == 0) warp_most[me >> 5] = most;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 8; ++i) most = fmaxf(most, warp_most[i]);
+        for (int k = 0; k < kAppendThreads / 32; ++k) most = fmaxf(most, warp_most[k]);
     }
     float s = power_scale(most);
     if (held > 0 && old >= s) s = old;
     if (me == 0 && (held == 0 || s != old)) *scale = s;
-    uint8_t* data = static_cast<uint8_t*>(c.data[w]) + page * c.page[w] + head * c.head[w];
+    uint8_t* const data = static_cast<uint8_t*>(c.data[w]) + page * c.page[w] + head * c.head[w];
     if (held > 0 && s != old) {
         // (a ratio of powers of two as the calls here leave them; a scale of another origin is taken as it is)
         const float ratio = __fdiv_rn(old, s);
         const int words = c.d / 4;
         for (int e = me; e < held * words; e += kThreads) {
-            const int t = e / words;
-            uint32_t* p = reinterpret_cast<uint32_t*>(data + t * c.token[w]) + (e - t * words);
-            const uint32_t q = *p;
-            *p = to_e4m3x4(float_of_e4m3(q) * ratio, float_of_e4m3(q >> 8) * ratio, float_of_e4m3(q >> 16) * ratio, float_of_e4m3(q >> 24) * ratio);
+            const int row = e / words;
+            uint32_t* q = reinterpret_cast<uint32_t*>(data + row * c.token[w]) + (e - row * words);
+            const uint32_t n = *q;
+            *q = to_e4m3x4(float_of_e4m3(n) * ratio, float_of_e4m3(n >> 8) * ratio, float_of_e4m3(n >> 16) * ratio, float_of_e4m3(n >> 24) * ratio);
         }
     }
     const bool power = (__float_as_int(s) & 0x7fffff) == 0 && s >= 1.17549435e-38f && s <= 1.329227996e36f;      // 2^-126 .. 2^120
     const float inv = power ? power_inverse(s) : 0.f;
-    const auto put = [&](int e, const Piece& u) {
-        int t, i;
-        place(e, t, i);
-        uint8_t* q = data + (long long)(held + t) * c.token[w] + i;
+    uint8_t* const to = data + held * c.token[w];
+    const auto put = [&](const Walk& p, const Piece& u) {
         if constexpr (WIDE) {
             uint2 out;
             if (power) out = odd ? u.template bytes<false>(0, inv) : u.template bytes<true>(0, inv);
@@ -116,15 +131,17 @@ __global__ void __launch_bounds__(256) tt_cache_append_kernel(const tt_cache_app
                 out.x = to_e4m3x4(__fdiv_rn(p0.x, s), __fdiv_rn(p0.y, s), __fdiv_rn(p1.x, s), __fdiv_rn(p1.y, s));
                 out.y = to_e4m3x4(__fdiv_rn(p2.x, s), __fdiv_rn(p2.y, s), __fdiv_rn(p3.x, s), __fdiv_rn(p3.y, s));
             }
-            *reinterpret_cast<uint2*>(q) = out;
-        } else *q = (uint8_t)to_e4m3x4(power ? u.v * inv : __fdiv_rn(u.v, s), 0.f, 0.f, 0.f);
+            *reinterpret_cast<uint2*>(to + p.at) = out;
+        } else to[p.at] = (uint8_t)to_e4m3x4(power ? u.v * inv : __fdiv_rn(u.v, s), 0.f, 0.f, 0.f);
     };
+    Walk q{i0, t0 * c.token[w] + i0};
+    const long long q_step = dt * c.token[w] + di, q_wrap = c.token[w] - c.d;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) if (me + k * kThreads < total) put(me + k * kThreads, v[k]);
-    for (int e = me + kHeld * kThreads; e < total; e += kThreads) {
+    for (int k = 0; k < kHeld; ++k, q.next(c.d, di, q_step, q_wrap)) if (k < n) put(q, v[k]);
+    for (int k = kHeld; k < n; ++k, q.next(c.d, di, q_step, q_wrap), p.next(c.d, di, x_step, x_wrap)) {
         Piece u;
-        load(e, u);
-        put(e, u);
+        load(p, u);
+        put(q, u);
     }
 }
 
@@ -845,7 +862,7 @@ extern "C" tt_status tt_cache_append(const tt_cache_append_args* a, void* stream
     // A warp has a page's tokens where there is hardly more than one of them, a CTA where there are many.
     const bool warp = (long long)(a->tokens / c.batch < c.block ? a->tokens / c.batch : c.block) * c.d <= 1024;
     const dim3 grid((unsigned)units, warp ? (2u * (unsigned)c.heads + 7u) / 8u : 2u * (unsigned)c.heads, 1);
-    const auto go = [&](auto by_warp, auto by_cta) { return status_of(launch(warp ? by_warp : by_cta, grid, 256, 0, 1, stream, *a)); };
+    const auto go = [&](auto by_warp, auto by_cta) { return status_of(launch(warp ? by_warp : by_cta, grid, warp ? 256 : kAppendThreads, 0, 1, stream, *a)); };
 #define TT_APPEND(TYPE) (wide ? go(tt_cache_append_kernel<TYPE, true, true>, tt_cache_append_kernel<TYPE, true, false>) : go(tt_cache_append_kernel<TYPE, false, true>, tt_cache_append_kernel<TYPE, false, false>))
     return a->type == TT_TYPE_F32 ? TT_APPEND(TT_TYPE_F32) : a->type == TT_TYPE_F16 ? TT_APPEND(TT_TYPE_F16) : TT_APPEND(TT_TYPE_BF16);
 #undef TT_APPEND

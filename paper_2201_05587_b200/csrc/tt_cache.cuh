@@ -7,28 +7,33 @@ namespace tt {
 
 __device__ __forceinline__ void report_invalid(unsigned* status) { atomicCAS(status, 0u, (unsigned)TT_ERR_INVALID_ARG); }
 
-// Work that is dealt by sequences of unknown sizes: sequence b owns the units starts[b] * mul / per + extra * b and up (as many as it can need
-// at most).  The whole warp looks for a unit's, 32 places at a time (a lane on its own would take the logarithm of the batch in loads, one after the other).
-__device__ __forceinline__ int sequence_of(const int* starts, int batch, long long mul, long long per, int extra, long long unit, long long& first) {
+// Work that is dealt by sequences of unknown sizes: sequence b owns the units begin(starts[b], b) and up (as many as it can need at most).  The
+// whole warp looks for a unit's, 32 places at a time (a lane on its own would take the logarithm of the batch in loads, one after the other).
+// False if the unit is in front of all (the starts do not rise from 0).
+template <class BEGIN>
+__device__ __forceinline__ bool sequence_of(const int* starts, int batch, const BEGIN& begin_of, long long unit, int& b, long long& first) {
     const int lane = threadIdx.x & 31;
-    const auto begin = [&](int b) { return starts[b] * mul / per + (long long)extra * b; };
+    const auto begin = [&](int i) { return (long long)begin_of(starts[i], i); };
     if (batch <= 128) {                                      // all places at once
-        int in = 0;
+        int in = __popc(__ballot_sync(0xffffffffu, lane < batch && begin(lane) <= unit));
+        if (batch > 32) {
 #pragma unroll
-        for (int i = 0; i < 128; i += 32) in += __popc(__ballot_sync(0xffffffffu, i + lane < batch && begin(i + lane) <= unit));
-        first = begin(max(0, in - 1));
-        return max(0, in - 1);
+            for (int i = 32; i < 128; i += 32) in += __popc(__ballot_sync(0xffffffffu, i + lane < batch && begin(i + lane) <= unit));
+        }
+        b = max(0, in - 1);
+    } else {
+        int n = batch;                                       // it is one of b .. b + n - 1
+        b = 0;
+        while (n > 1) {
+            const int step = (n + 31) / 32, i = b + lane * step;
+            const unsigned in = __ballot_sync(0xffffffffu, lane * step < n && begin(i) <= unit);
+            const int last = in ? 31 - __clz((int)in) : 0;   // (places rise; whatever they hold, the result is one of the batch)
+            n = min(step, n - last * step);
+            b += last * step;
+        }
     }
-    int lo = 0, n = batch;                                   // it is one of lo .. lo + n - 1
-    while (n > 1) {
-        const int step = (n + 31) / 32, b = lo + lane * step;
-        const unsigned in = __ballot_sync(0xffffffffu, lane * step < n && begin(b) <= unit);
-        const int last = in ? 31 - __clz((int)in) : 0;       // (places rise; whatever they hold, the result is one of the batch)
-        n = min(step, n - last * step);
-        lo += last * step;
-    }
-    first = begin(lo);
-    return lo;
+    first = begin(b);
+    return first <= unit;
 }
 
 constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it
@@ -62,18 +67,20 @@ struct TileView {
 __device__ __forceinline__ bool view_tile(const Attend& g, int tile_rows, long long unit, TileView& v) {
     const tt_cache& c = g.a.cache;
     long long first_unit = unit;
-    v.b = g.by_sequence ? (int)unit : sequence_of(g.a.starts, c.batch, g.group, tile_rows, 1, unit, first_unit);
+    bool found = true;
+    if (g.by_sequence) v.b = (int)unit;
+    else found = sequence_of(g.a.starts, c.batch, [&](int start, int b) { return (long long)start * g.group / tile_rows + b; }, unit, v.b, first_unit);
     v.start = g.a.starts[v.b];
     const int count = g.a.starts[v.b + 1] - v.start, length = g.a.lengths[v.b];
-    if (count == 0) return false;
-    if (count < 0 || v.start < 0 || v.start + (long long)count > g.a.tokens || length < 0 || length > g.max_length || (g.a.max_count > 0 && count > g.a.max_count)) {
+    if (found && count == 0) return false;
+    if (!found || count < 0 || v.start < 0 || v.start + (long long)count > g.a.tokens || length < 0 || length > g.max_length || (g.a.max_count > 0 && count > g.a.max_count)) {
         if (threadIdx.x == 0) report_invalid(g.a.status);
         return false;
     }
     const long long row0 = (unit - first_unit) * tile_rows, all = (long long)count * g.group;
     if (row0 >= all || all < g.least || all > g.most) return false;
     v.rows = (int)min((long long)tile_rows, all - row0);
-    v.t0 = (int)(row0 / g.group);
+    v.t0 = (int)((unsigned)row0 / (unsigned)g.group);       // (all rows of a sequence are less than 2^31)
     v.h0 = (int)(row0 - (long long)v.t0 * g.group);
     const int t1 = v.t0 + (v.h0 + v.rows - 1) / g.group;
     v.before = length - count;

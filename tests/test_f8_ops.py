@@ -625,6 +625,18 @@ def test_append_reports_what_only_the_device_sees():
         assert call.status() == B.TT_OK                         # (the look clears it)
 
 
+@gpu
+def test_append_reports_starts_that_do_not_rise_from_0():
+    p = Pages([80, 80], 1, 32, 16, seed=1)
+    before = p.k.view(torch.uint8).clone(), p.ks.clone()
+    x = torch.randn(200, 1, 32, generator=gen(1), device="cuda")
+    for starts in ([100, 110, 120], [100, 90, 120], [-40, -20, 0]):
+        call = B.cache_append(p.cache(), x, x, int32(starts), int32([0, 0]))
+        call.run()
+        assert call.status() == B.TT_ERR_INVALID_ARG, starts
+    assert torch.equal(before[0], p.k.view(torch.uint8)) and torch.equal(before[1], p.ks)
+
+
 # ---- GPU: attention ---------------------------------------------------------------------------------------------------------
 def reference_attention(p, counts, q, scale, causal, window):
     """Outputs and bounds of their errors in 64 bits, [tokens, heads_q, d]."""
@@ -839,6 +851,20 @@ def test_attention_reports_what_only_the_device_sees():
         call = B.cache_attention(p.cache(), q, torch.empty_like(q), int32([0, 2]), int32([20]), 0.1, **bound)
         call.run()
         assert call.status() == B.TT_ERR_INVALID_ARG, bound
+
+
+@gpu
+@pytest.mark.parametrize("heads_q,max_count", [(8, 0), (8, 2), (64, 0)])
+def test_attention_reports_starts_that_do_not_rise_from_0(heads_q, max_count):
+    p = Pages([80, 80], 1, 64, 16, seed=1)
+    q = torch.randn(200, heads_q, 64, generator=gen(1), device="cuda").to(torch.float16)
+    for starts in ([100, 102, 104], [100, 90, 104], [-40, -20, 0]):
+        y = torch.full_like(q, 7.0)
+        call = B.cache_attention(p.cache(), q, y, int32(starts), int32(p.lengths), 0.1, max_count=max_count)
+        call.run()
+        if max_count == 0 or starts[0] < 0 or starts[1] < starts[0]:
+            assert call.status() == B.TT_ERR_INVALID_ARG, starts
+        assert (y[:max(0, min(starts))] == 7.0).all()          # (a sequence whose own starts rise has its rows)
 
 
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
