@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2], raw_full[2], raw_empty[2], drained;
     __shared__ StepScales scales[4];
-    __shared__ int nan_first[D], nan_last[D];
+    __shared__ int nan_first[D], nan_last[D], nan_any;
+    __shared__ uint8_t sizes[kPromptRows];                                // of the queries' rows: the exponents of what they were multiplied by
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag, last_one;
 
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         mbar_init(smem_u32(&raw_full[0]), 1u); mbar_init(smem_u32(&raw_full[1]), 1u);
         mbar_init(smem_u32(&raw_empty[0]), 4u); mbar_init(smem_u32(&raw_empty[1]), 4u);
         mbar_init(smem_u32(&drained), 1u);
-        abort_flag = 0;
+        abort_flag = nan_any = 0;
         fence_mbar_init();
         fence_proxy_async_shared();
     }
@@ -141,41 +142,53 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     // a softmax thread's row
     const int tile = warp >> 3, half = (warp >> 2) & 1, r = tile * 128 + (int)(threadIdx.x & 127);      // (a half of its columns)
     const bool mine = warp < 16 && r < view.rows;
-    const int row_t = view.t0 + (view.h0 + r) / g.group, row_h = head * g.group + (view.h0 + r) % g.group;
+    const int row_t = view.t0 + (view.h0 + r) / g.group;
     float top = -INFINITY, used = 0.f, sum = 0.f, ref = 0.f;              // maximum; the one that O and the sum are relative to; the unit of O
     bool fine = true;
 
     if (warp < 16) {
         registers_up<96>();
         // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
-        const int lr = r & 127;
-        const long long at = (view.start + (long long)row_t) * g.a.q_token + (long long)row_h * g.a.q_head;
-        float most = 0.f;
-        if (mine) {
-#pragma unroll 8
-            for (int i = 0; i < D; i += 4) {
-                float v[4];
-                load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
+        // A warp has 16 rows of its tile, a row (two of 64) at a time, so that what it loads lies side by side.
+        {
+            constexpr int kAcross = D / 4, kAtOnce = 32 / kAcross;
+            const int i = lane % kAcross * 4;
+            int row = tile * 128 + (warp & 7) * 16 + lane / kAcross, t = (view.h0 + row) / g.group, h = view.h0 + row - t * g.group;
+            long long at = ((long long)view.start + view.t0 + t) * g.a.q_token + (long long)(head * g.group + h) * g.a.q_head + i;
+            const uint32_t to_ = q_s + (uint32_t)tile * S::kTile + (uint32_t)(i / 8 % S::kAtoms) * kAtom + (uint32_t)(i & 4) * 2u, chunk = (uint32_t)(i / (8 * S::kAtoms));
+#pragma unroll 1
+            for (int k = 0; k < 16; k += 8 * kAtOnce) {
+                uint2 raw[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most = finite_max(most, v[e]);
+                for (int e = 0; e < 8; ++e) {
+                    raw[e] = row + e * kAtOnce < view.rows ? raw_four(g.a.q, at, g.q_wide) : make_uint2(0u, 0u);
+#pragma unroll
+                    for (int next = 0; next < kAtOnce; ++next) {
+                        at += g.a.q_head;
+                        if (++h == g.group) { h = 0; at += g.a.q_token - g.group * g.a.q_head; }
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e, row += kAtOnce) {
+                    float v[4];
+                    four_of(raw[e], g.a.type, v);
+                    float most = finite_max(finite_max(finite_max(finite_max(0.f, v[0]), v[1]), v[2]), v[3]);
+#pragma unroll
+                    for (int d = 1; d < kAcross; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                    const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14, size = min(254, max(1, 127 + 14 + 127 - ex));
+                    const float up = __int_as_float(size << 23 | (g.scale_log2 < 0.f ? 1 << 31 : 0));      // (the factor of the scores is positive: their maximum is the products')
+                    const int lr = row & 127;
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to_ + (uint32_t)lr * 128u + ((chunk ^ (uint32_t)(lr & 7)) << 4)),
+                                 "r"(down2<TT_TYPE_F16>(v[0] * up, v[1] * up)), "r"(down2<TT_TYPE_F16>(v[2] * up, v[3] * up)) : "memory");
+                    if (i == 0) sizes[row] = (uint8_t)size;
+                }
             }
-        }
-        const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14;
-        const float size = __int_as_float((min(254, max(1, 127 + 14 + 127 - ex))) << 23);
-        const float up = g.scale_log2 < 0.f ? -size : size;               // (the factor of the scores is positive: their maximum is the products')
-        const float factor = fabsf(g.scale_log2) / size;
-        const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)lr * 128u;
-#pragma unroll 8
-        for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 4) {
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (mine) load_four(g.a.q, at + i, g.a.type, g.q_wide, v);
-            const uint32_t to_ = line + (uint32_t)(i / 8 % S::kAtoms) * kAtom + (((uint32_t)(i / (8 * S::kAtoms)) ^ (uint32_t)(lr & 7)) << 4) + (uint32_t)(i & 4) * 2u;
-            st_shared_u32(to_, down2<TT_TYPE_F16>(v[0] * up, v[1] * up));
-            st_shared_u32(to_ + 4u, down2<TT_TYPE_F16>(v[2] * up, v[3] * up));
         }
         fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&q_full));
+        named_sync(4 + tile, 256);
+        const float factor = fabsf(g.scale_log2) / __int_as_float((int)sizes[r] << 23);
 
         // ---------------- softmax ----------------
         const int row_pos = view.before + row_t;                          // the row sees tokens row_lo .. row_hi - 1
@@ -280,7 +293,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         // ---------------- out ----------------
         named_sync(1, kSoftmax + 128);                                               // (every NaN of the steps at the edges has been noted)
         const long long place = unit * c.heads + head;
-        constexpr int kPart = kPromptRows * (D + 2);
+        constexpr int kPart = kPromptRows * (D + 2);                     // O by eight columns of all rows, then the rows' maxima and sums
         const auto store = [&](int rr, int i, const float (&v)[4]) {
             const int tt = (view.h0 + rr) / g.group;
             store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
@@ -297,36 +310,70 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 tc_fence_after();
                 sum += tmem_ld1(s_t + (half ? 32u : 64u));
             }
-            if (fine) {
-                const int pos = row_pos;
-                const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
-                // O is in units of 2^4 and the largest scale; a split's part stays relative to its sum
-                const float unit_o = ref * 0.0625f * (active == 1 ? 1.f / sum : 1.f);
-                float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)r * D;
+            const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
+            // O is in units of 2^4 and the largest scale; a split's part stays relative to its sum
+            const float unit_o = ref * 0.0625f * (active == 1 ? 1.f / sum : 1.f);
+            float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + 8 * r;
+            const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)(r & 127) * (2u * D);      // (where the queries were)
 #pragma unroll 1
-                for (int h = half * (D / 2); h < (half + 1) * (D / 2); h += 32) {
-                    uint32_t v[32];
-                    if (steps > 0) {
-                        tmem_ld32(o_t + (uint32_t)h, v);
-                        tmem_wait_ld();
+            for (int h = half * (D / 2); h < (half + 1) * (D / 2); h += 16) {
+                uint32_t v[16];
+                if (steps > 0) {
+                    tmem_ld8u(o_t + (uint32_t)h, v);
+                    tmem_ld8u(o_t + (uint32_t)h + 8u, v + 8);
+                    tmem_wait_ld();
+                }
+#pragma unroll
+                for (int j = 0; j < 16; j += 8) {
+                    const int n = h + j, first = n % 64 / 8 * 8 * S::kAtoms + n / 64 * 8;      // the place of columns n .. n + 7 in the head
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = none ? 0.f : __uint_as_float(v[j + e]) * unit_o;
+                    if (nan_any) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (nan_first[first + e] <= row_pos || (g.a.window > 0 && nan_last[first + e] > row_pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
                     }
-                    if (mine) {
+                    if (active == 1) {
+                        const bool f16 = g.a.type == TT_TYPE_F16;
+                        uint32_t w[4];
 #pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const int n = h + j, first = n % 64 / 8 * 8 * S::kAtoms + n / 64 * 8 + n % 8;      // the place of column n in the head
-                            float x[4];
+                        for (int e = 0; e < 4; ++e) w[e] = f16 ? down2<TT_TYPE_F16>(x[2 * e], x[2 * e + 1]) : down2<TT_TYPE_BF16>(x[2 * e], x[2 * e + 1]);
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(line + (((uint32_t)(first >> 3) ^ (uint32_t)(r & 7)) << 4)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+                    } else if (mine && fine) {
+                        *reinterpret_cast<float4*>(left + first * kPromptRows) = make_float4(x[0], x[1], x[2], x[3]);
+                        *reinterpret_cast<float4*>(left + first * kPromptRows + 4) = make_float4(x[4], x[5], x[6], x[7]);
+                    }
+                }
+            }
+            if (active > 1 && mine && fine && half == 0) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, none ? 0.f : sum);
+            if (active == 1) {
+                named_sync(4 + tile, 256);
+                // rows of a tile to its warps, so that what a warp stores lies side by side
+                constexpr int kAcross = D / 8, kAtOnce = 32 / kAcross;
+                const int i = lane % kAcross;
+                int row = tile * 128 + (warp & 7) * 16 + lane / kAcross, t = (view.h0 + row) / g.group, h = view.h0 + row - t * g.group;
+                long long at = ((long long)view.start + view.t0 + t) * g.a.y_token + (long long)(head * g.group + h) * g.a.y_head + 8 * i;
+#pragma unroll 4
+                for (int k = 0; k < 16; k += kAtOnce, row += kAtOnce) {
+                    uint32_t w[4];
+                    read_shared<16>(q_s + (uint32_t)row * (2u * D) + (((uint32_t)i ^ (uint32_t)(row & 7)) << 4), w);
+                    if (row < view.rows && fine) {
+                        uint16_t* y = static_cast<uint16_t*>(g.a.y) + at;
+                        if (g.y_wide) {
+                            *reinterpret_cast<uint2*>(y) = make_uint2(w[0], w[1]);
+                            *reinterpret_cast<uint2*>(y + 4) = make_uint2(w[2], w[3]);
+                        } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                x[e] = none ? 0.f : __uint_as_float(v[j + e]) * unit_o;
-                                if (nan_first[first + e] <= pos || (g.a.window > 0 && nan_last[first + e] > pos - g.a.window)) x[e] = __int_as_float(0x7fffffff);
-                            }
-                            if (active == 1) store(r, first, x);
-                            else *reinterpret_cast<float4*>(left + first) = make_float4(x[0], x[1], x[2], x[3]);
+                            for (int e = 0; e < 8; ++e) y[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
                         }
                     }
-                    __syncwarp();
+#pragma unroll
+                    for (int next = 0; next < kAtOnce; ++next) {
+                        at += g.a.y_head;
+                        if (++h == g.group) { h = 0; at += g.a.y_token - g.group * g.a.y_head; }
+                    }
                 }
-                if (active > 1 && mine && half == 0) *reinterpret_cast<float2*>(g.partial + (place * g.splits + blockIdx.z) * kPart + (long long)kPromptRows * D + 2 * r) = make_float2(used, none ? 0.f : sum);
             }
         }
         tc_fence_before();
@@ -364,7 +411,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             float v[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
             for (int z = 0; z < active; ++z) {
-                const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (long long)rr * D + i));
+                const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (i >> 3) * (8 * kPromptRows) + 8 * rr + (i & 4)));
                 const float w = share[z * kPromptRows + rr];
                 v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
             }
@@ -429,6 +476,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     for (int q = 0; q < kPiece / 4; ++q) {
                         const uint32_t n = nan_bytes(w[q]);
                         if (n == 0u) continue;
+                        nan_any = 1;
                         for (int e = 0; e < 4; ++e)
                             if ((n >> (8 * e)) & 0x80u) {
                                 if (high) atomicMin(&nan_first[kPiece * piece + 4 * q + e], t + 16 * p + sub);
