@@ -349,8 +349,16 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             if (r < rows) {
                 const int2 at = q_row(r);
                 const long long first = at.x * g.a.q_token + at.y * g.a.q_head + cq * S::kKey;
+                uint2 raw[D / 16];
+                const auto load = [&](auto wide) {
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) load_four(g.a.q, first + i / (S::kKey / 4) * 4 * S::kKey + i % (S::kKey / 4) * 4, g.a.type, g.q_wide, v[i]);
+                    for (int i = 0; i < D / 16; ++i) raw[i] = raw_four(g.a.q, first + i / (S::kKey / 4) * 4 * S::kKey + i % (S::kKey / 4) * 4, decltype(wide)::value);
+                };
+                // (a branch for all loads: one for each makes them wait for each other)
+                if (g.q_wide) load(std::integral_constant<int, 1>());
+                else load(std::integral_constant<int, 0>());
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) four_of(raw[i], g.a.type, v[i]);
             } else {
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i)
@@ -743,8 +751,12 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
     g.scale_log2 = a.scale * 1.4426950408889634f;
     g.max_length = c.pages > 0 ? c.max_pages * c.block : 0;
     if (a.max_length > 0 && a.max_length < g.max_length) g.max_length = a.max_length;
-    g.q_wide = reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.q_token % 4 == 0 && a.q_head % 4 == 0;
-    g.y_wide = reinterpret_cast<uintptr_t>(a.y) % 8 == 0 && a.y_token % 4 == 0 && a.y_head % 4 == 0;
+    const auto wide = [](const void* p, long long token, long long head) {
+        const auto at = [&](int n) { return reinterpret_cast<uintptr_t>(p) % (2 * n) == 0 && token % n == 0 && head % n == 0; };
+        return at(8) ? 2 : at(4) ? 1 : 0;
+    };
+    g.q_wide = wide(a.q, a.q_token, a.q_head);
+    g.y_wide = wide(a.y, a.y_token, a.y_head);
     const int count = c.batch > 1 && a.max_count > 0 && a.max_count < a.tokens ? a.max_count : a.tokens;
     const long long most_rows = (long long)count * g.group;
     if (most_rows > 0x7fffffff) return TT_ERR_INVALID_ARG;

@@ -46,7 +46,7 @@ struct Attend {
     int span, share;                        // tokens that a tile can see; CTAs that all tokens are dealt to
     int least, most;                        // rows of the sequences that the kernel takes
     int by_sequence;                        // no more than one tile each: tile b is sequence b's
-    int q_wide, y_wide;                     // four values of q, of y at a time
+    int q_wide, y_wide;                     // values of q, of y at a time: four (1) or eight (2)
     float scale_log2;                       // the scale times log2(e)
     unsigned* counters; float* partial;
 };
@@ -110,6 +110,11 @@ __device__ __forceinline__ uint2 raw_four(const void* p, long long i, int wide) 
     const uint16_t* x = static_cast<const uint16_t*>(p) + i;
     if (wide) return *reinterpret_cast<const uint2*>(x);
     return make_uint2((uint32_t)x[0] | (uint32_t)x[1] << 16, (uint32_t)x[2] | (uint32_t)x[3] << 16);
+}
+__device__ __forceinline__ uint4 raw_eight(const void* p, long long i, int wide) {
+    if (wide == 2) return *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+    const uint2 a = raw_four(p, i, wide), b = raw_four(p, i + 4, wide);
+    return make_uint4(a.x, a.y, b.x, b.y);
 }
 __device__ __forceinline__ void four_of(uint2 u, int type, float (&v)[4]) {
     const float2 a = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.x) : up2<TT_TYPE_BF16>(u.x), b = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.y) : up2<TT_TYPE_BF16>(u.y);

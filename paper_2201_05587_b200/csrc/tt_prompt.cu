@@ -149,41 +149,50 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     if (warp < 16) {
         registers_up<96>();
         // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
-        // A warp has 16 rows of its tile, a row (two of 64) at a time, so that what it loads lies side by side.
-        {
-            constexpr int kAcross = D / 4, kAtOnce = 32 / kAcross;
-            const int i = lane % kAcross * 4;
-            int row = tile * 128 + (warp & 7) * 16 + lane / kAcross, t = (view.h0 + row) / g.group, h = view.h0 + row - t * g.group;
-            long long at = ((long long)view.start + view.t0 + t) * g.a.q_token + (long long)(head * g.group + h) * g.a.q_head + i;
-            const uint32_t to_ = q_s + (uint32_t)tile * S::kTile + (uint32_t)(i / 8 % S::kAtoms) * kAtom + (uint32_t)(i & 4) * 2u, chunk = (uint32_t)(i / (8 * S::kAtoms));
-#pragma unroll 1
-            for (int k = 0; k < 16; k += 8 * kAtOnce) {
-                uint2 raw[8];
+        // Eight lanes have a row, a warp 16 rows of its tile: what it loads lies side by side.  (A thread a row, 32 lines at a time, took 20000
+        // cycles, a third of a tile of 1024 tokens; the same by four values a lane took 9500, in instructions.)
+        const auto stage = [&](auto type) {
+            constexpr int TYPE = decltype(type)::value, kPieces = D / 64;
+            const int row0 = tile * 128 + (warp & 7) * 16 + (lane >> 3);
+            int t = (view.h0 + row0) / g.group, h = view.h0 + row0 - t * g.group;
+            long long at = ((long long)view.start + view.t0 + t) * g.a.q_token + (long long)(head * g.group + h) * g.a.q_head + 8 * (lane & 7);
+            Eights<TYPE, kPieces> x[4];
+            const auto load = [&](auto wide) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    raw[e] = row + e * kAtOnce < view.rows ? raw_four(g.a.q, at, g.q_wide) : make_uint2(0u, 0u);
+                for (int k = 0; k < 4; ++k) {
 #pragma unroll
-                    for (int next = 0; next < kAtOnce; ++next) {
-                        at += g.a.q_head;
-                        if (++h == g.group) { h = 0; at += g.a.q_token - g.group * g.a.q_head; }
-                    }
+                    for (int p = 0; p < kPieces; ++p) x[k].raw[p] = row0 + 4 * k < view.rows ? raw_eight(g.a.q, at + 64 * p, decltype(wide)::value) : make_uint4(0u, 0u, 0u, 0u);
+                    h += 4; at += 4 * g.a.q_head;
+                    while (h >= g.group) { h -= g.group; at += g.a.q_token - g.group * g.a.q_head; }
                 }
+            };
+            // (a branch for all loads: one for each makes them wait for each other)
+            if (g.q_wide == 2) load(std::integral_constant<int, 2>());
+            else if (g.q_wide == 1) load(std::integral_constant<int, 1>());
+            else load(std::integral_constant<int, 0>());
 #pragma unroll
-                for (int e = 0; e < 8; ++e, row += kAtOnce) {
-                    float v[4];
-                    four_of(raw[e], g.a.type, v);
-                    float most = finite_max(finite_max(finite_max(finite_max(0.f, v[0]), v[1]), v[2]), v[3]);
+            for (int k = 0; k < 4; ++k) {
+                float most = x[k].most();
+                if (!(most < INFINITY)) most = x[k].finite_most();
 #pragma unroll
-                    for (int d = 1; d < kAcross; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
-                    const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14, size = min(254, max(1, 127 + 14 + 127 - ex));
-                    const float up = __int_as_float(size << 23 | (g.scale_log2 < 0.f ? 1 << 31 : 0));      // (the factor of the scores is positive: their maximum is the products')
-                    const int lr = row & 127;
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to_ + (uint32_t)lr * 128u + ((chunk ^ (uint32_t)(lr & 7)) << 4)),
-                                 "r"(down2<TT_TYPE_F16>(v[0] * up, v[1] * up)), "r"(down2<TT_TYPE_F16>(v[2] * up, v[3] * up)) : "memory");
-                    if (i == 0) sizes[row] = (uint8_t)size;
+                for (int d = 1; d < 8; d <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, d));
+                const int ex = most > 0.f ? (__float_as_int(most) >> 23) : 127 + 14, size = min(254, max(1, 127 + 14 + 127 - ex));
+                const float up = __int_as_float(size << 23 | (g.scale_log2 < 0.f ? 1 << 31 : 0));      // (the factor of the scores is positive: their maximum is the products')
+                const int row = row0 + 4 * k, lr = row & 127;
+#pragma unroll
+                for (int p = 0; p < kPieces; ++p) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { const float2 v = x[k].pair(4 * p + e); w[e] = down2<TT_TYPE_F16>(v.x * up, v.y * up); }
+                    const int i = 8 * p + (lane & 7);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(q_s + (uint32_t)tile * S::kTile + (uint32_t)(i % S::kAtoms) * kAtom + (uint32_t)lr * 128u + ((uint32_t)((i / S::kAtoms) ^ (lr & 7)) << 4)),
+                                 "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
                 }
+                if ((lane & 7) == 0) sizes[row] = (uint8_t)size;
             }
-        }
+        };
+        if (g.a.type == TT_TYPE_F16) stage(std::integral_constant<int, TT_TYPE_F16>());
+        else stage(std::integral_constant<int, TT_TYPE_BF16>());
         fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&q_full));
@@ -360,7 +369,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     read_shared<16>(q_s + (uint32_t)row * (2u * D) + (((uint32_t)i ^ (uint32_t)(row & 7)) << 4), w);
                     if (row < view.rows && fine) {
                         uint16_t* y = static_cast<uint16_t*>(g.a.y) + at;
-                        if (g.y_wide) {
+                        if (g.y_wide == 2) *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+                        else if (g.y_wide) {
                             *reinterpret_cast<uint2*>(y) = make_uint2(w[0], w[1]);
                             *reinterpret_cast<uint2*>(y + 4) = make_uint2(w[2], w[3]);
                         } else {
