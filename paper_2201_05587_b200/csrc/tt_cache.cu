@@ -1,5 +1,6 @@
 // A paged cache of keys and values in e4m3, a scale for each page and head: new tokens into it, and attention over it.
 #include <cuda_runtime.h>
+#include <climits>
 #include <cstring>
 #include <type_traits>
 #include "tt_cache.cuh"
@@ -227,20 +228,28 @@ struct AttendShape {
 // The tokens of a split.  Only the device knows the lengths: the split that deals all sequences' tokens to the CTAs that the SMs hold at once, less a
 // fifth, as every sequence has a last split that is not full.  (8 sequences of up to 16384 tokens: 34 us so; by the longest that there may be 42.)  No
 // less than what the grid has room for.
+struct Lane { int start, next, length; };                    // of sequence `lane`
+__device__ __forceinline__ Lane lane_of(const Attend& g) {
+    const int b = threadIdx.x & 31;
+    if (g.splits == 1 || b >= g.a.cache.batch) return Lane{0, 0, 0};
+    return Lane{g.a.starts[b], g.a.starts[b + 1], g.a.lengths[b]};
+}
 template <int ROWS>
-__device__ __forceinline__ int split_tokens(const Attend& g) {
+__device__ __forceinline__ int split_tokens(const Attend& g, const Lane& mine) {
     constexpr int kGrain = kAttendWarps * kRun;
     const tt_cache& c = g.a.cache;
     if (g.splits == 1 || c.batch > 1024) return g.chunk;
     unsigned runs = 0u;                                      // of all sequences' tiles
-    for (int b = threadIdx.x & 31; b < c.batch; b += 32) {
-        const long long rows = (long long)(g.a.starts[b + 1] - g.a.starts[b]) * g.group;
-        const int length = min(max(g.a.lengths[b], 0), g.span);
-        if (rows >= g.least && rows <= g.most) runs += (unsigned)min((long long)(length + kRun - 1) / kRun * ((rows + ROWS - 1) / ROWS), 1ll << 20);
-    }
-    const long long all = __reduce_add_sync(0xffffffffu, min(runs, 1u << 26));
-    const long long share = (all * c.heads * kRun + g.share - 1) / g.share;
-    return max(g.chunk, (int)min((share + kGrain - 1) / kGrain * kGrain, (long long)g.span + kRun));
+    const auto add = [&](int start, int next, int length) {
+        const long long rows = (long long)(next - start) * g.group;
+        if (rows >= g.least && rows <= g.most) runs += (unsigned)min((long long)((unsigned)min(max(length, 0), g.span) + kRun - 1) / kRun * ((unsigned)(rows + ROWS - 1) / ROWS), 1ll << 20);
+    };
+    add(mine.start, mine.next, mine.length);
+    for (int b = (threadIdx.x & 31) + 32; b < c.batch; b += 32) add(g.a.starts[b], g.a.starts[b + 1], g.a.lengths[b]);
+    // (in 32-bit floating point: whatever it is rounded to, all CTAs have the same)
+    const float all = (float)__reduce_add_sync(0xffffffffu, min(runs, 1u << 26));
+    const float share = fminf(all * ((float)(c.heads * kRun) / (float)g.share), 1073741824.f);
+    return max(g.chunk, ((int)share + kGrain) / kGrain * kGrain);
 }
 
 template <int D, int NT>
@@ -249,6 +258,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t full_bar[kAttendWarps][S::kStages];
     __shared__ int last_one, abort_flag;
+    __shared__ long long y_at[S::kRows];
+    __shared__ int2 seen[S::kRows];
     volatile int* abortp = &abort_flag;
     if (threadIdx.x < kAttendWarps * S::kStages) mbar_init(smem_u32(&full_bar[0][0] + threadIdx.x), 1u);
     if (threadIdx.x == 0) {
@@ -263,13 +274,14 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     pdl_wait_prev();
     const tt_cache& c = g.a.cache;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, cq = lane & 3, head = blockIdx.y;
+    const Lane mine = lane_of(g);                            // (under way while the tile is looked up)
     TileView view;
     if (!view_tile(g, S::kRows, blockIdx.x, view)) return;
     const int b = view.b, start = view.start, rows = view.rows, t0 = view.t0, h0 = view.h0, before = view.before, lo = view.lo, hi = view.hi;
-    const int base = lo / kRun * kRun, chunk = split_tokens<S::kRows>(g);
-    const int active = hi > lo ? (hi - base + chunk - 1) / chunk : 1;
+    const int base = lo / kRun * kRun, chunk = split_tokens<S::kRows>(g, mine);
+    const int active = hi > lo ? (int)((unsigned)(hi - base + chunk - 1) / (unsigned)chunk) : 1;
     if ((int)blockIdx.z >= active) return;
-    const int from = base + (int)blockIdx.z * chunk, to = min(hi, from + chunk);
+    const int from = base + (int)blockIdx.z * chunk, to = hi - from > chunk ? from + chunk : hi;
 
     const uint32_t base_s = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base_s - smem_u32(smem_raw));
@@ -336,8 +348,17 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
 #pragma unroll
     for (int i = 0; i < S::kStages - 1; ++i) fetch(i, ring + (uint32_t)i * S::kStage, i);
 
-    // ---- queries: lane (g, c) has of rows g, g + 8, ... what it has of the keys ----
+    // ---- of each row: where its output is, and the tokens that it sees ----
     const auto q_row = [&](int r) { const int t = (h0 + r) / g.group; return make_int2(start + t0 + t, head * g.group + (h0 + r - t * g.group)); };
+    if ((int)threadIdx.x < S::kRows) {
+        const int2 at = q_row((int)threadIdx.x);
+        const int pos = before + (at.x - start);
+        y_at[threadIdx.x] = at.x * g.a.y_token + at.y * g.a.y_head;
+        seen[threadIdx.x] = make_int2(g.a.window > 0 ? pos - g.a.window + 1 : INT_MIN, g.a.causal ? min(to, pos + 1) : to);
+    }
+    __syncthreads();
+
+    // ---- queries: lane (g, c) has of rows g, g + 8, ... what it has of the keys ----
     uint32_t q[S::kQueryRegs ? NT : 1][D / 16][2];
     float factor[NT][2];                                     // of the rows 2c, 2c + 1: what turns a product into a score in powers of two
 #pragma unroll
@@ -414,10 +435,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 2; ++e) { top[n][e] = -INFINITY; sum[n][e] = 0.f; }
-    const auto sees = [&](int r, int tok) {
-        const int pos = before + t0 + (h0 + r) / g.group;
-        return tok < to && (!g.a.causal || tok <= pos) && (g.a.window <= 0 || tok > pos - g.a.window);
-    };
+    const auto sees = [&](int r, int tok) { const int2 s = seen[r]; return tok >= s.x && tok < s.y; };
 
     // what a lane reads of a step's boxes
     const int row0 = S::key_of(gq), rows_v[2] = {S::key_of(2 * cq), S::key_of(2 * cq + 1)};
@@ -621,10 +639,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             if (gq == 0) *reinterpret_cast<float2*>(line + D) = make_float2(top[n][e], total);
         }
     __syncthreads();
-    const auto store = [&](int r, int i, const float (&v)[4]) {
-        const int2 at_ = q_row(r);
-        store_four(g.a.y, at_.x * g.a.y_token + at_.y * g.a.y_head + i, g.a.type, g.y_wide, v);
-    };
+    const auto store = [&](int r, int i, const float (&v)[4]) { store_four(g.a.y, y_at[r] + i, g.a.type, g.y_wide, v); };
     const long long tile = (long long)blockIdx.x * c.heads + head;
     constexpr int kPart = S::kRows * (D + 2);
     float* left = g.partial + (tile * g.splits + blockIdx.z) * kPart;
@@ -693,17 +708,10 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         }
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < rows * (D / 4); e += kAttendWarps * 32) {
-        const int r = e / (D / 4), i = 4 * (e - r * (D / 4));
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 16
-        for (int z = 0; z < active; ++z) {
-            const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + r * D + i));
-            const float w = lists[z * S::kRows + r].x;
-            v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
-        }
-        store(r, i, v);
-    }
+    join_splits<kAttendWarps * 32>(rows * (D / 4), active,
+        [&](int e, int z) { return reinterpret_cast<const float4*>(parts + (long long)z * kPart + 4 * e); },
+        [&](int e, int z) { return lists[z * S::kRows + e / (D / 4)].x; },
+        [&](int e, const float (&v)[4]) { store(e / (D / 4), 4 * (e % (D / 4)), v); });
     if (threadIdx.x == 0) g.counters[tile] = 0u;             // ready for the next call
 }
 

@@ -2,6 +2,7 @@
 #pragma once
 #include "tt_ptx.cuh"
 #include "tt_f8.cuh"
+#include <type_traits>
 
 namespace tt {
 
@@ -34,6 +35,43 @@ __device__ __forceinline__ bool sequence_of(const int* starts, int batch, const 
     }
     first = begin(b);
     return first <= unit;
+}
+
+// The splits of a tile together: element e of the tile's `elements` vectors of four is the sum over splits of part(e, z) * share(e, z).  A thread has
+// 16 of them under way at a time, none behind another.
+template <int THREADS, class PART, class SHARE, class STORE>
+__device__ __forceinline__ void join_splits(int elements, int splits, const PART& part, const SHARE& share, const STORE& store) {
+    const auto go = [&](auto at_once) {
+        constexpr int E = decltype(at_once)::value, Z = 16 / E;
+        for (int e0 = threadIdx.x; e0 < elements; e0 += E * THREADS) {
+            float v[E][4];
+#pragma unroll
+            for (int k = 0; k < E; ++k) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0.f;
+            for (int z0 = 0; z0 < splits; z0 += Z) {
+                float4 f[E][Z];
+#pragma unroll
+                for (int k = 0; k < E; ++k)
+#pragma unroll
+                    for (int z = 0; z < Z; ++z) {
+                        f[k][z] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (e0 + k * THREADS < elements && z0 + z < splits) f[k][z] = __ldcg(part(e0 + k * THREADS, z0 + z));
+                    }
+#pragma unroll
+                for (int k = 0; k < E; ++k)
+#pragma unroll
+                    for (int z = 0; z < Z; ++z)
+                        if (e0 + k * THREADS < elements && z0 + z < splits) {
+                            const float w = share(e0 + k * THREADS, z0 + z);
+                            v[k][0] = fmaf(f[k][z].x, w, v[k][0]); v[k][1] = fmaf(f[k][z].y, w, v[k][1]);
+                            v[k][2] = fmaf(f[k][z].z, w, v[k][2]); v[k][3] = fmaf(f[k][z].w, w, v[k][3]);
+                        }
+            }
+#pragma unroll
+            for (int k = 0; k < E; ++k) if (e0 + k * THREADS < elements) store(e0 + k * THREADS, v[k]);
+        }
+    };
+    if (splits <= 4) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
 }
 
 constexpr int kStep = 16;                   // tokens of a step: pages are multiples of it

@@ -106,10 +106,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most)
     if (!view_tile(g, kPromptRows, unit, view)) return;
     const int base_token = view.lo / kPromptTokens * kPromptTokens;
-    const int active = view.hi > view.lo ? (view.hi - base_token + g.chunk - 1) / g.chunk : 1;
+    const int active = view.hi > view.lo ? (int)((unsigned)(view.hi - base_token + g.chunk - 1) / (unsigned)g.chunk) : 1;
     if ((int)blockIdx.z >= active) return;
-    const int from = base_token + (int)blockIdx.z * g.chunk, to = min(view.hi, from + g.chunk);
-    const int steps = to > from ? (to - from + kPromptTokens - 1) / kPromptTokens : 0;
+    const int from = base_token + (int)blockIdx.z * g.chunk, to = view.hi - from > g.chunk ? from + g.chunk : view.hi;
+    const int steps = to > from ? (to - from - 1) / kPromptTokens + 1 : 0;
     const int tiles = view.rows > 128 ? 2 : 1;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -416,17 +416,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             for (int z = 0; z < active; ++z) share[z * kPromptRows + r] *= inv;
         }
         named_sync(3, kSoftmax);
-        for (int e = threadIdx.x; e < view.rows * (D / 4); e += kSoftmax) {
-            const int rr = e / (D / 4), i = 4 * (e - rr * (D / 4));
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-            for (int z = 0; z < active; ++z) {
-                const float4 f = __ldcg(reinterpret_cast<const float4*>(parts + (long long)z * kPart + (i >> 3) * (8 * kPromptRows) + 8 * rr + (i & 4)));
-                const float w = share[z * kPromptRows + rr];
-                v[0] = fmaf(f.x, w, v[0]); v[1] = fmaf(f.y, w, v[1]); v[2] = fmaf(f.z, w, v[2]); v[3] = fmaf(f.w, w, v[3]);
-            }
-            store(rr, i, v);
-        }
+        join_splits<kSoftmax>(view.rows * (D / 4), active,
+            [&](int e, int z) { const int rr = e / (D / 4), i = 4 * (e % (D / 4)); return reinterpret_cast<const float4*>(parts + (long long)z * kPart + (i >> 3) * (8 * kPromptRows) + 8 * rr + (i & 4)); },
+            [&](int e, int z) { return share[z * kPromptRows + e / (D / 4)]; },
+            [&](int e, const float (&v)[4]) { store(e / (D / 4), 4 * (e % (D / 4)), v); });
         if (threadIdx.x == 0) g.counters[place] = 0u;                    // ready for the next call
     } else if (warp < 20) {
         registers_down<56>();
