@@ -227,18 +227,20 @@ struct AttendShape {
 
 // The tokens of a split.  Only the device knows the lengths: the split that deals all sequences' tokens to the CTAs that the SMs hold at once, less a
 // fifth, as every sequence has a last split that is not full.  (8 sequences of up to 16384 tokens: 34 us so; by the longest that there may be 42.)  No
-// less than what the grid has room for.
+// less than what the grid has room for, nor than what makes the join, which reads 14 bytes a cycle, as long as a split, whose warps take some
+// 8 + 6 NT cycles a token.  (One sequence of 14353 tokens, 8 rows of 128: 19 splits 16.3 us, 57 of them 19.0.)
 struct Lane { int start, next, length; };                    // of sequence `lane`
 __device__ __forceinline__ Lane lane_of(const Attend& g) {
     const int b = threadIdx.x & 31;
     if (g.splits == 1 || b >= g.a.cache.batch) return Lane{0, 0, 0};
     return Lane{g.a.starts[b], g.a.starts[b + 1], g.a.lengths[b]};
 }
+// `tokens` that the tile sees, `bytes` of a split's part
 template <int ROWS>
-__device__ __forceinline__ int split_tokens(const Attend& g, const Lane& mine) {
+__device__ __forceinline__ int split_tokens(const Attend& g, const Lane& mine, float tokens, float bytes) {
     constexpr int kGrain = kAttendWarps * kRun;
     const tt_cache& c = g.a.cache;
-    if (g.splits == 1 || c.batch > 1024) return g.chunk;
+    if (g.splits == 1 || c.batch > 1024) return g.chunk;       // (so many have no need of splits)
     unsigned runs = 0u;                                      // of all sequences' tiles
     const auto add = [&](int start, int next, int length) {
         const long long rows = (long long)(next - start) * g.group;
@@ -248,7 +250,8 @@ __device__ __forceinline__ int split_tokens(const Attend& g, const Lane& mine) {
     for (int b = (threadIdx.x & 31) + 32; b < c.batch; b += 32) add(g.a.starts[b], g.a.starts[b + 1], g.a.lengths[b]);
     // (in 32-bit floating point: whatever it is rounded to, all CTAs have the same)
     const float all = (float)__reduce_add_sync(0xffffffffu, min(runs, 1u << 26));
-    const float share = fminf(all * ((float)(c.heads * kRun) / (float)g.share), 1073741824.f);
+    const float join = sqrtf(tokens * bytes * (1.f / (14.f * (8.f + 0.75f * ROWS))));
+    const float share = fminf(fmaxf(join, all * ((float)(c.heads * kRun) / (float)g.share)), 1073741824.f);
     return max(g.chunk, ((int)share + kGrain) / kGrain * kGrain);
 }
 
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     TileView view;
     if (!view_tile(g, S::kRows, blockIdx.x, view)) return;
     const int b = view.b, start = view.start, rows = view.rows, t0 = view.t0, h0 = view.h0, before = view.before, lo = view.lo, hi = view.hi;
-    const int base = lo / kRun * kRun, chunk = split_tokens<S::kRows>(g, mine);
+    const int base = lo / kRun * kRun, chunk = split_tokens<S::kRows>(g, mine, (float)(hi - lo), 4.f * rows * D);
     const int active = hi > lo ? (int)((unsigned)(hi - base + chunk - 1) / (unsigned)chunk) : 1;
     if ((int)blockIdx.z >= active) return;
     const int from = base + (int)blockIdx.z * chunk, to = hi - from > chunk ? from + chunk : hi;
@@ -684,9 +687,17 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     __threadfence();
     const float* parts = g.partial + tile * g.splits * kPart;
     float2* lists = reinterpret_cast<float2*>(join);         // [split][row]: maximum and sum, then the split's share
-    for (int e = threadIdx.x; e < active * rows; e += kAttendWarps * 32) {
-        const int z = e / rows, r = e - z * rows;
-        lists[z * S::kRows + r] = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + S::kRows * D + 2 * r));
+    constexpr int kThreads = kAttendWarps * 32;
+    for (int e0 = threadIdx.x; e0 < active * S::kRows; e0 += 8 * kThreads) {
+        float2 ml[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int e = e0 + k * kThreads, z = e / S::kRows, r = e % S::kRows;
+            ml[k] = make_float2(0.f, 0.f);
+            if (z < active && r < rows) ml[k] = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + S::kRows * D + 2 * r));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (e0 + k * kThreads < active * S::kRows) lists[e0 + k * kThreads] = ml[k];
     }
     __syncthreads();
     for (int r = warp; r < rows; r += kAttendWarps) {
@@ -792,7 +803,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         constexpr int kGrain = kAttendWarps * kRun;
         f.span = (int)(span - kRun);
         f.share = (int)(c.batch > 1 ? slots * 4 / 5 : slots);
-        long long splits = c.batch > 1 ? 4 * slots / tiles : slots / tiles;
+        long long splits = 4 * slots / tiles;
         if (splits > kMostSplits) splits = kMostSplits;
         if (splits < 1) splits = 1;
         long long chunk = (span + splits - 1) / splits;
