@@ -645,17 +645,42 @@ tt_dense_f8_pair_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid
                     }
                 } else {
                     __syncwarp();
-                    for (int r = 0; r < 32 && row0 + r < g.rows_a; ++r) {
-                        const long long at = (long long)(row0 + r) * g.y_row + col;
-                        if (g.y_type == TT_TYPE_F32) {
-                            if (col + lane < g.rows_b) static_cast<float*>(g.y)[at + lane] = ld_shared_f32(staging + (uint32_t)r * 128u + ((uint32_t)((lane >> 2) ^ (r & 7)) << 4) + 4u * (uint32_t)(lane & 3));
-                        } else {
+                    if (g.y_type == TT_TYPE_F32) {
+                        float* y = static_cast<float*>(g.y) + (long long)row0 * g.y_row + col + lane;
+#pragma unroll 1
+                        for (int r = 0; r < 32; r += 8, y += 8 * g.y_row) {
+                            float v[8];
 #pragma unroll
-                            for (int j = 0; j < kCols; j += 32) {
-                                const uint32_t e = (uint32_t)(lane + j), x = kCols == 64 ? (uint32_t)(r & 7) : (uint32_t)((r >> 1) & 3);
-                                uint16_t v;
-                                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(staging + (uint32_t)r * (kCols * 2u) + (((e >> 3) ^ x) << 4) + 2u * (e & 7u)) : "memory");
-                                if (col + (int)e < g.rows_b) static_cast<uint16_t*>(g.y)[at + e] = v;
+                            for (int k = 0; k < 8; ++k) v[k] = ld_shared_f32(staging + (uint32_t)(r + k) * 128u + ((uint32_t)((lane >> 2) ^ k) << 4) + 4u * (uint32_t)(lane & 3));
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) if (row0 + r + k < g.rows_a && col + lane < g.rows_b) y[k * g.y_row] = v[k];
+                        }
+                    } else {
+                        // A lane has two values, a word of memory, or the second and the next lane's first where rows begin between two words.
+                        constexpr int kWords = kCols / 2, kRows = 32 / kWords;
+                        const int l = lane % kWords, sub = lane / kWords, n = g.rows_b - col;
+                        uint16_t* y = static_cast<uint16_t*>(g.y) + (long long)(row0 + sub) * g.y_row + col + 2 * l;
+#pragma unroll 1
+                        for (int r = sub; r < 32; r += 8 * kRows, y += 8 * kRows * g.y_row) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const int at = r + k * kRows, x = kCols == 64 ? at & 7 : (at >> 1) & 3;
+                                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[k]) : "r"(staging + (uint32_t)at * (kCols * 2u) + ((uint32_t)((l >> 2) ^ x) << 4) + 4u * (uint32_t)(l & 3)) : "memory");
+                            }
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                uint16_t* p = y + k * kRows * g.y_row;
+                                const uint32_t next = __shfl_down_sync(0xffffffffu, w[k], 1, kWords);
+                                if (row0 + r + k * kRows >= g.rows_a) continue;
+                                if ((reinterpret_cast<uintptr_t>(p) & 2u) == 0u) {
+                                    if (2 * l + 1 < n) *reinterpret_cast<uint32_t*>(p) = w[k];
+                                    else if (2 * l < n) *p = (uint16_t)w[k];
+                                } else {
+                                    if (l < kWords - 1 && 2 * l + 2 < n) *reinterpret_cast<uint32_t*>(p + 1) = __funnelshift_r(w[k], next, 16);
+                                    else if (2 * l + 1 < n) p[1] = (uint16_t)(w[k] >> 16);
+                                    if (l == 0 && n > 0) *p = (uint16_t)w[k];
+                                }
                             }
                         }
                     }
