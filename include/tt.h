@@ -475,7 +475,7 @@ tt_status tt_dense_static_scratch(const void* x, const void* w, const void* bias
  * What a program calls that keeps weights, keys and values in e4m3 (one sign, four exponent and three mantissa bits, largest value
  * 448, no infinities): the dense layer, the quantisation in front of it, rotary positions, and a paged cache with its attention.
  * Each call takes its arguments in a structure of plain pointers, sizes and strides (in elements, unless stated otherwise; the
- * innermost axis of every tensor is contiguous), checks them, enqueues one kernel on `cuda_stream` of the current device and returns.
+ * innermost axis of every tensor is contiguous), checks them, enqueues a kernel (attention two at most) on `cuda_stream` of the current device and returns.
  * Nothing is kept between calls and no device memory is allocated, so calls may be captured, and calls that share no output, status word
  * or workspace may run at the same time.  Null pointers, unknown types, sizes that are negative or too large and strides or addresses that a call
  * cannot take are TT_ERR_INVALID_ARG; what an e4m3 kernel is not built for (a head size, a page size) is TT_ERR_NOT_IMPLEMENTED.

@@ -740,6 +740,7 @@ static tt_status check_cache_memory(const tt_cache& c) {
     for (int w = 0; w < 2; ++w) {
         if (!c.data[w] || !c.scale[w] || reinterpret_cast<uintptr_t>(c.scale[w]) % 4 || !on16(c.data[w])) return TT_ERR_INVALID_ARG;
         if (c.page[w] < 0 || c.head[w] < 0 || c.token[w] < 0 || c.page[w] % 16 || c.head[w] % 16 || c.token[w] % 16 || c.s_page[w] < 0 || c.s_head[w] < 0) return TT_ERR_INVALID_ARG;
+        if (c.page[w] >= 1ll << 40 || c.head[w] >= 1ll << 40 || c.token[w] >= 1ll << 40) return TT_ERR_INVALID_ARG;      // (a tensor map takes no more)
     }
     return TT_OK;
 }

@@ -772,8 +772,11 @@ static cudaError_t launch_dense_f8_pair(const CUtensorMap& ta, const CUtensorMap
 
 using namespace tt;
 
+constexpr int kMostRows = 0x7fffff00;                       // of an axis: tiles reach behind its end
+constexpr int64_t kMostPitch = 1ll << 40;                   // bytes from row to row that a tensor map takes
+
 extern "C" tt_status tt_quantize(const tt_quantize_args* a, void* stream) {
-    if (!a || !known_type(a->x_type) || a->m < 0 || a->kk < 0 || (a->block_rows != 1 && a->block_rows != kF8Block)) return TT_ERR_INVALID_ARG;
+    if (!a || !known_type(a->x_type) || a->m < 0 || a->kk < 0 || a->m > kMostRows || a->kk > kMostRows || (a->block_rows != 1 && a->block_rows != kF8Block)) return TT_ERR_INVALID_ARG;
     if (a->m == 0 || a->kk == 0) return TT_OK;
     const int64_t bytes = type_bytes(a->x_type);
     if (!a->x || !a->q || !a->scales || a->x_row < a->kk || a->q_row < a->kk || a->s_row < 0 || a->s_block < 0) return TT_ERR_INVALID_ARG;
@@ -794,13 +797,13 @@ extern "C" tt_status tt_quantize(const tt_quantize_args* a, void* stream) {
 }
 
 extern "C" tt_status tt_dense_quantized(const tt_dense_quantized_args* a, void* stream) {
-    if (!a || !known_type(a->y_type) || a->m < 0 || a->nn < 0 || a->kk < 0 || a->act < TT_ACT_NONE || a->act > TT_ACT_GELU_ERF) return TT_ERR_INVALID_ARG;
+    if (!a || !known_type(a->y_type) || a->m < 0 || a->nn < 0 || a->kk < 0 || a->m > kMostRows || a->nn > kMostRows || a->kk > kMostRows || a->act < TT_ACT_NONE || a->act > TT_ACT_GELU_ERF) return TT_ERR_INVALID_ARG;
     if (a->m == 0 || a->nn == 0) return TT_OK;
     if (a->kk == 0) return TT_ERR_INVALID_ARG;             // (there is no sum to take)
     if (!a->x || !a->w || !a->x_scale || !a->w_scale || !a->y || !a->status) return TT_ERR_INVALID_ARG;
     if (a->x_row < a->kk || a->w_row < a->kk || a->y_row < a->nn || a->xs_row < 0 || a->xs_block < 0 || a->ws_row < 0 || a->ws_block < 0) return TT_ERR_INVALID_ARG;
-    if (!on16(a->x) || !on16(a->w) || a->x_row % 16 || a->w_row % 16) return TT_ERR_INVALID_ARG;
     const int64_t bytes = type_bytes(a->y_type);
+    if (!on16(a->x) || !on16(a->w) || a->x_row % 16 || a->w_row % 16 || a->x_row >= kMostPitch || a->w_row >= kMostPitch || a->y_row >= kMostPitch / bytes) return TT_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(a->y) % (uintptr_t)bytes || reinterpret_cast<uintptr_t>(a->x_scale) % 4 || reinterpret_cast<uintptr_t>(a->w_scale) % 4 ||
         reinterpret_cast<uintptr_t>(a->bias) % 4 || reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
     DenseF8 g{};

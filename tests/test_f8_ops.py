@@ -155,6 +155,16 @@ def test_refusals(fn, make, cases, want):
         assert call(C.byref(make(**kw)), None) == want, kw
 
 
+def test_sizes_and_strides_beyond_what_the_kernels_count():
+    most, far = (1 << 31) - 1, 1 << 40
+    for fn, make, cases in (("tt_quantize", quantize_args, [dict(m=most), dict(kk=most, x_row=most, q_row=most), dict(m=most, block_rows=128)]),
+                            ("tt_dense_quantized", dense_args, [dict(m=most), dict(nn=most, y_row=most), dict(kk=most, x_row=1 << 31, w_row=1 << 31), dict(x_row=far), dict(w_row=far), dict(y_row=far)]),
+                            ("tt_cache_append", lambda **kw: append_args(cache_struct(**kw)), [dict(page=(far, 16384)), dict(head=(8192, far)), dict(token=(far, 128))]),
+                            ("tt_cache_attention", lambda **kw: attention_args(cache_struct(**kw)), [dict(page=(16384, far)), dict(head=(far, 8192)), dict(token=(128, far))])):
+        for kw in cases:
+            assert getattr(B.lib(), fn)(C.byref(make(**kw)), None) == BAD, (fn, kw)
+
+
 def test_a_split_attention_needs_its_workspace():
     long = cache_struct(max_pages=2048, table_row=2048)
     n = C.c_int64()
