@@ -13,7 +13,8 @@ namespace tt {
 // (what is more than kHeld pieces a thread is read again, from the caches), their maximum, their conversion; where the page holds
 // tokens already and the scale has to rise, those are brought to it.
 //   Bytes are the bound, but a page is only some thousands of values, so what each thread does once counts as much: addresses are stepped, not
-// divided for.
+// divided for.  (Four prompts of up to 2048 tokens, 8 heads of 128, pages of 64: 8.8 us, 3.3 TB/s; with divisions, 64-bit ones for the sequences, and 256
+// threads 13.3.  64 single tokens 3.4 us.)
 constexpr int kAppendThreads = 128;         // of a CTA that has a page
 template <int TYPE, bool WIDE, bool WARP>
 __global__ void __launch_bounds__(WARP ? 256 : kAppendThreads, WARP ? 3 : 7) tt_cache_append_kernel(const tt_cache_append_args a) {
@@ -161,6 +162,7 @@ __global__ void __launch_bounds__(WARP ? 256 : kAppendThreads, WARP ? 3 : 7) tt_
 // scores' factor takes back.  Probabilities are rounded to 11 bits, times 2^15 and the page's scale over the largest so far, so that what is
 // 2^-29 of the largest still has all of them; sums are in 32 bits.
 //   The keys of a sequence are split over CTAs, of which the last to finish adds up what all have left in the workspace, in their order.
+//   (64 sequences of up to 8192 tokens, 32 heads over 8 of 128: 117 us, 5.3 TB/s, 0.81 of a copy's rate; one of 131072 tokens: 54 us, 0.76.)
 
 constexpr int kRun = 64;                    // tokens that a warp takes in a row
 constexpr int kAttendWarps = 4;

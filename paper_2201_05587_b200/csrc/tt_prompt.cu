@@ -9,6 +9,11 @@
 // would be, which 16 bits have room for (it is brought to 2^15 at most, and what is 2^-18 of the largest has all of its bits), and the row's sum has
 // the same factor.  A page's scale of values is in
 // P too, as the part of the exponent, over the largest scale so far.
+//   Two prompts of 2048 tokens behind as many, 32 heads over 8 of 128: 250 us, 825 TFLOP/s of 16-bit products, half of the tensor cores' rate.  A step
+// of 128 keys takes 3500 to 3900 cycles: the products 2050, the exponentials 2050 and the shared memory 2560, and a tile's chain (its softmax, then the
+// product that takes P and the one that makes the next scores) 3500, which is the bound.  The way in and out are 11000 and 6000 cycles of a CTA.
+// (Scores of the second 64 keys while P of the first is being made: 370 us, as the queries are read twice.  A part of the exponentials as polynomials:
+// slower, they are not the bound.)
 //   NaN in values that only some rows of the tile see (the steps at the edge of what is visible) are taken out of the product and put into
 // the outputs of the rows that do: a column's first such token (at the upper edge; its last one at the lower) decides.
 #include <cuda_runtime.h>
@@ -103,7 +108,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     volatile int* abortp = &abort_flag;
     pdl_wait_prev();
     TileView view;
-    const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most)
+    const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most; all heads' last ones first: 253 us for 249)
     if (!view_tile(g, kPromptRows, unit, view)) return;
     const int base_token = view.lo / kPromptTokens * kPromptTokens;
     const int active = view.hi > view.lo ? (int)((unsigned)(view.hi - base_token + g.chunk - 1) / (unsigned)g.chunk) : 1;
@@ -149,8 +154,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     if (warp < 16) {
         registers_up<96>();
         // ---------------- queries: a row as 16-bit floating point with a maximum of 2^14..2^15 ----------------
-        // Eight lanes have a row, a warp 16 rows of its tile: what it loads lies side by side.  (A thread a row, 32 lines at a time, took 20000
-        // cycles, a third of a tile of 1024 tokens; the same by four values a lane took 9500, in instructions.)
+        // Eight lanes have a row, a warp 16 rows of its tile: what it loads lies side by side.  (The two prompts above: a thread a
+        // row, in queries and outputs, 317 us; four values a lane 257; so 250.)
         const auto stage = [&](auto type) {
             constexpr int TYPE = decltype(type)::value, kPieces = D / 64;
             const int row0 = tile * 128 + (warp & 7) * 16 + (lane >> 3);
