@@ -210,7 +210,7 @@ struct AttendShape {
     static constexpr uint32_t kBox = kTokens * kLine, kStage = 2u * kTokens * D;
     static constexpr uint32_t kQuery = kQueryRegs ? 0u : NT * (D / 16) * 256u;
     static constexpr int kCtas = attend_ctas(D, NT);
-    static constexpr int kFits = (int)((227u * 1024u / kCtas - 3072u - kQuery) / (kAttendWarps * kStage));
+    static constexpr int kFits = (int)((227u * 1024u / kCtas - 3u * 1024u - kQuery) / (kAttendWarps * kStage));
     static constexpr int kStages = kFits > 6 ? 6 : kFits;                            // steps in shared memory: one is worked on, the others are under way
     static constexpr uint32_t kRing = kAttendWarps * kStages * kStage;
     static constexpr uint32_t kJoin = kAttendWarps * kRows * (D + 4) * 4u;           // the warps' results (over the ring)
