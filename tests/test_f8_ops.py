@@ -773,6 +773,45 @@ def test_attention_by_token_layout_strided_queries_and_shared_pages():
 
 
 @gpu
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("offset", [0, 1, 4])                    # of 16 bytes, of 2, of 8
+@pytest.mark.parametrize("heads,heads_q", [(2, 2), (1, 3), (2, 16)])
+@pytest.mark.parametrize("counts,lengths", [([90, 150], [300, 150]), ([40], [5000])])
+def test_attention_of_prompts_at_any_alignment(d, offset, heads, heads_q, counts, lengths):
+    p, tokens = Pages(lengths, heads, d, 16, seed=d + offset), sum(counts)
+    wide = (torch.randn(tokens, heads_q, d + 8, generator=gen(5), device="cuda") * 2).to(torch.float16)
+    into = torch.full((tokens + 1, heads_q, d + 8), -77.0, dtype=torch.float16, device="cuda")
+    q, y = wide[..., offset:offset + d], into[:tokens, :, offset:offset + d]
+    call = B.cache_attention(p.cache(), q, y, int32([0] + list(np.cumsum(counts))), int32(lengths), 1 / math.sqrt(d))
+    call.run()
+    assert call.status() == B.TT_OK
+    ref, off = reference_attention(p, counts, q, 1 / math.sqrt(d), True, 0)
+    got = y.double().cpu().numpy()
+    assert (np.abs(got - ref) <= off + HALF_STEP[torch.float16] * (np.abs(ref) + off) + 2.0 ** -25).all()
+    y.fill_(-77.0)
+    assert (into == -77.0).all()
+
+
+@gpu
+@pytest.mark.parametrize("n", [1348, 1349, 1351])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_dense_rows_that_begin_anywhere(n, kind):
+    m, k = 3001, 200                                            # (pairs of CTAs: 3001 x 1348 tiles of 256)
+    (x, xs, w, ws), bias = dense_case(m, n, k, seed=n), torch.randn(n, generator=gen(9), device="cuda")
+    ref, most = dense_reference(x, xs, w, ws, bias)
+    off = most * ADD * (k + 32)
+    into = torch.full((m + 1, n + 5), -77.0, dtype=TYPES[kind], device="cuda")
+    for first in (0, 1, 3):
+        y = into[:m, first:first + n]
+        call = B.dense_quantized(x, xs, w, ws, y, bias=bias)
+        call.run()
+        assert call.status() == B.TT_OK
+        assert (np.abs(y.double().cpu().numpy() - ref) <= off + HALF_STEP[TYPES[kind]] * (np.abs(ref) + off) + 2.0 ** -25).all()
+        y.fill_(-77.0)
+        assert (into == -77.0).all()
+
+
+@gpu
 def test_attention_scales_that_differ_by_much():
     p = Pages([256], 1, 64, 16, seed=6)
     e = torch.linspace(-30, 8, p.ks.numel(), device="cuda").round().view_as(p.ks)
