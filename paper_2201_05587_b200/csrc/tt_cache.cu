@@ -753,9 +753,10 @@ struct AttendPlan {
     long long few_units = 0, prompt_units = 0;              // 0: the kernel is not needed
     long long bytes = 0, prompt_at = 0;                     // of the workspace; where the second one's part begins
 };
-static long long workspace_part(const Attend& g, long long units) {
+// d: of a head, as the kernel is built for it
+static long long workspace_part(const Attend& g, long long units, int d) {
     const long long tiles = units * g.a.cache.heads;
-    return g.splits > 1 ? (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (g.a.cache.d + 2) * 4 : 0;
+    return g.splits > 1 ? (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (d + 2) * 4 : 0;
 }
 static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan) {
     const tt_cache& c = a.cache;
@@ -815,7 +816,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         f.chunk = (int)chunk;
         f.splits = (int)((span + chunk - 1) / chunk);
         if (f.splits < 1) f.splits = 1;
-        plan.bytes = workspace_part(f, plan.few_units);
+        plan.bytes = workspace_part(f, plan.few_units, c.d);
     }
     if (prompts) {
         Attend& p = plan.prompt;
@@ -837,7 +838,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         p.chunk = (int)(chunk < span ? chunk : (span + kPromptTokens - 1) / kPromptTokens * kPromptTokens);
         p.splits = (int)((span + p.chunk - 1) / p.chunk);
         plan.prompt_at = plan.bytes = (plan.bytes + 15) / 16 * 16;
-        plan.bytes += workspace_part(p, plan.prompt_units);
+        plan.bytes += workspace_part(p, plan.prompt_units, prompt_head(c.d));
     }
     return TT_OK;
 }
@@ -858,8 +859,8 @@ static cudaError_t launch_attend(const Attend& g, long long units, void* stream)
         const tt_cache& c = g.a.cache;
         const int box = c.block >= S::kTokens ? S::kTokens : kStep;
         // (without pages nothing is read: the map is of any memory)
-        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], S::kLine, box)
-                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, S::kLine, box);
+        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], S::kLine, true, box)
+                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, S::kLine, true, box);
         if (st != TT_OK) return cudaErrorInvalidValue;
     }
     return launch(tt_attend_few_kernel<D, NT>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kAttendWarps * 32, S::kBytes, 1, stream, maps[0], maps[1], g);

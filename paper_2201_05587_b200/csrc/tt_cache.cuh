@@ -91,7 +91,8 @@ struct Attend {
 constexpr int kPromptRows = 256;            // rows of a tile of tt_attend_prompt_kernel
 constexpr int kPromptSplits = 32;           // its most splits of a sequence
 constexpr int kPromptTokens = 128;          // tokens of a step of it
-bool prompt_built_for(int d);
+constexpr int prompt_head(int d) { return d <= 64 ? 64 : 128; }      // what tt_attend_prompt_kernel is built for that holds a head of d
+constexpr bool prompt_built_for(int d) { return d <= 128; }
 cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream);
 
 // What a tile of rows has to do with the tokens of its sequence: false if there is nothing (or an error, which is reported).

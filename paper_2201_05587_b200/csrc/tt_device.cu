@@ -199,17 +199,17 @@ private:
 }  // namespace
 
 // A paged cache's bytes [pages][heads][tokens][d], strides in bytes -> 4-D tensor map, box = [line, box_tokens] of one page and head, lines swizzled
-// (line 0: whole tokens, as they lie).
-tt_status encode_pages(void* out, const void* base, int d, int tokens, int heads, int pages, long long token, long long head, long long page, int line, int box_tokens) {
+// or as they lie (what a line has more than d bytes is zeros).
+tt_status encode_pages(void* out, const void* base, int d, int tokens, int heads, int pages, long long token, long long head, long long page, int line, bool swizzle, int box_tokens) {
     EncodeTiledFn fn = encode_fn();
     if (!fn) return TT_ERR_CUDA;
     cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)tokens, (cuuint64_t)heads, (cuuint64_t)pages};
     // (the stride of an axis of one is not used, whatever it is)
     cuuint64_t strides[3] = {(cuuint64_t)token, (cuuint64_t)(heads > 1 ? head : token), (cuuint64_t)(pages > 1 ? page : token)};
-    cuuint32_t box[4] = {(cuuint32_t)(line ? line : d), (cuuint32_t)box_tokens, 1, 1};
+    cuuint32_t box[4] = {(cuuint32_t)line, (cuuint32_t)box_tokens, 1, 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
     CUresult r = fn(reinterpret_cast<CUtensorMap*>(out), CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, line == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : line == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : line == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, !swizzle ? CU_TENSOR_MAP_SWIZZLE_NONE : line == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : line == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : line == 32 ? CU_TENSOR_MAP_SWIZZLE_32B : CU_TENSOR_MAP_SWIZZLE_NONE,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? TT_OK : TT_ERR_CUDA;
 }

@@ -273,6 +273,6 @@ tt_status bind_device(tt_workload* w);                          // workspace + s
 tt_status launch(tt_workload* w, const tt_tensors* t, void* stream);
 void release_device(tt_workload* w);
 tt_status encode_bytes(void* out, const void* base, long long cols, long long rows, long long pitch, int box_rows);   // of 8-bit operands
-tt_status encode_pages(void* out, const void* base, int d, int tokens, int heads, int pages, long long token, long long head, long long page, int line, int box_tokens);
+tt_status encode_pages(void* out, const void* base, int d, int tokens, int heads, int pages, long long token, long long head, long long page, int line, bool swizzle, int box_tokens);
 tt_status encode_output(void* out, void* base, int bytes, long long cols, long long rows, long long pitch, int box_cols);
 }  // namespace tt

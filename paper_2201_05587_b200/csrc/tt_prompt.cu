@@ -1,12 +1,14 @@
 // Attention of prompts over the paged e4m3 cache: many rows (queries of the heads that share a key head) for each key, so the products and the
 // exponentials are the bound, not the cache's bytes.
 //
+// Built for heads of 64 and 128 values; what a shorter head lacks (32, 96) is zeros, which the copies and the queries' warps fill in.
 // A CTA has two tiles of 128 rows and walks the keys 128 at a time.  Four warps bring keys and values from the pages, turn them into 16-bit floating
 // point (exactly) and leave them as operand tiles, which serve both tiles of rows.  S = Q K^T goes to tensor memory; two threads of the
 // softmax warps have a row of it, take its maximum, and leave P = 2^(s - m) in S's place as the first operand of O += P V, whose sums stay
 // in tensor memory.  While one tile's softmax runs, the tensor core is at the other tile's products.
-//   O is multiplied only when a maximum has grown by more than 2^11 since it was last: P may be up to 2^11 times what it
-// would be, which 16 bits have room for (it is brought to 2^15 at most, and what is 2^-18 of the largest has all of its bits), and the row's sum has
+//   O is multiplied only when a maximum has grown by more than 2^8 since it was last: P may be up to 2^8 times what it
+// would be, which 16 bits have room for (it is brought to 2^15 at most, and what is 2^-21 of the largest has all of its bits; with 2^11 and 2^-18
+// a column of small values beside one key of nearly all the weight was off by more than a rounding), and the row's sum has
 // the same factor.  A page's scale of values is in
 // P too, as the part of the exponent, over the largest scale so far.
 //   Two prompts of 2048 tokens behind as many, 32 heads over 8 of 128: 250 us, 825 TFLOP/s of 16-bit products, half of the tensor cores' rate.  A step
@@ -166,7 +168,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
 #pragma unroll
-                    for (int p = 0; p < kPieces; ++p) x[k].raw[p] = row0 + 4 * k < view.rows ? raw_eight(g.a.q, at + 64 * p, decltype(wide)::value) : make_uint4(0u, 0u, 0u, 0u);
+                    for (int p = 0; p < kPieces; ++p) x[k].raw[p] = row0 + 4 * k < view.rows && 64 * p + 8 * (lane & 7) < c.d ? raw_eight(g.a.q, at + 64 * p, decltype(wide)::value) : make_uint4(0u, 0u, 0u, 0u);
                     h += 4; at += 4 * g.a.q_head;
                     while (h >= g.group) { h -= g.group; at += g.a.q_token - g.group * g.a.q_head; }
                 }
@@ -250,10 +252,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 tc_fence_after();
                 const float seen = top;
                 top = max_of(top, mx, tmem_ld1(s_t + (half ? 16u : 32u)));
-                // O and the sum follow the maximum when it is 2^11 ahead, and the largest scale at once
+                // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
                 const float new_ref = ld_shared_f32(smem_u32(&scales[i & 3].ref));
                 const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
-                const bool move = top > used + 11.f || first || ref != new_ref;
+                const bool move = top > used + 8.f || first || ref != new_ref;
                 if (__any_sync(0xffffffffu, move)) {
                     const float now = top == -INFINITY ? 0.f : top;
                     const float alpha = seen != -INFINITY ? exp2_fast(used - now) : 0.f;
@@ -309,6 +311,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         const long long place = unit * c.heads + head;
         constexpr int kPart = kPromptRows * (D + 2);                     // O by eight columns of all rows, then the rows' maxima and sums
         const auto store = [&](int rr, int i, const float (&v)[4]) {
+            if (i >= c.d) return;
             const int tt = (view.h0 + rr) / g.group;
             store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
         };
@@ -325,8 +328,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 sum += tmem_ld1(s_t + (half ? 32u : 64u));
             }
             const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
-            // O is in units of 2^4 and the largest scale; a split's part stays relative to its sum
-            const float unit_o = ref * 0.0625f * (active == 1 ? 1.f / sum : 1.f);
+            // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
+            const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
             float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + 8 * r;
             const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)(r & 127) * (2u * D);      // (where the queries were)
 #pragma unroll 1
@@ -372,7 +375,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 for (int k = 0; k < 16; k += kAtOnce, row += kAtOnce) {
                     uint32_t w[4];
                     read_shared<16>(q_s + (uint32_t)row * (2u * D) + (((uint32_t)i ^ (uint32_t)(row & 7)) << 4), w);
-                    if (row < view.rows && fine) {
+                    if (row < view.rows && 8 * i < c.d && fine) {
                         uint16_t* y = static_cast<uint16_t*>(g.a.y) + at;
                         if (g.y_wide == 2) *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
                         else if (g.y_wide) {
@@ -515,7 +518,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const int* table = c.table + view.b * c.table_row;
             const int shift = 31 - __clz(c.block), box = min(c.block, kPromptTokens);                // tokens of a box
             const uint32_t raw0 = base + 6u * S::kTile;
-            const auto held = [&](int i) { const int t = from + i * kPromptTokens + 16 * (lane & 7); return i < steps && t + 15 >= view.lo && t < to; };
+            // (a box is copied as a whole, by its first group's page: it is held if any of its tokens is)
+            const auto held = [&](int i) { const int t = from + i * kPromptTokens + (16 * (lane & 7) & ~(box - 1)); return i < steps && t + box > view.lo && t < to; };
             const auto page_of = [&](int i) { return held(i) ? table[(from + i * kPromptTokens + 16 * (lane & 7)) >> shift] : -1; };
             const auto good = [&](int i, int pg) {
                 if ((unsigned)pg < (unsigned)c.pages) return pg;
@@ -549,8 +553,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     // (a share of less than 2^-40 of the largest scale is taken as that)
                     const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
                     sc.key[lane] = ks;
-                    sc.shift[lane] = lg + 4.f;
-                    sc.back[lane] = exp2_fast(-lg) * 0.0625f;
+                    sc.shift[lane] = lg + 7.f;
+                    sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
                     if (lane == 0) sc.ref = most;
                 }
                 __syncwarp();
@@ -634,8 +638,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     }
 }
 
-bool prompt_built_for(int d) { return d == 64 || d == 128; }
-
 template <int D>
 static cudaError_t launch_prompt(const Attend& g, long long units, void* stream) {
     typedef PromptShape<D> S;
@@ -646,14 +648,14 @@ static cudaError_t launch_prompt(const Attend& g, long long units, void* stream)
     const tt_cache& c = g.a.cache;
     for (int w = 0; w < 2; ++w) {
         // (without pages nothing is read: the map is of any memory)
-        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], 0, c.block)
-                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, 0, c.block);
+        const tt_status st = g.max_length > 0 ? encode_pages(&maps[w], c.data[w], c.d, c.block, c.heads, c.pages, c.token[w], c.head[w], c.page[w], D, false, c.block)
+                                              : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, D, false, c.block);
         if (st != TT_OK) return cudaErrorInvalidValue;
     }
     return launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, maps[0], maps[1], g);
 }
 cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream) {
-    return g.a.cache.d == 64 ? launch_prompt<64>(g, units, stream) : launch_prompt<128>(g, units, stream);
+    return prompt_head(g.a.cache.d) == 64 ? launch_prompt<64>(g, units, stream) : launch_prompt<128>(g, units, stream);
 }
 
 }  // namespace tt

@@ -722,6 +722,18 @@ def test_attention_of_prompts(d, window):
 
 
 @gpu
+@pytest.mark.parametrize("d", [32, 96])
+@pytest.mark.parametrize("block", [16, 128])
+@pytest.mark.parametrize("window", [0, 1000])
+def test_attention_of_prompts_with_short_heads(d, block, window):
+    p = Pages([700, 64, 1500, 20], 2, d, block, seed=d)
+    check_attention(p, [300, 64, 40, 3], 6, window=window)
+    p = Pages([6000], 1, d, block, seed=d + 1)
+    check_attention(p, [70], 2, kind="f16", window=window)
+    check_attention(p, [70], 2, causal=False)
+
+
+@gpu
 @pytest.mark.parametrize("length,window", [(5000, 0), (9001, 0), (9001, 4000)])
 def test_attention_splits_a_long_sequence(length, window):
     p = Pages([length, 3, 2049], 2, 64, 64, seed=length)
