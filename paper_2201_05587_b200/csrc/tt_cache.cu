@@ -826,14 +826,15 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         plan.prompt_units = (long long)a.tokens * g.group / kPromptRows + c.batch;
         const long long tiles = plan.prompt_units * c.heads, span = span_of(kPromptRows) + kPromptTokens;
         if (tiles > 0x7fffffffll) return TT_ERR_INVALID_ARG;
-        // Fewer tiles than SMs: the keys are split as well, into shares of 1024 tokens at least.
+        // Few tiles: the keys are split as well, into shares of 256 tokens at least, for 128 CTAs at most (144 of heads of 128 values are slower than
+        // 104: 64 tokens over 16000, 8 heads, 50 us and 38) and 16 shares, which the join has under way at once.  Short ones are not worth it (300
+        // tokens, 8 heads: 14 us whole, 18 in two).
         long long chunk = span;
-        if (tiles < kSms) {
-            const long long shares = kSms / tiles;
+        if (2 * tiles <= kPromptCtas && span >= 6 * kPromptTokens) {
+            const long long shares = kPromptCtas / tiles < kPromptSplits ? kPromptCtas / tiles : kPromptSplits;
             chunk = (span + shares - 1) / shares;
             chunk = (chunk + kPromptTokens - 1) / kPromptTokens * kPromptTokens;
-            if (chunk < 1024) chunk = 1024;
-            while ((span + chunk - 1) / chunk > kPromptSplits) chunk += kPromptTokens;
+            if (chunk < 2 * kPromptTokens) chunk = 2 * kPromptTokens;
         }
         p.chunk = (int)(chunk < span ? chunk : (span + kPromptTokens - 1) / kPromptTokens * kPromptTokens);
         p.splits = (int)((span + p.chunk - 1) / p.chunk);

@@ -71,6 +71,7 @@ __device__ __forceinline__ void join_splits(int elements, int splits, const PART
         }
     };
     if (splits <= 4) go(std::integral_constant<int, 4>());
+    else if (splits <= 8) go(std::integral_constant<int, 2>());
     else go(std::integral_constant<int, 1>());
 }
 
@@ -89,7 +90,8 @@ struct Attend {
     unsigned* counters; float* partial;
 };
 constexpr int kPromptRows = 256;            // rows of a tile of tt_attend_prompt_kernel
-constexpr int kPromptSplits = 32;           // its most splits of a sequence
+constexpr int kPromptSplits = 16;           // its most splits of a sequence
+constexpr int kPromptCtas = 128;            // CTAs of it that tiles are split for
 constexpr int kPromptTokens = 128;          // tokens of a step of it
 constexpr int prompt_head(int d) { return d <= 64 ? 64 : 128; }      // what tt_attend_prompt_kernel is built for that holds a head of d
 constexpr bool prompt_built_for(int d) { return d <= 128; }

@@ -11,7 +11,7 @@
 // a column of small values beside one key of nearly all the weight was off by more than a rounding), and the row's sum has
 // the same factor.  A page's scale of values is in
 // P too, as the part of the exponent, over the largest scale so far.
-//   Two prompts of 2048 tokens behind as many, 32 heads over 8 of 128: 250 us, 825 TFLOP/s of 16-bit products, half of the tensor cores' rate.  A step
+//   Two prompts of 2048 tokens behind as many, 32 heads over 8 of 128: 252 us, 817 TFLOP/s of 16-bit products, half of the tensor cores' rate.  A step
 // of 128 keys takes 3500 to 3900 cycles: the products 2050, the exponentials 2050 and the shared memory 2560, and a tile's chain (its softmax, then the
 // product that takes P and the one that makes the next scores) 3500, which is the bound.  The way in and out are 11000 and 6000 cycles of a CTA.
 // (Scores of the second 64 keys while P of the first is being made: 370 us, as the queries are read twice.  A part of the exponentials as polynomials:
@@ -79,12 +79,17 @@ __device__ __forceinline__ float2 ld_shared_v2f(uint32_t addr) {
 template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Named barriers: 1 the softmax and the warps of keys and values, 2 the softmax and the MMA warp (at the end), 3 the softmax alone.
+// Named barriers: 1 the softmax and the warps of keys and values, 2 the softmax and the MMA warp (at the end), 4 and 5 a tile's softmax.
 __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // What the softmax needs to know of a step's eight groups of 16 tokens.
 struct alignas(16) StepScales { float key[8], shift[8], back[8]; float ref; };
+
+// Splits of a tile that have anything to do.
+__device__ __forceinline__ int prompt_splits(const Attend& g, const TileView& view) {
+    return view.hi > view.lo ? (int)((unsigned)(view.hi - view.lo / kPromptTokens * kPromptTokens + g.chunk - 1) / (unsigned)g.chunk) : 1;
+}
 
 template <int D>
 struct PromptShape {
@@ -103,7 +108,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     __shared__ int nan_first[D], nan_last[D], nan_any;
     __shared__ uint8_t sizes[kPromptRows];                                // of the queries' rows: the exponents of what they were multiplied by
     __shared__ uint32_t tmem_slot;
-    __shared__ int abort_flag, last_one;
+    __shared__ int late[6];                                               // what the way out needs (the softmax has no registers to keep it in)
+    __shared__ int abort_flag;
 
     const tt_cache& c = g.a.cache;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, head = blockIdx.y;
@@ -113,7 +119,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     const long long unit = (long long)gridDim.x - 1 - blockIdx.x;       // (the last tiles see the most; all heads' last ones first: 253 us for 249)
     if (!view_tile(g, kPromptRows, unit, view)) return;
     const int base_token = view.lo / kPromptTokens * kPromptTokens;
-    const int active = view.hi > view.lo ? (int)((unsigned)(view.hi - base_token + g.chunk - 1) / (unsigned)g.chunk) : 1;
+    const int active = prompt_splits(g, view);
     if ((int)blockIdx.z >= active) return;
     const int from = base_token + (int)blockIdx.z * g.chunk, to = view.hi - from > g.chunk ? from + g.chunk : view.hi;
     const int steps = to > from ? (to - from - 1) / kPromptTokens + 1 : 0;
@@ -132,6 +138,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         mbar_init(smem_u32(&raw_empty[0]), 4u); mbar_init(smem_u32(&raw_empty[1]), 4u);
         mbar_init(smem_u32(&drained), 1u);
         abort_flag = nan_any = 0;
+        late[0] = view.start + view.t0; late[1] = view.h0; late[2] = view.rows; late[3] = active; late[4] = view.before + view.t0; late[5] = view.hi;
         fence_mbar_init();
         fence_proxy_async_shared();
     }
@@ -148,8 +155,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 
     // a softmax thread's row
     const int tile = warp >> 3, half = (warp >> 2) & 1, r = tile * 128 + (int)(threadIdx.x & 127);      // (a half of its columns)
-    const bool mine = warp < 16 && r < view.rows;
-    const int row_t = view.t0 + (view.h0 + r) / g.group;
     float top = -INFINITY, used = 0.f, sum = 0.f, ref = 0.f;              // maximum; the one that O and the sum are relative to; the unit of O
     bool fine = true;
 
@@ -207,8 +212,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         const float factor = fabsf(g.scale_log2) / __int_as_float((int)sizes[r] << 23);
 
         // ---------------- softmax ----------------
-        const int row_pos = view.before + row_t;                          // the row sees tokens row_lo .. row_hi - 1
-        const int row_hi = g.a.causal ? min(view.hi, row_pos + 1) : view.hi, row_lo = g.a.window > 0 ? row_pos + 1 - g.a.window : 0;
+        const volatile int* out = late;
+        // the row's position, and the tokens lo .. hi - 1 that it sees (looked up again wherever they are needed)
+        struct Seen { int pos, lo, hi; };
+        const auto seen_by_row = [&] {
+            const int pos = out[4] + (out[1] + r) / g.group;
+            return Seen{pos, g.a.window > 0 ? pos + 1 - g.a.window : 0, g.a.causal ? min(out[5], pos + 1) : out[5]};
+        };
         const uint32_t s_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kScores + (uint32_t)tile * 128u;
         const uint32_t o_t = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::kOut + (uint32_t)(tile * D);
         if (tile < tiles) {
@@ -220,13 +230,14 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 const bool whole = t >= view.whole_lo && t + kPromptTokens <= view.whole_hi;
                 // This half has columns 32 * half .. + 31 and the 32 that are 64 further on (so both halves' first 32 let a product begin); of a
                 // place k, `column` is relative to 32 * half, and the row sees columns j_lo .. j_hi - 1.
-                const int j_lo = row_lo - t - 32 * half, j_hi = row_hi - t - 32 * half;
                 const auto column = [](int k) { return k < 32 ? k : k + 32; };
                 uint32_t v[64];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) tmem_ld32(s_t + 32u * (uint32_t)half + 64u * h, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * h]));
                 tmem_wait_ld();
                 if (!whole) {
+                    const Seen s = seen_by_row();
+                    const int j_lo = s.lo - t - 32 * half, j_hi = s.hi - t - 32 * half;
 #pragma unroll
                     for (int k = 0; k < 64; ++k) v[k] = column(k) >= j_lo && column(k) < j_hi ? v[k] : 0xff800000u;      // (-inf)
                 }
@@ -308,13 +319,10 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         }
         // ---------------- out ----------------
         named_sync(1, kSoftmax + 128);                                               // (every NaN of the steps at the edges has been noted)
+        const int token0 = out[0], h0 = out[1], rows = out[2], active = out[3];
+        const bool mine = r < rows;
         const long long place = unit * c.heads + head;
         constexpr int kPart = kPromptRows * (D + 2);                     // O by eight columns of all rows, then the rows' maxima and sums
-        const auto store = [&](int rr, int i, const float (&v)[4]) {
-            if (i >= c.d) return;
-            const int tt = (view.h0 + rr) / g.group;
-            store_four(g.a.y, (view.start + view.t0 + (long long)tt) * g.a.y_token + (long long)(head * g.group + (view.h0 + rr) % g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
-        };
         if (tile < tiles) {
             if (steps > 0 && fine) fine = __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(steps - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
             tc_fence_after();
@@ -327,7 +335,9 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 tc_fence_after();
                 sum += tmem_ld1(s_t + (half ? 32u : 64u));
             }
-            const bool none = steps == 0 || row_hi <= max(row_lo, from) || row_lo >= to;      // the row sees nothing here
+            const Seen s = seen_by_row();
+            const int row_pos = s.pos;
+            const bool none = steps == 0 || s.hi <= max(s.lo, from) || s.lo >= to;      // the row sees nothing here
             // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
             const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
             float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + 8 * r;
@@ -369,13 +379,13 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 // rows of a tile to its warps, so that what a warp stores lies side by side
                 constexpr int kAcross = D / 8, kAtOnce = 32 / kAcross;
                 const int i = lane % kAcross;
-                int row = tile * 128 + (warp & 7) * 16 + lane / kAcross, t = (view.h0 + row) / g.group, h = view.h0 + row - t * g.group;
-                long long at = ((long long)view.start + view.t0 + t) * g.a.y_token + (long long)(head * g.group + h) * g.a.y_head + 8 * i;
+                int row = tile * 128 + (warp & 7) * 16 + lane / kAcross, t = (h0 + row) / g.group, h = h0 + row - t * g.group;
+                long long at = ((long long)token0 + t) * g.a.y_token + (long long)(head * g.group + h) * g.a.y_head + 8 * i;
 #pragma unroll 4
                 for (int k = 0; k < 16; k += kAtOnce, row += kAtOnce) {
                     uint32_t w[4];
                     read_shared<16>(q_s + (uint32_t)row * (2u * D) + (((uint32_t)i ^ (uint32_t)(row & 7)) << 4), w);
-                    if (row < view.rows && 8 * i < c.d && fine) {
+                    if (row < rows && 8 * i < c.d && fine) {
                         uint16_t* y = static_cast<uint16_t*>(g.a.y) + at;
                         if (g.y_wide == 2) *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
                         else if (g.y_wide) {
@@ -397,38 +407,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         tc_fence_before();
         __syncwarp();
         named_arrive(2, kSoftmax + 32);                                             // (the tensor memory has been read)
-        if (active == 1) return;
-
-        // ---------------- the splits together, by the last CTA of the tile ----------------
-        __threadfence();
-        named_sync(3, kSoftmax);
-        if (threadIdx.x == 0) last_one = atomicAdd(g.counters + place, 1u) == (unsigned)active - 1u;
-        named_sync(3, kSoftmax);
-        if (!last_one) return;
-        __threadfence();
-        const float* parts = g.partial + place * g.splits * kPart;
-        float* share = reinterpret_cast<float*>(smem_raw);               // [split][row]
-        if (mine && half == 0) {
-            float mx = -INFINITY, l = 0.f;
-            for (int z = 0; z < active; ++z) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * r));
-                if (ml.y != 0.f) mx = fmaxf(mx, ml.x);
-            }
-            for (int z = 0; z < active; ++z) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(parts + (long long)z * kPart + kPromptRows * D + 2 * r));
-                const float k = ml.y != 0.f ? exp2_fast(ml.x - mx) : 0.f;
-                if (ml.y != 0.f) l += ml.y * k;
-                share[z * kPromptRows + r] = k;
-            }
-            const float inv = l != 0.f ? 1.f / l : 0.f;
-            for (int z = 0; z < active; ++z) share[z * kPromptRows + r] *= inv;
-        }
-        named_sync(3, kSoftmax);
-        join_splits<kSoftmax>(view.rows * (D / 4), active,
-            [&](int e, int z) { const int rr = e / (D / 4), i = 4 * (e % (D / 4)); return reinterpret_cast<const float4*>(parts + (long long)z * kPart + (i >> 3) * (8 * kPromptRows) + 8 * rr + (i & 4)); },
-            [&](int e, int z) { return share[z * kPromptRows + e / (D / 4)]; },
-            [&](int e, const float (&v)[4]) { store(e / (D / 4), 4 * (e % (D / 4)), v); });
-        if (threadIdx.x == 0) g.counters[place] = 0u;                    // ready for the next call
     } else if (warp < 20) {
         registers_down<56>();
         // ---------------- keys and values: pages -> operand tiles ----------------
@@ -638,6 +616,58 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     }
 }
 
+// The splits of a tile together, kBandRows of its rows a CTA, in the order of the splits.  A kernel of its own: what one SM reads of another's results
+// comes at 14 bytes a cycle, and a split of a tile is 130 KB.  (Two prompts of 300
+// tokens over 8000, 4 heads over one of 128: 40 us; joined by the last CTA of a tile 79.)
+constexpr int kBandRows = 16;
+template <int D>
+__global__ void __launch_bounds__(128) tt_attend_join_kernel(const Attend g) {
+    __shared__ float share[kPromptSplits * kBandRows];
+    pdl_allow_next();
+    pdl_wait_prev();
+    const tt_cache& c = g.a.cache;
+    constexpr int kBands = kPromptRows / kBandRows, kPart = kPromptRows * (D + 2);
+    const int head = blockIdx.y, row0 = (int)blockIdx.x % kBands * kBandRows;
+    const long long unit = blockIdx.x / kBands;
+    TileView view;
+    if (!view_tile(g, kPromptRows, unit, view)) return;
+    const int active = prompt_splits(g, view), rows = min(kBandRows, view.rows - row0);
+    if (active == 1 || rows <= 0) return;
+    const float* parts = g.partial + (unit * c.heads + head) * g.splits * kPart;
+    // eight lanes have a row: its maxima and sums of the splits
+    const int r = (int)threadIdx.x >> 3, l = (int)threadIdx.x & 7;
+    constexpr int kOwn = kPromptSplits / 8;
+    float2 ml[kOwn];
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        ml[k] = make_float2(-INFINITY, 0.f);
+        if (l + 8 * k < active && r < rows) ml[k] = *reinterpret_cast<const float2*>(parts + (long long)(l + 8 * k) * kPart + kPromptRows * D + 2 * (row0 + r));
+    }
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) if (ml[k].y != 0.f) mx = fmaxf(mx, ml[k].x);
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+        ml[k].x = ml[k].y != 0.f ? exp2_fast(ml[k].x - mx) : 0.f;
+        if (ml[k].y != 0.f) sum += ml[k].y * ml[k].x;
+    }
+#pragma unroll
+    for (int d = 4; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) share[(l + 8 * k) * kBandRows + r] = ml[k].x * inv;
+    __syncthreads();
+    join_splits<128>(rows * (D / 4), active,
+        [&](int e, int z) { const int rr = row0 + e / (D / 4), i = 4 * (e % (D / 4)); return reinterpret_cast<const float4*>(parts + (long long)z * kPart + (i >> 3) * (8 * kPromptRows) + 8 * rr + (i & 4)); },
+        [&](int e, int z) { return share[z * kBandRows + e / (D / 4)]; },
+        [&](int e, const float (&v)[4]) {
+            const int rr = view.h0 + row0 + e / (D / 4), i = 4 * (e % (D / 4)), t = rr / g.group;
+            if (i < c.d) store_four(g.a.y, (view.start + view.t0 + (long long)t) * g.a.y_token + (long long)(head * g.group + rr - t * g.group) * g.a.y_head + i, g.a.type, g.y_wide, v);
+        });
+}
+
 template <int D>
 static cudaError_t launch_prompt(const Attend& g, long long units, void* stream) {
     typedef PromptShape<D> S;
@@ -652,7 +682,9 @@ static cudaError_t launch_prompt(const Attend& g, long long units, void* stream)
                                               : encode_pages(&maps[w], reinterpret_cast<const void*>(reinterpret_cast<uintptr_t>(g.a.y) & ~uintptr_t(15)), c.d, c.block, 1, 1, c.d, c.d, c.d, D, false, c.block);
         if (st != TT_OK) return cudaErrorInvalidValue;
     }
-    return launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, maps[0], maps[1], g);
+    const cudaError_t e = launch(tt_attend_prompt_kernel<D>, dim3((unsigned)units, (unsigned)g.a.cache.heads, (unsigned)g.splits), kPromptThreads, S::kBytes, 1, stream, maps[0], maps[1], g);
+    if (e != cudaSuccess || g.splits == 1) return e;
+    return launch(tt_attend_join_kernel<D>, dim3((unsigned)units * (kPromptRows / kBandRows), (unsigned)g.a.cache.heads, 1), 128, 0, 1, stream, g);
 }
 cudaError_t launch_attend_prompt(const Attend& g, long long units, void* stream) {
     return prompt_head(g.a.cache.d) == 64 ? launch_prompt<64>(g, units, stream) : launch_prompt<128>(g, units, stream);
