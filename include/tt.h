@@ -475,7 +475,7 @@ tt_status tt_dense_static_scratch(const void* x, const void* w, const void* bias
  * What a program calls that keeps weights, keys and values in e4m3 (one sign, four exponent and three mantissa bits, largest value
  * 448, no infinities): the dense layer, the quantisation in front of it, rotary positions, and a paged cache with its attention.
  * Each call takes its arguments in a structure of plain pointers, sizes and strides (in elements, unless stated otherwise; the
- * innermost axis of every tensor is contiguous), checks them, enqueues a kernel (attention two at most) on `cuda_stream` of the current device and returns.
+ * innermost axis of every tensor is contiguous), checks them, enqueues a kernel (attention three at most) on `cuda_stream` of the current device and returns.
  * What a call writes overlaps neither itself (the two tensors of a rotary call or an append, say) nor, but where it is said, what it reads.
  * Nothing is kept between calls and no device memory is allocated, so calls may be captured, and calls that share no output, status word
  * or workspace may run at the same time.  Null pointers, unknown types, sizes that are negative or too large and strides or addresses that a call
