@@ -561,7 +561,7 @@ tt_status tt_cache_append(const tt_cache_append_args* a, void* cuda_stream);
  * max_count: the most queries of any sequence, max_length: the longest of the lengths, bounds that the work is dealt by (0: not known, then
  * tokens and max_pages * block); a sequence beyond them is reported in the status word.
  * workspace: tt_cache_attention_workspace bytes of device memory on a 16-byte boundary, cleared once before its first call; calls leave it
- * ready for the next one.  Runs that share a workspace follow each other: the caller orders them when they go to different streams.
+ * ready for the next one, of whatever sizes.  Runs that share a workspace follow each other: the caller orders them when they go to different streams.
  * Deterministic. */
 typedef struct tt_cache_attention_args {
     tt_cache cache;

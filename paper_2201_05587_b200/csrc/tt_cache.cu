@@ -751,12 +751,15 @@ static tt_status check_cache_memory(const tt_cache& c) {
 struct AttendPlan {
     Attend few{}, prompt{};
     long long few_units = 0, prompt_units = 0;              // 0: the kernel is not needed
-    long long bytes = 0, prompt_at = 0;                     // of the workspace; where the second one's part begins
+    long long bytes = 0, prompt_at = 0;                     // of the workspace; where the prompts' part begins
 };
-// d: of a head, as the kernel is built for it
+// The workspace begins with the counters of tt_attend_few_kernel, in a place that is theirs whatever the sizes of a call: they are zeros between calls
+// of any sizes.  (A tile has splits where there are no more than 2 * slots of them, see plan_attend.)
+constexpr int kCounterBytes = 4096;
+static_assert(2 * kSms * 3 * 4 <= kCounterBytes, "a counter for each tile that is split");
+// The sums behind them.  d: of a head, as the kernel is built for it
 static long long workspace_part(const Attend& g, long long units, int d) {
-    const long long tiles = units * g.a.cache.heads;
-    return g.splits > 1 ? (tiles * 4 + 15) / 16 * 16 + tiles * g.splits * g.rows * (d + 2) * 4 : 0;
+    return g.splits > 1 ? units * g.a.cache.heads * g.splits * g.rows * (d + 2) * 4 : 0;
 }
 static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan) {
     const tt_cache& c = a.cache;
@@ -791,6 +794,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
     // what a tile's rows and a step span, so that no step is at both ends of it.)
     const bool prompts = most_rows > kFewRows && prompt_built_for(c.d) && (a.window == 0 || a.window > kPromptRows / g.group + 2 * kPromptTokens + 2);
     const bool few = !prompts || c.batch > 1;
+    long long few_bytes = 0, prompt_bytes = 0;
     if (few) {
         Attend& f = plan.few;
         f = g;
@@ -816,7 +820,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         f.chunk = (int)chunk;
         f.splits = (int)((span + chunk - 1) / chunk);
         if (f.splits < 1) f.splits = 1;
-        plan.bytes = workspace_part(f, plan.few_units, c.d);
+        few_bytes = workspace_part(f, plan.few_units, c.d);
     }
     if (prompts) {
         Attend& p = plan.prompt;
@@ -838,15 +842,15 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
         }
         p.chunk = (int)(chunk < span ? chunk : (span + kPromptTokens - 1) / kPromptTokens * kPromptTokens);
         p.splits = (int)((span + p.chunk - 1) / p.chunk);
-        plan.prompt_at = plan.bytes = (plan.bytes + 15) / 16 * 16;
-        plan.bytes += workspace_part(p, plan.prompt_units, prompt_head(c.d));
+        prompt_bytes = workspace_part(p, plan.prompt_units, prompt_head(c.d));
     }
+    plan.prompt_at = kCounterBytes + (few_bytes + 15) / 16 * 16;
+    plan.bytes = few_bytes + prompt_bytes > 0 ? plan.prompt_at + prompt_bytes : 0;
     return TT_OK;
 }
-static void place(Attend& g, long long units, void* workspace, long long at) {
-    uint8_t* w = static_cast<uint8_t*>(workspace) + (g.splits > 1 ? at : 0);
-    g.counters = reinterpret_cast<unsigned*>(w);
-    g.partial = reinterpret_cast<float*>(w + (units * g.a.cache.heads * 4 + 15) / 16 * 16);
+static void place(Attend& g, void* workspace, long long at) {
+    g.counters = static_cast<unsigned*>(workspace);
+    g.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + (g.splits > 1 ? at : 0));
 }
 
 template <int D, int NT>
@@ -925,13 +929,13 @@ extern "C" tt_status tt_cache_attention(const tt_cache_attention_args* a, void* 
         reinterpret_cast<uintptr_t>(a->status) % 4) return TT_ERR_INVALID_ARG;
     if (plan.bytes > 0 && (!a->workspace || !on16(a->workspace) || a->workspace_bytes < plan.bytes)) return TT_ERR_INVALID_ARG;
     if (plan.prompt_units > 0) {
-        place(plan.prompt, plan.prompt_units, a->workspace, plan.prompt_at);
+        place(plan.prompt, a->workspace, plan.prompt_at);
         s = status_of(launch_attend_prompt(plan.prompt, plan.prompt_units, stream));
         if (s != TT_OK || plan.few_units == 0) return s;
     }
     const Attend& g = plan.few;
     const long long units = plan.few_units;
-    place(plan.few, units, a->workspace, 0);
+    place(plan.few, a->workspace, kCounterBytes);
     switch (c.d) {
         case 32: return status_of(launch_attend_rows<32>(g, units, stream));
         case 64: return status_of(launch_attend_rows<64>(g, units, stream));

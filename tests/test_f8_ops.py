@@ -928,6 +928,27 @@ def test_attention_reports_starts_that_do_not_rise_from_0(heads_q, max_count):
         assert (y[:max(0, min(starts))] == 7.0).all()          # (a sequence whose own starts rise has its rows)
 
 
+@gpu
+def test_one_workspace_serves_calls_of_all_sizes():
+    # (batch, heads, query heads, new tokens, length): most of them split, by either kernel, each over what the ones before have left
+    sizes = [(1, 8, 8, 1, 5000), (8, 8, 8, 1, 2500), (32, 2, 8, 1, 1100), (1, 1, 4, 70, 6000), (3, 1, 8, 2, 4000), (1, 8, 8, 1, 5000), (2, 1, 2, 40, 5000), (9, 8, 8, 1, 2600)]
+    workspace = torch.zeros(1 << 26, dtype=torch.uint8, device="cuda")
+    for i, (batch, heads, heads_q, count, length) in enumerate(sizes):
+        p = Pages([length - 7 * b for b in range(batch)], heads, 64, 64, seed=i)
+        counts = [count] * batch
+        q = (torch.randn(batch * count, heads_q, 64, generator=gen(i), device="cuda") * 2).to(torch.float16)
+        y = torch.full_like(q, -77.0)
+        call = B.cache_attention(p.cache(), q, y, int32([count * b for b in range(batch + 1)]), int32(p.lengths), 0.125, max_count=count)
+        assert call.args.workspace_bytes <= workspace.numel()
+        call.args.workspace, call.args.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        for _ in range(2):
+            call.run()
+            assert call.status() == B.TT_OK
+            ref, off = reference_attention(p, counts, q, 0.125, True, 0)
+            assert (np.abs(y.double().cpu().numpy() - ref) <= off + HALF_STEP[torch.float16] * (np.abs(ref) + off) + 2.0 ** -25).all(), i
+            y.fill_(-77.0)
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
