@@ -301,14 +301,15 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     }();
     const int steps = (groups + S::kGroups - 1) / S::kGroups;
     const auto token_of = [&](int group) { return from + ((group >> 2) * kAttendWarps + warp) * kRun + (group & 3) * kStep; };
-    // Lane l has the page and the scales of group 32 i + l, and of the set of 32 behind it.
+    // Lane l has the page and the scales of group 32 i + l, and of the set of 32 behind it.  A split's first groups may be of pages in front of what any
+    // row sees, which the sequence need not have any more: zeros, as behind the last group.
     const int* table = c.table + b * c.table_row;
     const int shift = 31 - __clz(c.block);
     struct Set { int page; float ks, vs; };
     const auto look_up = [&](int set) {
         const int group = 32 * set + lane;
         Set x{-1, 0.f, 0.f};
-        if (group < groups) {
+        if (group < groups && (token_of(group) | (c.block - 1)) >= lo) {
             x.page = table[token_of(group) >> shift];
             if ((unsigned)x.page >= (unsigned)c.pages) {
                 report_invalid(g.a.status);

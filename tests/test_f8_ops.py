@@ -949,6 +949,20 @@ def test_one_workspace_serves_calls_of_all_sizes():
             y.fill_(-77.0)
 
 
+@gpu
+@pytest.mark.parametrize("block", [16, 32, 64])
+@pytest.mark.parametrize("length,count,heads_q,window", [(300, 1, 4, 20), (300, 3, 4, 37), (745, 5, 2, 301), (5000, 2, 8, 2100), (1500, 40, 2, 1000), (6000, 40, 2, 4000), (400, 40, 2, 30)])
+def test_attention_needs_no_page_in_front_of_the_window(block, length, count, heads_q, window):
+    given_back = (length - count + 1 - window) // block            # pages that no query sees
+    for entry in (-1, None):
+        p = Pages([length], 1, 64, block, seed=window)
+        p.ks[p.free[:1]], p.vs[p.free[:1]] = math.nan, math.nan
+        p.ks[p.free[1:2]], p.vs[p.free[1:2]] = math.inf, math.inf
+        for j in range(given_back):                                # none, or one of another's with scales of anything
+            p.table[0, j] = entry if entry is not None else p.free[j % 2]
+        check_attention(p, [count], heads_q, window=window)
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
