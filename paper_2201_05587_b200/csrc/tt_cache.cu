@@ -778,6 +778,7 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
     g.scale_log2 = a.scale * 1.4426950408889634f;
     g.max_length = c.pages > 0 ? c.max_pages * c.block : 0;
     if (a.max_length > 0 && a.max_length < g.max_length) g.max_length = a.max_length;
+    if (a.window >= g.max_length) g.a.window = 0;             // (it hides nothing, and the first token of such a window need not be a 32-bit number)
     const auto wide = [](const void* p, long long token, long long head) {
         const auto at = [&](int n) { return reinterpret_cast<uintptr_t>(p) % (2 * n) == 0 && token % n == 0 && head % n == 0; };
         return at(8) ? 2 : at(4) ? 1 : 0;
@@ -789,11 +790,11 @@ static tt_status plan_attend(const tt_cache_attention_args& a, AttendPlan& plan)
     if (most_rows > 0x7fffffff) return TT_ERR_INVALID_ARG;
     const auto span_of = [&](int rows) {
         const long long span = g.max_length, tokens = rows / g.group + 2;
-        return a.window > 0 && a.window + tokens < span ? a.window + tokens : span;
+        return g.a.window > 0 && g.a.window + tokens < span ? g.a.window + tokens : span;
     };
     // More than kFewRows rows of a sequence are a prompt's: its tiles take the tensor cores, whose minimum is 128 rows.  (A window must be longer than
     // what a tile's rows and a step span, so that no step is at both ends of it.)
-    const bool prompts = most_rows > kFewRows && prompt_built_for(c.d) && (a.window == 0 || a.window > kPromptRows / g.group + 2 * kPromptTokens + 2);
+    const bool prompts = most_rows > kFewRows && prompt_built_for(c.d) && (g.a.window == 0 || g.a.window > kPromptRows / g.group + 2 * kPromptTokens + 2);
     const bool few = !prompts || c.batch > 1;
     long long few_bytes = 0, prompt_bytes = 0;
     if (few) {

@@ -963,6 +963,16 @@ def test_attention_needs_no_page_in_front_of_the_window(block, length, count, he
         check_attention(p, [count], heads_q, window=window)
 
 
+@gpu
+@pytest.mark.parametrize("heads_q", [1, 8])
+def test_attention_with_a_window_as_long_as_a_number_can_be(heads_q):
+    for lengths, counts in (([3, 50], [8, 20]), ([100], [120])):      # (queries in front of the tokens see none)
+        p = Pages(lengths, 1, 64, 16, seed=2)
+        y = check_attention(p, counts, heads_q, window=(1 << 31) - 1)
+        assert torch.equal(y, check_attention(p, counts, heads_q))
+        check_attention(p, counts, heads_q, window=max(lengths))      # (another form may take it: the same within the roundings)
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
