@@ -159,8 +159,9 @@ __global__ void __launch_bounds__(WARP ? 256 : kAppendThreads, WARP ? 3 : 7) tt_
 // a ring of the warp's own, so the loop has no barrier but theirs.  (Copied by the lanes, 16 bytes each, they were bound by what the load
 // unit takes, 4 TB/s.)
 //   e4m3 -> 16-bit floating point is exact, and so is a row of queries: brought to a maximum of 2^14..2^15 by a power of two, which the
-// scores' factor takes back.  Probabilities are rounded to 11 bits, times 2^15 and the page's scale over the largest so far, so that what is
-// 2^-29 of the largest still has all of them; sums are in 32 bits.
+// scores' factor takes back.  What a probability is rounded to 11 bits as has the scale of the page's values in it, and the running maximum is one of
+// scores with those scales: it is of each row's own tokens, so that no page that only another row sees takes bits from it. 2^-29 of the
+// largest still has all of them; sums are in 32 bits.
 //   The keys of a sequence are split over CTAs, of which the last to finish adds up what all have left in the workspace, in their order.
 //   (64 sequences of up to 8192 tokens, 32 heads over 8 of 128: 117 us, 5.3 TB/s, 0.81 of a copy's rate; one of 131072 tokens: 54 us, 0.76.)
 
@@ -305,10 +306,10 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     // row sees, which the sequence need not have any more: zeros, as behind the last group.
     const int* table = c.table + b * c.table_row;
     const int shift = 31 - __clz(c.block);
-    struct Set { int page; float ks, vs; };
+    struct Set { int page; float ks, lg; };                  // lg: of the values' scale, a power of two (0 is 2^-126)
     const auto look_up = [&](int set) {
         const int group = 32 * set + lane;
-        Set x{-1, 0.f, 0.f};
+        Set x{-1, 0.f, -126.f};
         if (group < groups && (token_of(group) | (c.block - 1)) >= lo) {
             x.page = table[token_of(group) >> shift];
             if ((unsigned)x.page >= (unsigned)c.pages) {
@@ -316,7 +317,8 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
                 x.page = -1;                                  // (a box outside of the tensor is zeros)
             } else {
                 x.ks = c.scale[0][x.page * c.s_page[0] + head * c.s_head[0]];
-                x.vs = c.scale[1][x.page * c.s_page[1] + head * c.s_head[1]];
+                const float vs = c.scale[1][x.page * c.s_page[1] + head * c.s_head[1]];
+                if (!(vs <= 1.17549435e-38f)) x.lg = log2f(vs);
             }
         }
         return x;
@@ -436,7 +438,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
-    float top[NT][2], sum[NT][2], ref = 0.f;                 // ref: the largest scale of values so far, the unit of o
+    float top[NT][2], sum[NT][2], ref = -50.f;               // ref: the largest scale of values so far, as a power of two; the unit of o is 2^(ref - 15)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -466,13 +468,29 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
         if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
         const int t = token_of(step * S::kGroups);
         const bool whole = t >= view.whole_lo && t + S::kTokens <= view.whole_hi && step * S::kGroups + S::kGroups <= groups;
-        float ks[S::kGroups], vs[S::kGroups], new_ref = ref;
+        float ks[S::kGroups], lg[S::kGroups], new_ref = ref;
 #pragma unroll
         for (int i = 0; i < S::kGroups; ++i) {
             const int group = step * S::kGroups + i;         // (a last step may have fewer: zeros)
             ks[i] = __shfl_sync(0xffffffffu, now.ks, group & 31);
-            vs[i] = __shfl_sync(0xffffffffu, now.vs, group & 31);
-            new_ref = fmaxf(new_ref, vs[i]);
+            lg[i] = __shfl_sync(0xffffffffu, now.lg, group & 31);
+            new_ref = fmaxf(new_ref, lg[i]);
+        }
+        if (new_ref != ref) {                                // o stays as it is: what it is relative to is lower by as much as its unit is higher
+            const float more = exp2_fast(fminf(new_ref - ref, 120.f));      // (not infinite: the first time the sum is 0)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) { top[n][e] -= new_ref - ref; sum[n][e] *= more; }
+            ref = new_ref;
+        }
+        // A page's scale over the largest, which is added to its scores, and what takes it (and the 2^15) out of the sum again.  (2^-80 at least, so that
+        // all probabilities of 2^-46 and more are in the sum; NaN stays, but for the sum, whose rows need not see it.)
+        float back[S::kGroups];
+#pragma unroll
+        for (int i = 0; i < S::kGroups; ++i) {
+            lg[i] = lg[i] < ref - 80.f ? -80.f : lg[i] - ref;
+            back[i] = exp2_fast(fminf(-lg[i], 80.f) - 15.f);
         }
         // scores of 16 tokens x rows: tokens g, g + 8 and rows 2c, 2c + 1 of each eight (in two sums, a chain of products half as long)
         float s[S::kGroups][NT][2][4];
@@ -510,13 +528,9 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             }
         }
         // the running maximum, in powers of two
-        const float shrink = ref == new_ref ? 1.f : __fdividef(ref, new_ref);
-        bool moved = shrink != 1.f;
-        ref = new_ref;
-        float unit[S::kGroups], alpha[NT][2];
+        bool moved = false;
+        float alpha[NT][2];
         uint32_t pb[S::kGroups][NT][2];
-#pragma unroll
-        for (int i = 0; i < S::kGroups; ++i) unit[i] = vs[i] == new_ref ? 32768.f : __fdividef(vs[i], new_ref) * 32768.f;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             float v[S::kGroups][4];
@@ -524,7 +538,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             for (int i = 0; i < S::kGroups; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[i][e] = (s[i][n][0][e] + s[i][n][1][e]) * (factor[n][e & 1] * ks[i]);
+                    v[i][e] = fmaf(s[i][n][0][e] + s[i][n][1][e], factor[n][e & 1] * ks[i], lg[i]);
                     if (!whole) v[i][e] = sees(8 * n + 2 * cq + (e & 1), t + kStep * i + row0 + 8 * (e >> 1)) ? v[i][e] : -INFINITY;
                 }
 #pragma unroll
@@ -532,7 +546,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
                 float mx = fmaxf(v[0][e], v[0][e + 2]);
 #pragma unroll
                 for (int i = 1; i < S::kGroups; ++i) mx = fmaxf(mx, fmaxf(v[i][e], v[i][e + 2]));
-                mx = fmaxf(top[n][e], octet_max(mx));
+                mx = fmaxf(top[n][e], octet_max(mx) - 15.f);      // (P is 2^15 at most)
                 const float ref_max = mx == -INFINITY ? 0.f : mx;
                 const float keep = exp2_fast(top[n][e] - ref_max);
                 moved = moved || mx != top[n][e];
@@ -542,15 +556,15 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
                 for (int i = 0; i < S::kGroups; ++i) {
                     v[i][e] = exp2_fast(v[i][e] - ref_max);
                     v[i][e + 2] = exp2_fast(v[i][e + 2] - ref_max);
-                    add += v[i][e] + v[i][e + 2];
+                    add = fmaf(v[i][e] + v[i][e + 2], back[i], add);
                 }
                 sum[n][e] = fmaf(sum[n][e], keep, add);
-                alpha[n][e] = keep * shrink;
+                alpha[n][e] = keep;
             }
 #pragma unroll
             for (int i = 0; i < S::kGroups; ++i) {
-                pb[i][n][0] = transpose_8x8(down2<TT_TYPE_F16>(v[i][0] * unit[i], v[i][1] * unit[i]));
-                pb[i][n][1] = transpose_8x8(down2<TT_TYPE_F16>(v[i][2] * unit[i], v[i][3] * unit[i]));
+                pb[i][n][0] = transpose_8x8(down2<TT_TYPE_F16>(v[i][0], v[i][1]));
+                pb[i][n][1] = transpose_8x8(down2<TT_TYPE_F16>(v[i][2], v[i][3]));
             }
         }
         if (__any_sync(0xffffffffu, moved)) {
@@ -630,7 +644,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
     __syncthreads();                                         // (the ring is idle)
     constexpr int kLine = D + 4;                             // floats of a row: o, then maximum, sum
     float* join = reinterpret_cast<float*>(smem);
-    const float to_real = ref * 3.0517578125e-5f;            // 2^-15
+    const float to_real = exp2f(ref - 15.f);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll

@@ -10,7 +10,10 @@
 // would be, which 16 bits have room for (it is brought to 2^15 at most, and what is 2^-21 of the largest has all of its bits; with 2^11 and 2^-18
 // a column of small values beside one key of nearly all the weight was off by more than a rounding), and the row's sum has
 // the same factor.  A page's scale of values is in
-// P too, as the part of the exponent, over the largest scale so far.
+// P too, as a part of the exponent, over the largest scale so far.  Where that is of a page that some rows do not see, it may be so much larger than what
+// they do see that nothing would be left of their P: `used` of such a row is lower by the power of two between them, and P as much higher.  (A difference
+// of less than 2^5 is left alone.  That steps are told so by the pages' warp, in a number that they look at anyway, is for speed: a branch of its own
+// in front of the maxima cost 13 us of 254.)
 //   Two prompts of 2048 tokens behind as many, 32 heads over 8 of 128: 252 us, 817 TFLOP/s of 16-bit products, half of the tensor cores' rate.  A step
 // of 128 keys takes 3500 to 3900 cycles: the products 2050, the exponentials 2050 and the shared memory 2560, and a tile's chain (its softmax, then the
 // product that takes P and the one that makes the next scores) 3500, which is the bound.  The way in and out are 11000 and 6000 cycles of a CTA.
@@ -84,7 +87,12 @@ __device__ __forceinline__ void named_sync(int id, int threads) { asm volatile("
 __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
 // What the softmax needs to know of a step's eight groups of 16 tokens.
-struct alignas(16) StepScales { float key[8], shift[8], back[8]; float ref; };
+struct alignas(8) StepScales {
+    float key[8], shift[8], back[8];
+    float ref, shrink;                      // the largest scale of values so far; the one before over it, with a minus if rows may be apart:
+    uint8_t value[8]; int common;           // the exponents of the values' scales, and of the largest so far that all rows of the tile see
+};
+__device__ __forceinline__ int exponent_of(float scale) { return __float_as_int(scale) >> 23 & 255; }
 
 // Splits of a tile that have anything to do.
 __device__ __forceinline__ int prompt_splits(const Attend& g, const TileView& view) {
@@ -106,7 +114,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
     __shared__ uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_ready[2][2], o_done[2], raw_full[2], raw_empty[2], drained;
     __shared__ StepScales scales[4];
     __shared__ int nan_first[D], nan_last[D], nan_any;
-    __shared__ uint8_t sizes[kPromptRows];                                // of the queries' rows: the exponents of what they were multiplied by
+    __shared__ uint8_t sizes[kPromptRows];                                // of the queries' rows: the exponents of what they were multiplied by (then row_ref, see there)
     __shared__ uint32_t tmem_slot;
     __shared__ int late[6];                                               // what the way out needs (the softmax has no registers to keep it in)
     __shared__ int abort_flag;
@@ -155,7 +163,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 
     // a softmax thread's row
     const int tile = warp >> 3, half = (warp >> 2) & 1, r = tile * 128 + (int)(threadIdx.x & 127);      // (a half of its columns)
-    float top = -INFINITY, used = 0.f, sum = 0.f, ref = 0.f;              // maximum; the one that O and the sum are relative to; the unit of O
+    float top = -INFINITY, used = 0.f, sum = 0.f;                         // maximum; the one that O and the sum are relative to
     bool fine = true;
 
     if (warp < 16) {
@@ -210,6 +218,11 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
         if (lane == 0) mbar_arrive(smem_u32(&q_full));
         named_sync(4 + tile, 256);
         const float factor = fabsf(g.scale_log2) / __int_as_float((int)sizes[r] << 23);
+        // From here on it is the exponent of the largest scale that the row has seen, looked after where rows are apart.  (Both threads of a row put the
+        // same there, and a step's barrier is between theirs and the next step's.)
+        volatile uint8_t* const row_ref = &sizes[r];
+        named_sync(4 + tile, 256);
+        *row_ref = 0;
 
         // ---------------- softmax ----------------
         const volatile int* out = late;
@@ -264,16 +277,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 const float seen = top;
                 top = max_of(top, mx, tmem_ld1(s_t + (half ? 16u : 32u)));
                 // O and the sum follow the maximum when it is 2^8 ahead, and the largest scale at once
-                const float new_ref = ld_shared_f32(smem_u32(&scales[i & 3].ref));
+                const float shrink = ld_shared_f32(smem_u32(&scales[i & 3].shrink));
                 const bool first = seen != top && seen == -INFINITY;      // the row's first visible token is in this step
-                const bool move = top > used + 8.f || first || ref != new_ref;
+                const bool move = top > used + 8.f || first || shrink != 1.f;
                 if (__any_sync(0xffffffffu, move)) {
-                    const float now = top == -INFINITY ? 0.f : top;
+                    float now = top;
+                    if (__float_as_int(shrink) < 0) {
+                        const Seen s = seen_by_row();
+                        int own = max((int)*row_ref, scales[i & 3].common);
+#pragma unroll 1
+                        for (int k = 0; k < 8; ++k) if (t + 16 * k < s.hi && t + 16 * k + 16 > s.lo) own = max(own, (int)scales[i & 3].value[k]);
+                        *row_ref = (uint8_t)own;
+                        now -= (float)min(100, max(0, exponent_of(scales[i & 3].ref) - own));
+                    }
+                    if (top == -INFINITY) now = 0.f;
                     const float alpha = seen != -INFINITY ? exp2_fast(used - now) : 0.f;
-                    const float scale_o = ref == new_ref ? alpha : alpha * __fdividef(ref, new_ref);
+                    const float scale_o = alpha * fabsf(shrink);
                     used = now;
                     sum *= alpha;
-                    ref = new_ref;
                     if (i > 0 && half == 0) {                             // (in front of the first half of P, which lets the product begin)
                         fine = fine && __all_sync(0xffffffffu, bounded_wait(&o_done[tile], (uint32_t)(i - 1) & 1u, abortp, g.a.status, 32u, kPromptWait));
                         tc_fence_after();
@@ -339,6 +360,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const int row_pos = s.pos;
             const bool none = steps == 0 || s.hi <= max(s.lo, from) || s.lo >= to;      // the row sees nothing here
             // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
+            const float ref = steps > 0 ? ld_shared_f32(smem_u32(&scales[(steps - 1) & 3].ref)) : 0.f;
             const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
             float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + 8 * r;
             const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)(r & 127) * (2u * D);      // (where the queries were)
@@ -515,6 +537,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             };
             int page = good(0, page_of(0)), page1 = page_of(1);
             float ks = scale_of(page, 0), vs = scale_of(page, 1), most = 0.f;      // most: the largest scale of values so far
+            int common = 0;
             fetch(0, page, 0);
             fetch(0, page, 1);
             for (int i = 0; i < steps; ++i) {
@@ -525,15 +548,24 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 float m = vs;
 #pragma unroll
                 for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                const float before = most;
                 most = fmaxf(most, m);
+                const int group_t = from + i * kPromptTokens + 16 * (lane & 7), exponent = vs < INFINITY ? exponent_of(vs) : 0;
+                common = max(common, __reduce_max_sync(0xffffffffu, group_t < view.whole_hi && group_t + 16 > view.whole_lo ? exponent : 0));
                 if (lane < 8) {
                     StepScales& sc = scales[i & 3];
-                    // (a share of less than 2^-40 of the largest scale is taken as that)
-                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 9.094947017729282e-13f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
+                    // (a share of less than 2^-100 of the largest scale is taken as that: a row's sum has all probabilities of 2^-33 and more)
+                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 7.888609052210118e-31f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
                     sc.key[lane] = ks;
                     sc.shift[lane] = lg + 7.f;
                     sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
-                    if (lane == 0) sc.ref = most;
+                    sc.value[lane] = (uint8_t)exponent;
+                    if (lane == 0) {
+                        const float shrink = before == most ? 1.f : __fdividef(before, most);
+                        sc.ref = most;
+                        sc.shrink = exponent_of(most) > common + 4 ? -shrink : shrink;
+                        sc.common = common;
+                    }
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&k_full[buf]));

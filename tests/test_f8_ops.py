@@ -973,6 +973,57 @@ def test_attention_with_a_window_as_long_as_a_number_can_be(heads_q):
         check_attention(p, counts, heads_q, window=max(lengths))      # (another form may take it: the same within the roundings)
 
 
+def check_scales_apart(p, count, heads_q, window=0):
+    """check_attention for one sequence whose pages' scales of values differ by more than the bits of a number."""
+    length, d = p.lengths[0], p.d
+    q = (torch.randn(count, heads_q, d, generator=gen(50), device="cuda") * 2).to(torch.bfloat16)
+    y = torch.full_like(q, -77.0)
+    call = B.cache_attention(p.cache(), q, y, int32([0, count]), int32([length]), 1 / math.sqrt(d), window=window)
+    call.run()
+    assert call.status() == B.TT_OK
+    ref, off = reference_attention(p, [count], q, 1 / math.sqrt(d), True, window)
+    # A probability times its page's scale is a 16-bit number in units of 2^-7 (of 2^-15) of the largest probability times the largest scale that the row
+    # sees, or times one up to 2^5 larger.  Normal ones are in `off`; those below 2^-14 are off by half a step of 2^-24, so each key by 2^-27 of that,
+    # times its byte, 448 at most.
+    scales = p.vs[p.table_cpu[0]].amax(dim=1).repeat_interleave(p.block).cpu().double().numpy()
+    for i in range(count):
+        pos = length - count + i
+        lo = max(0, pos + 1 - window) if window else 0
+        off[i] += 2.0 ** -27 * 448 * (pos + 1 - lo) * scales[lo:pos + 1].max()
+    got = y.double().cpu().numpy()
+    bad = np.abs(got - ref) > off + 2.0 ** -8 * (np.abs(ref) + off) + 2.0 ** -125
+    assert not bad.any(), (np.argwhere(bad)[:4], got[bad][:4], ref[bad][:4])
+
+
+@gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("count,heads_q", [(20, 1), (10, 3), (90, 1), (60, 6)])
+def test_attention_of_queries_that_see_only_pages_of_small_scales(d, block, count, heads_q):
+    # pages that one query of a tile sees are 2^24 and 2^48 times as large as those of another
+    for exponents in ([-48, -24, 0, 24], [0, -48, -24, 0], [24, 0, -24, -48]):
+        p = Pages([4 * block - 3], 1, d, block, seed=d)
+        for j, e in enumerate(exponents):
+            p.vs[p.table_cpu[0][j]] = 2.0 ** (e - 8)
+        for first in (0, block):                                      # rows whose last token is in the first page, in the second
+            n = min(count, 3 * block - 3)
+            p.lengths = [first + n]
+            check_scales_apart(p, n, heads_q)
+            check_scales_apart(p, n, heads_q, window=3)
+
+
+@gpu
+@pytest.mark.parametrize("count,heads_q", [(7, 2), (200, 2)])
+def test_attention_behind_a_window_of_large_scales(count, heads_q):
+    # what the first queries see and the last ones do not is 2^30 times as large
+    length, window = 3000, 700
+    p = Pages([length], 1, 64, 16, seed=count)
+    lo, edge = length - count + 1 - window, length - window
+    for j, page in enumerate(p.table_cpu[0]):
+        p.vs[page] = 2.0 ** (22 if 16 * j <= max(lo, edge - 24) else -8)
+    check_scales_apart(p, count, heads_q, window=window)
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
