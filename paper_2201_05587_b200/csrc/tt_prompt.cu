@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             const bool none = steps == 0 || s.hi <= max(s.lo, from) || s.lo >= to;      // the row sees nothing here
             // O is in units of 2^7 and the largest scale; a split's part stays relative to its sum
             const float ref = steps > 0 ? ld_shared_f32(smem_u32(&scales[(steps - 1) & 3].ref)) : 0.f;
-            const float unit_o = ref * 0.0078125f * (active == 1 ? 1.f / sum : 1.f);
+            const float unit_o = 0.0078125f * (active == 1 ? 1.f / sum : 1.f);      // (the scale apart: 2^-126 times this is no normal number)
             float* left = g.partial + (place * g.splits + blockIdx.z) * kPart + 8 * r;
             const uint32_t line = q_s + (uint32_t)tile * S::kTile + (uint32_t)(r & 127) * (2u * D);      // (where the queries were)
 #pragma unroll 1
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     const int n = h + j, first = n % 64 / 8 * 8 * S::kAtoms + n / 64 * 8;      // the place of columns n .. n + 7 in the head
                     float x[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = none ? 0.f : __uint_as_float(v[j + e]) * unit_o;
+                    for (int e = 0; e < 8; ++e) x[e] = none ? 0.f : __uint_as_float(v[j + e]) * unit_o * ref;
                     if (nan_any) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e)

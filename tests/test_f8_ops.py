@@ -1024,6 +1024,23 @@ def test_attention_behind_a_window_of_large_scales(count, heads_q):
     check_scales_apart(p, count, heads_q, window=window)
 
 
+@gpu
+@pytest.mark.parametrize("exponent", [-126, -100, -60, 0, 60, 100])
+@pytest.mark.parametrize("count,heads_q", [(1, 4), (20, 1), (100, 1)])
+def test_attention_of_values_of_any_size(exponent, count, heads_q):
+    p = Pages([300], 1, 64, 16, seed=4)
+    p.vs.fill_(2.0 ** -7)
+    q = (torch.randn(count, heads_q, 64, generator=gen(1), device="cuda") * 2).to(torch.bfloat16)
+    want = check_attention(p, [count], heads_q, q=q).clone()
+    p.vs.fill_(2.0 ** exponent)
+    y = torch.empty_like(q)
+    B.cache_attention(p.cache(), q, y, int32([0, count]), int32([300]), 0.125).run()
+    want = want.double() * 2.0 ** (exponent + 7)
+    # the same bits but for another power of two, unless a result is no normal number of the type
+    normal = want.abs() >= 2.0 ** -126
+    assert torch.equal(y.double()[normal], want[normal]) and (y.double() - want).abs()[~normal].le(2.0 ** -133).all()
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
