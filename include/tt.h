@@ -533,7 +533,9 @@ tt_status tt_rotary_turns(const double* frequencies, size_t n, uint64_t* turns);
 /* A cache of keys (index 0) and values (1) in e4m3.  Page p holds `block` tokens of every head: the value i of slot t of head h is the byte
  * data[p * page + h * head + t * token + i] times scale[p * s_page + h * s_head].  Token j of sequence b is slot j % block of page
  * table[b * table_row + j / block].  data starts on a 16-byte boundary, page, head and token are multiples of 16; block is 16, 32, 64 or
- * 128; d is a multiple of 32 up to 256. */
+ * 128; d is a multiple of 32 up to 256.  Scales are finite and not negative (0 may count as 2^-126); one that is not finite makes the outputs of
+ * the queries that see its page NaN.  Any values will do, but a query keeps the bits of its outputs only of pages whose scales of values are no
+ * less than 2^-80 of the largest that the queries of its sequence see. */
 typedef struct tt_cache {
     void* data[2]; float* scale[2];
     int64_t page[2], head[2], token[2], s_page[2], s_head[2];

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kAttendWarps * 32, (AttendShape<D, NT>::kCtas)
             } else {
                 x.ks = c.scale[0][x.page * c.s_page[0] + head * c.s_head[0]];
                 const float vs = c.scale[1][x.page * c.s_page[1] + head * c.s_head[1]];
-                if (!(vs <= 1.17549435e-38f)) x.lg = log2f(vs);
+                if (!(vs <= 1.17549435e-38f)) x.lg = vs < INFINITY ? log2f(vs) : __int_as_float(0x7fffffff);
             }
         }
         return x;

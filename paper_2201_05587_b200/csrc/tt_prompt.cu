@@ -63,6 +63,11 @@ __device__ __forceinline__ float max_of(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
     return m;
 }
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
 __device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
     float2 r;
     asm("{\n\t.reg .b64 a, b;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 a, a, b;\n\tmov.b64 {%0, %1}, a;\n\t}"
@@ -89,8 +94,8 @@ __device__ __forceinline__ void named_arrive(int id, int threads) { asm volatile
 // What the softmax needs to know of a step's eight groups of 16 tokens.
 struct alignas(8) StepScales {
     float key[8], shift[8], back[8];
-    float ref, shrink;                      // the largest scale of values so far; the one before over it, with a minus if rows may be apart:
-    uint8_t value[8]; int common;           // the exponents of the values' scales, and of the largest so far that all rows of the tile see
+    float ref, shrink;                      // the largest scale of values so far; the one before over it, with a minus if rows are to be looked at on their own:
+    uint8_t value[8]; int common;           // the exponents of the values' scales (255: not finite), and of the largest so far that all rows of the tile see
 };
 __device__ __forceinline__ int exponent_of(float scale) { return __float_as_int(scale) >> 23 & 255; }
 
@@ -264,8 +269,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 for (int k = 2; k < 16; k += 2)
 #pragma unroll
                     for (int gr = 0; gr < 4; ++gr) m[gr] = max_of(m[gr], __uint_as_float(v[16 * gr + k]), __uint_as_float(v[16 * gr + k + 1]));
-                // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well)
-                const auto factor_of = [&](float key) { return fmaxf(factor * key, 1.17549435e-38f); };
+                // (a factor of 0, of a page of zeros, would make NaN of -inf: the smallest one does as well; NaN stays)
+                const auto factor_of = [&](float key) { return max_or_nan(factor * key, 1.17549435e-38f); };
                 keys = make_float4(factor_of(keys.x), factor_of(keys.y), factor_of(keys.z), factor_of(keys.w));
                 float mx = max_of(fmaxf(m[0] * keys.x, m[1] * keys.y), m[2] * keys.z, m[3] * keys.w);
                 // The halves tell each other their maxima in tensor memory, in a column that its writer has read and that nobody but the reader writes next.
@@ -285,8 +290,18 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     if (__float_as_int(shrink) < 0) {
                         const Seen s = seen_by_row();
                         int own = max((int)*row_ref, scales[i & 3].common);
+                        // (a scale that is not finite reaches the rows that see its page by their factor, and no others)
 #pragma unroll 1
-                        for (int k = 0; k < 8; ++k) if (t + 16 * k < s.hi && t + 16 * k + 16 > s.lo) own = max(own, (int)scales[i & 3].value[k]);
+                        for (int k = 0; k < 8; ++k) {
+                            const int value = scales[i & 3].value[k];
+                            const bool sees = t + 16 * k < s.hi && t + 16 * k + 16 > s.lo;
+                            if (sees && value < 255) own = max(own, value);
+                            else if ((k >> 1 & 1) == half) {
+                                const float f = sees ? __int_as_float(0x7fffffff) : 1.17549435e-38f;
+                                const int gr = (k & 1) + 2 * (k >> 2);
+                                keys = make_float4(gr == 0 ? f : keys.x, gr == 1 ? f : keys.y, gr == 2 ? f : keys.z, gr == 3 ? f : keys.w);
+                            }
+                        }
                         *row_ref = (uint8_t)own;
                         now -= (float)min(100, max(0, exponent_of(scales[i & 3].ref) - own));
                     }
@@ -545,17 +560,19 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                 const float ks1 = scale_of(next, 0), vs1 = scale_of(next, 1);
                 // the scales, before the keys report: what lay here four steps ago has been read
                 if (!wait(&k_empty[buf], ((uint32_t)(i >> 1) & 1u) ^ 1u, 42u)) break;
-                float m = vs;
+                const float value = vs < INFINITY ? vs : 0.f;
+                float m = value;
 #pragma unroll
                 for (int d = 4; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 const float before = most;
                 most = fmaxf(most, m);
-                const int group_t = from + i * kPromptTokens + 16 * (lane & 7), exponent = vs < INFINITY ? exponent_of(vs) : 0;
-                common = max(common, __reduce_max_sync(0xffffffffu, group_t < view.whole_hi && group_t + 16 > view.whole_lo ? exponent : 0));
+                const int group_t = from + i * kPromptTokens + 16 * (lane & 7), exponent = vs < INFINITY ? exponent_of(vs) : 255;
+                common = max(common, __reduce_max_sync(0xffffffffu, group_t < view.whole_hi && group_t + 16 > view.whole_lo && exponent < 255 ? exponent : 0));
+                const bool odd = __any_sync(0xffffffffu, exponent == 255 || !(ks < INFINITY));
                 if (lane < 8) {
                     StepScales& sc = scales[i & 3];
                     // (a share of less than 2^-100 of the largest scale is taken as that: a row's sum has all probabilities of 2^-33 and more)
-                    const float unit = most > 0.f ? fmaxf(__fdividef(vs, most), 7.888609052210118e-31f) : 1.f, lg = vs == most ? 0.f : log2f(unit);
+                    const float unit = most > 0.f ? fmaxf(__fdividef(value, most), 7.888609052210118e-31f) : 1.f, lg = value == most ? 0.f : log2f(unit);
                     sc.key[lane] = ks;
                     sc.shift[lane] = lg + 7.f;
                     sc.back[lane] = exp2_fast(-lg) * 0.0078125f;
@@ -563,7 +580,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
                     if (lane == 0) {
                         const float shrink = before == most ? 1.f : __fdividef(before, most);
                         sc.ref = most;
-                        sc.shrink = exponent_of(most) > common + 4 ? -shrink : shrink;
+                        sc.shrink = odd || exponent_of(most) > common + 4 ? -shrink : shrink;
                         sc.common = common;
                     }
                 }

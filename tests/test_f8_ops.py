@@ -1041,6 +1041,28 @@ def test_attention_of_values_of_any_size(exponent, count, heads_q):
     assert torch.equal(y.double()[normal], want[normal]) and (y.double() - want).abs()[~normal].le(2.0 ** -133).all()
 
 
+@gpu
+@pytest.mark.parametrize("which,scale", [("ks", math.nan), ("vs", math.nan), ("vs", math.inf)])
+@pytest.mark.parametrize("count,heads_q,d", [(4, 2, 64), (20, 1, 256), (100, 2, 64), (100, 1, 128)])
+@pytest.mark.parametrize("at", [0, 20, -1])                          # the page: the first, one in the middle, the last
+def test_attention_nan_scales_reach_the_rows_that_see_their_page(which, scale, count, heads_q, d, at):
+    p = Pages([450], 1, d, 16, seed=8)
+    q = torch.randn(count, heads_q, d, generator=gen(1), device="cuda").to(torch.float16)
+    for window in (0, 390):
+        clean = check_attention(p, [count], heads_q, q=q, window=window).clone()
+        page = p.table_cpu[0][at]
+        keep = getattr(p, which)[page].clone()
+        getattr(p, which)[page] = scale
+        y = torch.empty_like(q)
+        B.cache_attention(p.cache(), q, y, int32([0, count]), int32([450]), 1 / math.sqrt(d), window=window).run()
+        j = at % len(p.table_cpu[0])
+        pos = torch.arange(450 - count, 450, device="cuda")
+        sees = (16 * j <= pos) & ((16 * j + 16 > pos + 1 - window) if window else True)
+        assert torch.isnan(y[sees]).all()
+        assert torch.equal(y[~sees], clean[~sees])
+        getattr(p, which)[page] = keep
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
