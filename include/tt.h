@@ -500,8 +500,9 @@ typedef struct tt_quantize_args {
 tt_status tt_quantize(const tt_quantize_args* a, void* cuda_stream);
 
 /* y[m,nn] = act(bias[nn] + sum over blocks b of 128 columns of xs(m,b) ws(nn/128,b) sum_kk x[m,kk] w[nn,kk]): x [m,kk] and w [nn,kk] in e4m3,
- * xs a scale for each row and block, ws one for each 128 x 128 block, any values.  A block's products are summed by the tensor core,
- * blocks are added up in 32 bits.  x and w start on 16-byte boundaries and so do their rows (x_row, w_row multiples of 16).
+ * xs a scale for each row and block, ws one for each 128 x 128 block, any values with xs ws below 2^128.  A block's products are summed by the
+ * tensor core, blocks are added up in 32 bits, times xs ws, which is rounded to 32 bits first (below 2^-126 to a multiple of 2^-149: outputs below
+ * 2^-100 may show it).  kk is 1 at least.  x and w start on 16-byte boundaries and so do their rows (x_row, w_row multiples of 16).
  * bias may be NULL.  Deterministic. */
 typedef struct tt_dense_quantized_args {
     const void* x; const void* w; const float* x_scale; const float* w_scale; const float* bias; void* y; uint32_t* status;

@@ -1063,6 +1063,24 @@ def test_attention_nan_scales_reach_the_rows_that_see_their_page(which, scale, c
         getattr(p, which)[page] = keep
 
 
+@gpu
+@pytest.mark.parametrize("m,n,k", [(5, 300, 1300), (40, 700, 300), (200, 300, 900), (300, 1000, 260), (3000, 2000, 300)])
+@pytest.mark.parametrize("xe,we", [(-126, -17), (-17, -126), (-149, 10), (-126, 0), (-126, 120), (100, 1)])
+def test_dense_scales_of_the_smallest_and_largest_products(m, n, k, xe, we):
+    x, _, w, _ = dense_case(m, n, k, 9)
+    kb, nb = -(-k // 128), -(-n // 128)
+    xs = ((1 + torch.rand(kb, m, generator=gen(3), device="cuda").double()) * 2.0 ** xe).float()
+    ws = ((1 + torch.rand(nb, kb, generator=gen(4), device="cuda").double()) * 2.0 ** we).float()
+    y = torch.empty(m, n, device="cuda")
+    call = B.dense_quantized(x, xs, w, ws, y)
+    call.run()
+    assert call.status() == B.TT_OK
+    ref, most = dense_reference(x, xs, w, ws, None)
+    # the products, the two scales and the additions in 32 bits; a product of scales below 2^-126 is off by 2^-150 at most, and a block's sum is 2^25 at most
+    off = most * ADD * (128 + 3 * (kb + 1)) + (kb * 2.0 ** -125 if xe + we < -126 else 0)
+    assert (np.abs(y.double().cpu().numpy() - ref) <= off).all()
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
