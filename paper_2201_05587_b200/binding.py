@@ -594,21 +594,30 @@ def dense_static_scratch(x, w, bias, y, act, rec):
 class Call:
     """One call of an 8-bit operator: ``run`` enqueues it on the current stream of its tensors' device, ``status`` reads what only the
     device has seen.  A call that has a status word or a workspace is made outside of stream captures; its runs share them, so they
-    follow each other: the caller orders them when they go to different streams."""
+    follow each other: the caller orders them when they go to different streams.  It may be dropped while runs are under way on any stream; a
+    captured one is kept as long as the graph is replayed, and the tensors that it was made of belong to the caller as ever."""
 
-    def __init__(self, name, args, keep, device, status=None):
+    def __init__(self, name, args, keep, device, status=None, workspace=None):
         lib()
         self.name, self.args, self._keep, self._status = name, args, keep, status
         self._device, self._index = device, device.index
         self._address = C.cast(getattr(_lib, name), C.c_void_p).value
+        # the call's own device words, and the streams that their memory waits for when it is given back
+        self._words = [t for t in (status, workspace) if t is not None]
+        self._streams = {_torch._C._cuda_getCurrentRawStream(self._index)} if self._words else None
 
     def run(self):
         torch = _torch
+        stream = torch._C._cuda_getCurrentRawStream(self._index)
+        if self._words and stream not in self._streams:
+            for t in self._words:
+                t.record_stream(torch.cuda.current_stream(self._device))
+            self._streams.add(stream)
         if torch.cuda.current_device() == self._index:
-            st = _call.call(self._address, self.args, torch._C._cuda_getCurrentRawStream(self._index))
+            st = _call.call(self._address, self.args, stream)
         else:
             with torch.cuda.device(self._index):
-                st = _call.call(self._address, self.args, torch._C._cuda_getCurrentRawStream(self._index))
+                st = _call.call(self._address, self.args, stream)
         if st != TT_OK:
             raise TTError(st, self.name)
 
@@ -816,7 +825,7 @@ def cache_attention(cache, q, y, starts, lengths, scale, causal=True, window=0, 
     _check(lib().tt_cache_attention_workspace(C.byref(a), C.byref(n)), "tt_cache_attention")
     workspace = _device_words(device, n.value)
     a.workspace, a.workspace_bytes = workspace.data_ptr(), n.value
-    return Call("tt_cache_attention", a, (cache, q, y, starts, lengths, workspace), device, status)
+    return Call("tt_cache_attention", a, (cache, q, y, starts, lengths), device, status, workspace)
 
 
 def transfer_tune(workloads, tensor_sets, pool, opts: tt_tune_opts | None = None):

@@ -1081,6 +1081,31 @@ def test_dense_scales_of_the_smallest_and_largest_products(m, n, k, xe, we):
     assert (np.abs(y.double().cpu().numpy() - ref) <= off).all()
 
 
+@gpu
+def test_words_of_a_call_stay_until_its_runs_on_other_streams_are_done():
+    p = Pages([6000], 1, 64, 64, seed=1)
+    q = torch.randn(1, 4, 64, generator=gen(1), device="cuda").to(torch.float16)
+    y, starts, lengths = torch.empty_like(q), int32([0, 1]), int32([6000])
+    want = check_attention(p, [1], 4, q=q, scale=0.1)
+    call = B.cache_attention(p.cache(), q, y, starts, lengths, 0.1)
+    held, n = call.args.workspace, call.args.workspace_bytes
+    word = call.args.status
+    assert n > 0
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1 << 28)
+        call.run()
+        done = torch.cuda.Event()
+        done.record()
+    del call
+    while_it_runs = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(4)] + [torch.empty(4, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    assert not done.query()                                           # (the run is still to come)
+    assert held not in [t.data_ptr() for t in while_it_runs] and word not in [t.data_ptr() for t in while_it_runs]
+    side.synchronize()
+    assert torch.equal(y, want)
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
