@@ -1106,6 +1106,41 @@ def test_words_of_a_call_stay_until_its_runs_on_other_streams_are_done():
     assert torch.equal(y, want)
 
 
+@gpu
+@pytest.mark.parametrize("which", ["k", "v"])
+@pytest.mark.parametrize("count,heads_q,d,length,window", [
+    (12, 2, 64, 80, 0), (30, 1, 128, 200, 0), (14, 2, 160, 100, 0), (9, 3, 256, 90, 0), (40, 2, 256, 90, 0),                    # few rows of a tile, long heads
+    (12, 2, 64, 200, 50), (30, 1, 128, 200, 70), (9, 3, 256, 300, 33), (60, 2, 32, 200, 40),                                    # ... behind a window
+    (4, 2, 64, 5000, 0), (4, 2, 64, 5000, 3000), (90, 2, 64, 900, 600), (90, 2, 96, 900, 600), (100, 1, 128, 1200, 700),        # splits; prompts behind a window
+    (70, 2, 64, 6000, 0), (70, 2, 128, 6000, 0), (70, 2, 64, 6000, 3000), (33, 1, 32, 4000, 2500)])                             # prompts in splits
+def test_attention_nan_reaches_the_rows_that_see_it_in_every_form(which, count, heads_q, d, length, window):
+    p = Pages([length], 1, d, 16, seed=8)
+    data, col = (p.k, 3) if which == "k" else (p.v, d - 5)
+    q = torch.randn(count, heads_q, d, generator=gen(1), device="cuda").to(torch.float16)
+    clean = check_attention(p, [count], heads_q, q=q, window=window).clone()
+    pos = torch.arange(length - count, length, device="cuda")
+    # seen from the middle of the queries on, by the last alone, by all; behind a window by the first, by the first ones; by none
+    places = [length - count // 2, length - 1, (length - count) // 2] + ([length - count + 1 - window, length - window - count // 2, length - count - window] if window else [])
+    for at in places:
+        page, slot = p.table_cpu[0][at // 16], at % 16
+        keep = data.view(torch.uint8)[page, 0, slot, col].clone()
+        data.view(torch.uint8)[page, 0, slot, col] = 0xff
+        y = torch.full_like(q, -77.0)
+        call = B.cache_attention(p.cache(), q, y, int32([0, count]), int32([length]), 1 / math.sqrt(d), window=window)
+        call.run()
+        assert call.status() == B.TT_OK
+        sees = (at <= pos) & ((at > pos - window) if window else True)
+        nan = torch.isnan(y)
+        want = torch.zeros_like(nan)
+        if which == "k":
+            want[sees] = True
+        else:
+            want[sees, :, col] = True
+        assert torch.equal(nan, want), at
+        assert torch.equal(y[~want], clean[~want]), at
+        data.view(torch.uint8)[page, 0, slot, col] = keep
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
