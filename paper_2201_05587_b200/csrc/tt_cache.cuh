@@ -145,7 +145,6 @@ __device__ __forceinline__ void read_shared(uint32_t addr, uint32_t (&v)[N / 4])
 }
 // A non-zero byte for each e4m3 byte of the word that is NaN.
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
-// Four values of a 16-bit type.
 // Four 16-bit values as they lie in memory, and as 32-bit ones.
 __device__ __forceinline__ uint2 raw_four(const void* p, long long i, int wide) {
     const uint16_t* x = static_cast<const uint16_t*>(p) + i;
@@ -161,7 +160,6 @@ __device__ __forceinline__ void four_of(uint2 u, int type, float (&v)[4]) {
     const float2 a = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.x) : up2<TT_TYPE_BF16>(u.x), b = type == TT_TYPE_F16 ? up2<TT_TYPE_F16>(u.y) : up2<TT_TYPE_BF16>(u.y);
     v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
 }
-__device__ __forceinline__ void load_four(const void* p, long long i, int type, int wide, float (&v)[4]) { four_of(raw_four(p, i, wide), type, v); }
 __device__ __forceinline__ void store_four(void* p, long long i, int type, int wide, const float (&v)[4]) {
     if (wide) {
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =

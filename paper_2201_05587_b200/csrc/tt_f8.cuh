@@ -83,10 +83,6 @@ __device__ __forceinline__ void store_wide(void* p, const float (&v)[N]) {
     }
 }
 // One value of a type known at run time.
-__device__ __forceinline__ float load_one(const void* p, long long i, int type) {
-    return type == TT_TYPE_F32 ? static_cast<const float*>(p)[i] : type == TT_TYPE_F16 ? __half2float(static_cast<const __half*>(p)[i])
-                                                                                       : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-}
 __device__ __forceinline__ void store_one(void* p, long long i, int type, float v) {
     if (type == TT_TYPE_F32) static_cast<float*>(p)[i] = v;
     else if (type == TT_TYPE_F16) static_cast<__half*>(p)[i] = __float2half_rn(v);

@@ -74,10 +74,6 @@ __device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
         : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-__device__ __forceinline__ void tmem_ld8u(uint32_t taddr, uint32_t* v) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]) : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ float2 ld_shared_v2f(uint32_t addr) {
     float2 v;
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
@@ -316,8 +312,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
 #pragma unroll 1
                         for (int h = 0; h < D; h += 16) {                 // (few at a time: the scores are in registers)
                             uint32_t o[16];
-                            tmem_ld8u(o_t + (uint32_t)h, o);
-                            tmem_ld8u(o_t + (uint32_t)h + 8u, o + 8);
+                            tmem_ld8(o_t + (uint32_t)h, o);
+                            tmem_ld8(o_t + (uint32_t)h + 8u, o + 8);
                             tmem_wait_ld();
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scale_o);
@@ -383,8 +379,8 @@ __global__ void __launch_bounds__(kPromptThreads, 1) tt_attend_prompt_kernel(con
             for (int h = half * (D / 2); h < (half + 1) * (D / 2); h += 16) {
                 uint32_t v[16];
                 if (steps > 0) {
-                    tmem_ld8u(o_t + (uint32_t)h, v);
-                    tmem_ld8u(o_t + (uint32_t)h + 8u, v + 8);
+                    tmem_ld8(o_t + (uint32_t)h, v);
+                    tmem_ld8(o_t + (uint32_t)h + 8u, v + 8);
                     tmem_wait_ld();
                 }
 #pragma unroll
