@@ -239,7 +239,8 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
     __syncthreads();
     if (g.split > 1) cluster_arrive();                      // (this CTA's barriers and landing place exist)
     // Tensor memory is taken behind the wait for the launch in front and before the next one may begin: a CTA that waits for a launch holds none that
-    // the launch could be waiting for.  The copies do not wait for it.
+    // the launch could be waiting for.  Nor does one hold any while it waits for the peers of its cluster: a peer may be waiting for what another
+    // stream's CTA holds on its SM, and that one's own peer for this CTA's.  The copies do not wait for it.
     pdl_wait_prev();
     constexpr uint32_t kTmemCols = kBufs * TN < 32 ? 32 : kBufs * TN;
     uint32_t tmem_base = 0u;
@@ -390,7 +391,13 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
                 for (int j = 0; j < kCols; j += 4) st_shared_v4(base + r * kLine + (uint32_t)(half * kCols + j) * 4u, acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
             }
             fence_proxy_async_shared();
-            asm volatile("bar.sync 2, 256;" ::: "memory");
+            tc_fence_before();
+            asm volatile("bar.sync 2, 288;" ::: "memory");
+        } else if (warp == 1) {
+            __syncwarp();
+            asm volatile("bar.sync 2, 288;" ::: "memory");
+            tc_fence_after();
+            tmem_dealloc(tmem_base, kTmemCols);
         }
         __syncwarp();
         if (g.split > 1) cluster_wait();                    // the peers are there
@@ -433,12 +440,14 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
             cluster_wait();
         }
     }
-    tc_fence_before();
-    __syncthreads();
-    if (warp == 1) {
-        __syncwarp();
-        tc_fence_after();
-        tmem_dealloc(tmem_base, kTmemCols);
+    if ((SWAP || kAlone) && g.split == 1) {
+        tc_fence_before();
+        __syncthreads();
+        if (warp == 1) {
+            __syncwarp();
+            tc_fence_after();
+            tmem_dealloc(tmem_base, kTmemCols);
+        }
     }
 }
 

@@ -1141,6 +1141,39 @@ def test_attention_nan_reaches_the_rows_that_see_it_in_every_form(which, count, 
         data.view(torch.uint8)[page, 0, slot, col] = keep
 
 
+@gpu
+def test_dense_beside_a_layer_that_takes_all_tensor_memory():
+    # Clusters of two kernels on two streams, of which an SM has room for a CTA of each but not for their tensor memory: neither waits for a peer that waits
+    # for what it holds.
+    from paper_2201_05587_b200 import workloads as W
+    spec = W._dense(512, 256, 512, act=B.TT_ACT_NONE, name="beside")
+    wl = spec.workload()
+    info = wl.apply(B.make_record(B.TT_FAMILY_GEMM_TC, tile_n=64, tile_k=32, stages=2, split_k=4, mma_m_axis=1, acc_split=8))
+    assert info.tmem_cols == 512 and info.legal.split_k == 4
+    t, tensors = W.device_tensors(spec, W.make_inputs(spec, 1))
+    x, xs, w, ws = dense_case(8, 4096, 4096)
+    y = torch.empty(8, 4096, device="cuda")
+    call = B.dense_quantized(x, xs, w, ws, y)
+    call.run()
+    wl.run(tensors)
+    torch.cuda.synchronize()
+    want = y.clone(), t["y"].clone()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        y.zero_()
+        t["y"].zero_()
+        torch.cuda.synchronize()
+        for _ in range(20):
+            with torch.cuda.stream(streams[0]):
+                call.run()
+            with torch.cuda.stream(streams[1]):
+                wl.run(tensors)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(t["y"], want[1])
+    assert call.status() == B.TT_OK and wl.status() == B.TT_OK
+    wl.close()
+
+
 # ---- GPU: together, as a program uses them ------------------------------------------------------------------------------
 class Layer:
     """One attention block of a decoder whose weights and cache are in e4m3: quantise, project, turn, append, attend, quantise, project."""
