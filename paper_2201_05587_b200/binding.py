@@ -811,7 +811,8 @@ def cache_append(cache, k, v, starts, lengths) -> Call:
 
 def cache_attention(cache, q, y, starts, lengths, scale, causal=True, window=0, max_count=0, max_length=0) -> Call:
     """tt_cache_attention: y [tokens, heads_q, d] of the queries q [tokens, heads_q, d] (float16 or bfloat16) over the cache, batched as in
-    cache_append.  max_count and max_length: bounds on a sequence's queries and on the lengths, where the program knows them."""
+    cache_append.  max_count and max_length: bounds on a sequence's queries and on the lengths, where the program knows them; single tokens
+    want max_count=1 (without it 64 of them over 4096 tokens take 195 us for 114)."""
     _need(q.dim() == 3 and y.shape == q.shape and y.dtype == q.dtype and q.shape[2] == cache.c.d, "q and y [tokens, heads_q, d] of the cache")
     cache._batch(starts, lengths)
     device = _same_device(q, y, starts, lengths, *cache.keep)

@@ -158,12 +158,12 @@ __global__ void __launch_bounds__(WARP ? 256 : kAppendThreads, WARP ? 3 : 7) tt_
 // columns; which keys, and which columns, is chosen so that the swizzled lines of a box are read without bank conflicts.  Boxes arrive by TMA in
 // a ring of the warp's own, so the loop has no barrier but theirs.  (Copied by the lanes, 16 bytes each, they were bound by what the load
 // unit takes, 4 TB/s.)
-//   e4m3 -> 16-bit floating point is exact, and so is a row of queries: brought to a maximum of 2^14..2^15 by a power of two, which the
-// scores' factor takes back.  What a probability is rounded to 11 bits as has the scale of the page's values in it, and the running maximum is one of
+//   e4m3 -> 16-bit floating point is exact, and so is a row of queries but for what is below 2^-29 of its largest: brought to a maximum of 2^14..2^15
+// by a power of two, which the scores' factor takes back.  What a probability is rounded to 11 bits as has the scale of the page's values in it, and the running maximum is one of
 // scores with those scales: it is of each row's own tokens, so that no page that only another row sees takes bits from it. 2^-29 of the
 // largest still has all of them; sums are in 32 bits.
 //   The keys of a sequence are split over CTAs, of which the last to finish adds up what all have left in the workspace, in their order.
-//   (64 sequences of up to 8192 tokens, 32 heads over 8 of 128: 117 us, 5.3 TB/s, 0.81 of a copy's rate; one of 131072 tokens: 54 us, 0.76.)
+//   (64 sequences of up to 8192 tokens, 32 heads over 8 of 128: 119 us, 5.1 TB/s, 0.79 of a copy's rate; one of 131072 tokens: 54 us, 0.76.)
 
 constexpr int kRun = 64;                    // tokens that a warp takes in a row
 constexpr int kAttendWarps = 4;
@@ -231,7 +231,7 @@ struct AttendShape {
 // The tokens of a split.  Only the device knows the lengths: the split that deals all sequences' tokens to the CTAs that the SMs hold at once, less a
 // fifth, as every sequence has a last split that is not full.  (8 sequences of up to 16384 tokens: 34 us so; by the longest that there may be 42.)  No
 // less than what the grid has room for, nor than what makes the join, which reads 14 bytes a cycle, as long as a split, whose warps take some
-// 8 + 6 NT cycles a token.  (One sequence of 14353 tokens, 8 rows of 128: 19 splits 16.3 us, 57 of them 19.0.)
+// 8 + 6 NT cycles a token.  (One sequence of 14353 tokens, 8 rows of 128: 19 splits 16 us, 57 of them 19.)
 struct Lane { int start, next, length; };                    // of sequence `lane`
 __device__ __forceinline__ Lane lane_of(const Attend& g) {
     const int b = threadIdx.x & 31;

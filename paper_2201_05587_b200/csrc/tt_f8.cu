@@ -12,7 +12,7 @@ namespace tt {
 //
 // s = 2^ceil(log2(max |x| / 448)) comes from the bits of the maximum, x / s is a product with the power 1 / s, so the only rounding is the
 // one to e4m3.  Bound by memory: every value is read once and kept in registers between the maximum and the conversion.
-// (8192 x 4096 in 16 bits: 19.0 us, 5.3 TB/s, 0.82 of a copy's rate.  A row: 2.7 us, the rate of launches.)
+// (8192 x 4096 in 16 bits: 19.0 us, 5.3 TB/s, 0.82 of a copy's rate.  A row: 2.5 to 2.8 us, the rate of launches.)
 
 // Rows of activations: a warp has one block of columns of eight rows, of four at a time, so that the scales of a block come out side by side.  Eight
 // lanes have a row's block, 8 values of either half each (a warp's loads are whole lines).
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(256) tt_quantize_lines_kernel(const tt_quantiz
     }
 }
 
-// Blocks of 128 x 128: a CTA each, a thread has 8 columns of every sixteenth row.
+// Blocks of 128 x 128: a CTA each, a thread has 8 columns of every sixteenth row.  (4096 x 4096 in 16 bits: 11.7 us; weights are quantised once.)
 template <int TYPE>
 __global__ void __launch_bounds__(256) tt_quantize_blocks_kernel(const tt_quantize_args a, int blocks, int wide) {
     __shared__ float warp_most[8];
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(256) tt_quantize_blocks_kernel(const tt_quanti
 //
 // Rows on the 128 lanes are the tokens, or (SWAP) the weights' rows where there are too few tokens to fill them.  `split` CTAs of
 // a cluster share a tile's blocks where there are fewer tiles than SMs, leave their sums in shared memory and add up a band of columns each,
-// in the order of the splits.  (8 x 4096 x 4096: 5.7 us, 2.9 TB/s with the launch, whose own share is 3 us; 333 x 1000 x 1960: 8.6 us.)
+// in the order of the splits.  (8 x 4096 x 4096: 5.8 us, 2.9 TB/s with the launch, whose own share is 3 us; 333 x 1000 x 1960: 9.2 us.)
 
 struct DenseF8 {
     const float* a_scale; long long as_row, as_block;     // of operand A's rows (normal: per row, SWAP: per 128 rows)
@@ -455,7 +455,9 @@ tt_dense_f8_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_cons
 // tcgen05.mma.cta_group::2 reads both CTAs', so an SM takes in (128 + TN / 2) * 128 bytes for 128 * TN * 128 products: 64 bytes a cycle at the tensor
 // core's rate, which is what an SM can get from the L2 (a 128 x 128 tile of one CTA needs twice that).  Two accumulators; the
 // sixteen read-out warps have a quarter of a block's sums each, 4 warps a scheduler, so that one waits for tensor memory while another adds.
-// (8192 x 4096 x 4096: 127 us at full clocks, 2.2 PFLOP/s; 150 us, 1.8 PFLOP/s, when repeated until the power limit sets the clock.)
+// (8192 x 4096 x 4096: 127 us at full clocks, 2.2 PFLOP/s; 150 us, 1.8 PFLOP/s, when repeated until the power limit sets the clock.  The read-out is
+// the bound: a compare and a select more for each block of it are 7 us, and the tensor cores are busy for 58 % of the time.  At 256 columns a thread
+// spills 49 words.)
 constexpr int kPairThreads = 128 + 512;                    // a warpgroup of TMA and MMA, four of read-out (96 registers each at launch; 32 and 112)
 constexpr unsigned kPairStaging = 16 * 4096;                // a block of 32 rows x 128 bytes for each read-out warp
 constexpr int kPairSmem = 230400;

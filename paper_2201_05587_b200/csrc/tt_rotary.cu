@@ -6,7 +6,7 @@
 //
 // A thread has the pairs of one 16-byte piece of a head (or of two, in the layout of halves), takes their sines once, and goes through every
 // head_step-th head with them: bound by memory, as long as the sines (some 40 instructions a pair) are shared by enough heads.  (8192 tokens, 40 heads
-// of 128, half of each turned: 29.4 us, 5.7 TB/s, 0.88 of a copy's rate.  16 tokens: 3.0 us.)
+// of 128, half of each turned: 29.4 us, 5.7 TB/s, 0.88 of a copy's rate.  16 tokens: 2.8 to 3.1 us.)
 #include <cuda_runtime.h>
 #include <cmath>
 #include "tt_ptx.cuh"
